@@ -25,6 +25,7 @@
  *
  * Serialized format (schema "byoc-subgraph", version 1), a JSON object:
  *   "inputs":    [{"name", "shape", "dtype": "f32"|"bf16", "layout": "NCHW"|"ROWMAJOR"}]
+ *                or {"name", "shape": [n], "dtype": "i32"}: positions or lengths
  *   "constants": [{"name", "index", "shape", "dtype"}]   index into the
  *                constant array passed to create; conv weights OIHW, dense
  *                weights [out, in], biases [out]
@@ -45,6 +46,45 @@
  *                     along channels (attrs axis 1), each with a multiple of
  *                     8 channels; bf16 graphs
  *   add[_relu|_relu6|_leaky] two tensors of one shape
+ * Composites of transformer layers, on row-major tensors (a row per token) of
+ * bf16 and f32 graphs:
+ *   qdense[_bias][_add][_relu|_relu6|_gelu|_leaky]   data [M,K], weight [N,K]
+ *                     dense on 8-bit codes with a scale for each token and
+ *                     output channel: with a_m = max_k |x_mk|, b_n = max_k |w_nk|,
+ *                     sum_k rint(127 x_mk / a_m) rint(127 w_nk / b_n) exactly
+ *                     in int32, times (a_m / 127)(b_n / 127), then bias,
+ *                     residual and activation.  A row that holds an infinity or a
+ *                     NaN gives NaN.  K <= 131072.
+ *   rotary            data [M,C], positions [M] (i32) -> [M, (heads + kv_heads) D]
+ *                     turns the first `rotary_dim` columns of each of the
+ *                     leading heads + kv_heads heads of D columns of a row; the columns
+ *                     after those heads (values of a packed projection) are not read.
+ *       attrs heads, kv_heads (default 0), head_dim D (even, at most 512),
+ *       rotary_dim (even, default D), layout "half" (pairs i, i + rotary_dim / 2;
+ *       default) or "interleaved" (2i, 2i + 1), base (default 10000), scaling
+ *       {"type": "linear"|"ntk"|"yarn", "factor" >= 1, and for yarn
+ *       "original_length", "beta_fast" (32), "beta_slow" (1),
+ *       "attention_factor" (0.1 ln(factor) + 1)} for contexts longer than
+ *       trained on.  Pair i turns by position * base^(-2i / rotary_dim), exactly for
+ *       every 32-bit position.
+ *   qk_norm_rotary    data, query weight [D][, key weight [D] if kv_heads > 0],
+ *                     positions: the same after x / sqrt(mean(x^2) + eps) * weight
+ *                     over each head; also attrs eps (default 1e-6)
+ *   attention         queries [B Lq, *], keys [B Lk, *], values [B Lk, *]
+ *                     -> [B Lq, heads D]: softmax(scale q k^T) v of heads that
+ *                     lie side by side in the rows, query head h with key
+ *                     head h / (heads / kv_heads); Lq and Lk may differ
+ *                     (cross attention, single tokens), and several inputs
+ *                     may be one tensor (a packed projection).
+ *       attrs batch B, heads, kv_heads (default heads, a divisor of it), head_dim D
+ *       (multiple of 8, at most 256), scale (default D^-1/2), causal (default
+ *       false: with it query i of a sequence of n keys sees the first
+ *       n - Lq + i + 1), q_col, k_col, v_col (first column of the heads, a multiple
+ *       of 8, default 0).  f32 rows have a multiple of 4 columns.
+ *   attention_lengths also lengths [B] (i32): sequence b has min(max(n, 0), Lk)
+ *                     keys; what its further rows hold does not matter.
+ *                     A query that sees no key gives zeros.
+ * Buffers that these composites read or write directly are aligned to 16 bytes.
  * A leaky ReLU (suffix _leaky) takes its slope from attrs alpha in [0, 1)
  * (default 0.1).
  * All nodes of a graph share one out_dtype, the graph's compute type:
@@ -101,7 +141,8 @@ typedef enum {
   BYOC_ERR_INTERNAL = 7
 } byoc_status;
 
-typedef enum { BYOC_F32 = 0, BYOC_BF16 = 1 } byoc_dtype;
+/* BYOC_I32: index inputs only (token positions, sequence lengths). */
+typedef enum { BYOC_F32 = 0, BYOC_BF16 = 1, BYOC_I32 = 3 } byoc_dtype;
 typedef enum { BYOC_NCHW = 0, BYOC_NHWC = 1, BYOC_ROWMAJOR = 2 } byoc_layout;
 
 /* One constant handed to create: host memory, C-contiguous, in the layout
@@ -134,7 +175,10 @@ typedef enum {
   BYOC_K_ADD = 5,       /* standalone elementwise add                   */
   BYOC_K_TRANSFORM = 6, /* boundary layout / dtype transform            */
   BYOC_K_REDUCE = 7,    /* split-K reduction with the fused epilogue    */
-  BYOC_K_CONV_I8 = 8    /* implicit-GEMM conv / dense on int8 MFMA      */
+  BYOC_K_CONV_I8 = 8,   /* implicit-GEMM conv / dense on int8 MFMA      */
+  BYOC_K_QDENSE = 9,    /* qdense: its rows' quantization and product   */
+  BYOC_K_ROTARY = 10,
+  BYOC_K_ATTENTION = 11
 } byoc_kernel_kind;
 
 /* One entry of the launch sequence a run enqueues.  Independent convolutions
@@ -216,7 +260,7 @@ byoc_status byoc_subgraph_num_io(const byoc_subgraph* g, int32_t* n_in, int32_t*
 byoc_status byoc_subgraph_io_desc(const byoc_subgraph* g, int32_t is_output, int32_t idx,
                                   byoc_tensor_desc* desc);
 
-/* Multiply-accumulates of the conv and dense composites (the cost measure
+/* Multiply-accumulates of the conv, dense and qdense composites (the cost measure
  * of the paper's TensorRT fallback rule, Sec. 4.1), bytes of packed
  * constants and bytes of the intermediate arena.  Any pointer may be NULL. */
 byoc_status byoc_subgraph_stats(const byoc_subgraph* g, int64_t* macs, int64_t* weight_bytes,

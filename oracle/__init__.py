@@ -26,11 +26,13 @@ graph  the JSON subgraph reader and executor, modes "exact" and "bf16io".
 brute  pure-Python scalar loops of the same definitions, for tiny shapes.
 quant  the affine int8 (partial quantization) definitions and an executor
        of int8 subgraphs.
+transformer  the transformer-layer operators (8-bit dense with a scale for each
+       row, rotation of heads with their norms, attention).
 
 Every function is pinned by a CPU test against something other than itself
 (brute force, closed forms, library routines, invariants); see tests/.
 """
 
 from .bf16 import round_bf16, bf16_bits  # noqa: F401
-from . import ops, graph, brute, quant  # noqa: F401
+from . import ops, graph, brute, quant, transformer  # noqa: F401
 from .graph import run_graph, run_node, load_graph  # noqa: F401

@@ -21,7 +21,11 @@ strides, padding, count_include_pad, default false: the divisor counts only
 positions inside the image), ``concatenate`` (any number of inputs joined
 along the channel axis), ``add[_relu|_relu6|_leaky]``; a leaky ReLU takes
 its slope from ``attrs.alpha`` (default 0.1).  Inputs of a node are listed in
-the order data, weight, bias, residual.
+the order data, weight, bias, residual.  Transformer-layer composites (module
+``transformer``): ``qdense`` with dense's suffixes (its weights are quantized as
+given, also in a bf16 graph), ``rotary`` (data, positions), ``qk_norm_rotary`` (data,
+query weight[, key weight], positions), ``attention`` (queries, keys, values) and
+``attention_lengths`` (also lengths); positions and lengths are i32 inputs.
 
 Precision semantics.  A node whose ``out_dtype`` is "bf16" belongs to a bf16
 graph: its activations are bf16 values, its weights are rounded to bf16 (ties
@@ -40,7 +44,7 @@ import json
 
 import numpy as np
 
-from . import ops
+from . import ops, transformer
 from .bf16 import round_bf16
 
 _ACTS = ("relu6", "relu", "gelu", "leaky")
@@ -55,11 +59,12 @@ def load_graph(js):
 
 def parse_composite(name):
     """Split a pattern name into (op, has_bias, has_add, activation)."""
-    if name in ("max_pool2d", "global_avg_pool2d", "avg_pool2d", "concatenate"):
+    if name in ("max_pool2d", "global_avg_pool2d", "avg_pool2d", "concatenate",
+                "rotary", "qk_norm_rotary", "attention", "attention_lengths"):
         return name, False, False, None
     parts = name.split("_")
     op = parts[0]
-    if op not in ("conv2d", "dense", "add"):
+    if op not in ("conv2d", "dense", "qdense", "add"):
         raise ValueError("unknown composite %r" % name)
     rest = parts[1:]
     act = None
@@ -102,11 +107,13 @@ def run_node(node, args, mode="bf16io"):
     dtype = node.get("out_dtype", "f32")
     op, has_bias, has_add, act = parse_composite(name)
     args = [np.asarray(a, dtype=np.float64) for a in args]
-    if op in ("conv2d", "dense"):
+    if op in ("conv2d", "dense", "qdense"):
         x, w = args[0], args[1]
-        if dtype == "bf16":
+        if dtype == "bf16" and op != "qdense":
             w = round_bf16(w)
-        if op == "conv2d":
+        if op == "qdense":
+            y = transformer.qdense(x, w)
+        elif op == "conv2d":
             y = ops.conv2d(x, w, tuple(attrs.get("strides", (1, 1))),
                            tuple(attrs.get("padding", (0, 0, 0, 0))),
                            int(attrs.get("groups", 1)))
@@ -130,6 +137,10 @@ def run_node(node, args, mode="bf16io"):
                            tuple(attrs.get("strides", (1, 1))),
                            tuple(attrs.get("padding", (1, 1, 1, 1))),
                            bool(attrs.get("count_include_pad", False)))
+    elif op in ("rotary", "qk_norm_rotary"):
+        y = transformer.rotary(attrs, args[0], args[-1], args[1:-1] if op == "qk_norm_rotary" else None)
+    elif op in ("attention", "attention_lengths"):
+        y = transformer.attention(attrs, *args)
     elif op == "concatenate":
         y = ops.concatenate(args, axis=1)
     else:
@@ -167,7 +178,7 @@ def run_graph(graph, consts, inputs, mode="bf16io", keep=False):
         if list(a.shape) != list(desc["shape"]):
             raise ValueError("input %s: shape %s != %s" % (desc["name"], a.shape, desc["shape"]))
         consumer = _graph_dtype_of_consumers(g, desc["name"])
-        if desc.get("dtype") == "bf16" or consumer == "bf16":
+        if desc.get("dtype") != "i32" and (desc.get("dtype") == "bf16" or consumer == "bf16"):
             a = round_bf16(a)
         vals[desc["name"]] = a
     for c in g.get("constants", []):

@@ -16,7 +16,8 @@ LIB = os.path.join(PKG, "libbyoc.so")
 ROOT = os.path.dirname(PKG)
 
 SOURCES = ["json.cpp", "graph.cpp", "capi.cpp", "engine.cpp", "conv_mfma.hip", "conv_dma.hip", "conv_pipe.hip", "conv_few.hip", "conv_halo.hip", "bottleneck.hip", "ir_block.hip", "stem.hip", "dense_rows.hip", "conv_f32.hip", "conv_f32_mfma.hip",
-           "vector_ops.hip", "layout.hip", "conv_i8.hip", "quant.hip", "static_scratch.hip"]
+           "vector_ops.hip", "layout.hip", "conv_i8.hip", "quant.hip", "static_scratch.hip",
+           "qdense.hip", "rotary.hip", "attention.hip"]
 
 # -packed-fp32-ops: keep the compiler from emitting packed fp32 ALU ops.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall",

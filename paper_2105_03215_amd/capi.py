@@ -14,10 +14,10 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libbyoc.so")
 
 BYOC_OK = 0
-F32, BF16 = 0, 1
+F32, BF16, I32 = 0, 1, 3
 NCHW, NHWC, ROWMAJOR = 0, 1, 2
 KIND_NAMES = ["conv_mfma", "conv_f32", "depthwise", "maxpool", "avgpool", "add", "transform",
-              "reduce", "conv_i8"]
+              "reduce", "conv_i8", "qdense", "rotary", "attention"]
 STATUS_NAMES = ["OK", "INVALID_ARG", "PARSE", "UNSUPPORTED", "SHAPE", "DEVICE", "OOM", "INTERNAL"]
 
 # Every entry point declared in include/byoc.h.
@@ -151,7 +151,7 @@ def _ptr(t):
     return t.data_ptr()
 
 
-_ELEM_DTYPE = {"bf16": "torch.bfloat16", "f32": "torch.float32"}
+_ELEM_DTYPE = {"bf16": "torch.bfloat16", "f32": "torch.float32", "i32": "torch.int32"}
 
 
 def _check_tensor(t, desc, device, what):
@@ -202,7 +202,7 @@ class Subgraph:
     def io_desc(self, is_output, idx):
         d = TensorDesc()
         _check(self.lib.byoc_subgraph_io_desc(self.handle, int(is_output), int(idx), ctypes.byref(d)))
-        return {"dtype": "bf16" if d.dtype == BF16 else "f32",
+        return {"dtype": {F32: "f32", BF16: "bf16", I32: "i32"}[d.dtype],
                 "layout": ["NCHW", "NHWC", "ROWMAJOR"][d.layout],
                 "shape": [d.shape[i] for i in range(d.ndim)]}
 
@@ -252,7 +252,7 @@ class Subgraph:
 
     def _torch_io(self):
         import torch
-        kinds = {"bf16": torch.bfloat16, "f32": torch.float32}
+        kinds = {"bf16": torch.bfloat16, "f32": torch.float32, "i32": torch.int32}
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is None:
             def raw(device):

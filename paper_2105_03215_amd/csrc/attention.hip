@@ -1,0 +1,374 @@
+// Softmax attention with keys of another length than the queries: cross
+// attention to an encoder's states, causal self attention, single tokens over a
+// long context.
+//
+// One pass over the keys with the running maximum and sum of the softmax:
+//   m' = max(m, max_j s_j),  l' = l 2^(m - m') + sum_j 2^(s_j - m'),
+//   o' = o 2^(m - m') + sum_j 2^(s_j - m') v_j,   o / l at the end,
+// with s = (q . k) scale log2(e) in float32.
+//
+// Rows of queries are packed over the heads that share a key head: row
+// r = i * group + g of (batch b, key head h) is query i of head h * group + g, so
+// that one read of the keys serves the whole group.
+//
+// Both products run transposed on 32x32 MFMA tiles: S^T = K Q^T leaves 16 keys of
+// one query row in each lane, so the softmax needs one exchange between the two
+// halves of the wave, and its result is, in place, the right operand of
+// O^T = V^T P^T: register group i of a lane half h holds keys 8 (i / 4) + 4 h + i % 4,
+// and V^T is read in the same order (the order of a sum over keys is free).
+#include <algorithm>
+#include <type_traits>
+
+#include "lds_dma.h"
+
+namespace byoc {
+namespace {
+
+using namespace dma;
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
+
+constexpr int kKeys = 32;   // keys of a tile
+constexpr int kCols = 32;   // packed query rows of a tile
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// max / sum over the two halves of the wave (lanes l and l ^ 32)
+__device__ __forceinline__ float half_max(float x) {
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Keys that packed row r of batch b sees.
+__device__ __forceinline__ int seen_keys(const AttnParams& p, int len, int r) {
+  if (r >= p.q_len * p.group) return 0;
+  if (!p.causal) return len;
+  return min(max(len - p.q_len + r / p.group + 1, 0), len);
+}
+
+__device__ __forceinline__ int batch_len(const AttnParams& p, int b) {
+  return p.lengths ? min(max(p.lengths[b], 0), p.k_len) : p.k_len;
+}
+
+// Swizzle keys of the LDS tiles, on 16-byte chunks of a row: key rows are read 16
+// bytes per lane down the rows, value rows 8 bytes per lane with four rows and 16
+// columns per 16 lanes; either way 16 lanes meet every bank once.
+template <int CPR>
+__device__ __forceinline__ int k_key(int row) {
+  return CPR == 8 ? (row >> 1) & 7 : row & 15;
+}
+template <int CPR>
+__device__ __forceinline__ int v_key(int row) {
+  return CPR == 8 ? ((row >> 1) & 1) << 2 : ((row & 3) << 2) | ((row >> 2) & 3);
+}
+
+// A workgroup takes 32 packed query rows of one (batch, key head) and a share of
+// its keys; its waves take tiles of 32 keys in turn, each through its own LDS
+// tiles, without a barrier until their results meet at the end.
+template <typename T, int DP, int NW>
+__global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int ES = sizeof(T);
+  constexpr int RB = DP * ES;         // bytes of an LDS row
+  constexpr int CPR = RB / 16;        // its 16-byte chunks
+  constexpr int TILE = kKeys * RB;    // bytes of a tile
+  constexpr int NBUF = BF ? 2 : 1;
+  constexpr int NI = TILE / 1024;     // loads of a tile per lane
+  constexpr int DB = DP / 32;         // 32-column blocks of the output
+  __shared__ __align__(16) char lds[NW * NBUF * 2 * TILE];
+  __shared__ float ml[NW][2][kCols];
+  static_assert(sizeof(lds) + sizeof(ml) <= kLdsLimit, "LDS");
+  static_assert(NW * NBUF * 2 * TILE >= NW * DP * kCols * 4, "the waves' results take the tiles' place");
+
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int R = p.q_len * p.group;
+  const int ncb = (R + kCols - 1) / kCols;
+  int bid = blockIdx.x;
+  const int bh = bid % (p.batch * p.kv_heads);
+  bid /= p.batch * p.kv_heads;
+  const int cb = bid % ncb, split = bid / ncb;
+  const int b = bh / p.kv_heads, kh = bh - b * p.kv_heads;
+  const int len = batch_len(p, b);
+  const int row = cb * kCols + col;
+  const int lim = seen_keys(p, len, row);
+  const int kend = seen_keys(p, len, min(cb * kCols + kCols, R) - 1);  // (rows see more keys further down)
+  const int tiles = (kend + kKeys - 1) / kKeys;
+  const int per = (tiles + p.splits - 1) / p.splits;
+  const int t_end = min(split * per + per, tiles);
+
+  // this lane's part of its query row: 16-byte chunks 2 st + h
+  constexpr int QS = CPR / 2;
+  uint4 qf[QS];
+  {
+    const int i = row / p.group, g = row - i * p.group;
+    const char* qp = (const char*)p.q + ((int64_t)(b * (int64_t)p.q_len + i) * p.ldq + (kh * p.group + g) * p.D) * ES;
+#pragma unroll
+    for (int st = 0; st < QS; ++st) {
+      const int c = 2 * st + h;
+      qf[st] = row < R && c * 16 < p.D * ES ? *(const uint4*)(qp + c * 16) : make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+
+  const int64_t sk = p.ldk * ES, sv = p.ldv * ES;
+  const char* kb = (const char*)p.k + (int64_t)b * p.k_len * sk + kh * p.D * ES;
+  const char* vb = (const char*)p.v + (int64_t)b * p.k_len * sv + kh * p.D * ES;
+  char* mine = lds + wave * (NBUF * 2 * TILE);
+  auto fill = [&](int buf, int t) {
+    const int k0 = t * kKeys;
+    const int n = t < t_end ? min(kKeys, len - k0) : 0;  // rows past the length read as zeros, whatever they hold
+    const i32x4 kr = buffer_rsrc(kb + (int64_t)k0 * sk, n > 0 ? (n - 1) * (int)sk + p.D * ES : 0);
+    const i32x4 vr = buffer_rsrc(vb + (int64_t)k0 * sv, n > 0 ? (n - 1) * (int)sv + p.D * ES : 0);
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(mine + buf * 2 * TILE));
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int r = (i * 64 + lane) / CPR, s = (i * 64 + lane) % CPR;
+      const int c = s ^ k_key<CPR>(r);
+      lds_fill16(kr, at + i * 1024, c * 16 < p.D * ES ? (uint32_t)(r * (int)sk + c * 16) : kOOB);
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int r = (i * 64 + lane) / CPR, s = (i * 64 + lane) % CPR;
+      const int c = s ^ v_key<CPR>(r);
+      lds_fill16(vr, at + TILE + i * 1024, c * 16 < p.D * ES ? (uint32_t)(r * (int)sv + c * 16) : kOOB);
+    }
+  };
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) o[d] = f32x16{};
+  float m = -INFINITY, l = 0.0f;
+  const float c2 = p.scale * 1.44269504088896340736f;
+
+  auto compute = [&](int buf, int t) {
+    const char* kt = mine + buf * 2 * TILE;
+    const char* vt = kt + TILE;
+    f32x16 s{};
+#pragma unroll
+    for (int st = 0; st < QS; ++st) {
+      const uint4 a = *(const uint4*)(kt + col * RB + (((2 * st + h) ^ k_key<CPR>(col)) * 16));
+      if constexpr (BF) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(qf[st]), s, 0, 0, 0);
+      } else {
+        const f32x4 af = __builtin_bit_cast(f32x4, a), bf = __builtin_bit_cast(f32x4, qf[st]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(af[e], bf[e], s, 0, 0, 0);
+      }
+    }
+    const int k0 = t * kKeys + 4 * h;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = k0 + 8 * (i >> 2) + (i & 3) < lim ? s[i] * c2 : -INFINITY;
+      top = fmaxf(top, s[i]);
+    }
+    const float mn = fmaxf(m, half_max(top));
+    const float use = mn == -INFINITY ? 0.0f : mn;  // (no key seen yet: every weight is zero)
+    const float keep = exp2_(m - use);
+    m = mn;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = exp2_(s[i] - use);
+      sum += s[i];
+    }
+    l = l * keep + sum;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] *= keep;
+    if constexpr (BF) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        // (weights rounded to bf16 for the matrix cores: relative 2^-9 each, as the values' own)
+        uint4 pf;
+        pf.x = pack2_bf16(s[8 * ks + 0], s[8 * ks + 1]);
+        pf.y = pack2_bf16(s[8 * ks + 2], s[8 * ks + 3]);
+        pf.z = pack2_bf16(s[8 * ks + 4], s[8 * ks + 5]);
+        pf.w = pack2_bf16(s[8 * ks + 6], s[8 * ks + 7]);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          uint2 vf[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int r = ks * 16 + 8 * j + 4 * h + ((lane & 15) >> 2);
+            const int c = d * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+            const char* at = vt + r * RB + ((c ^ v_key<CPR>(r)) * 16) + (lane & 1) * 8;
+            vf[j] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at));
+          }
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(make_uint4(vf[0].x, vf[0].y, vf[1].x, vf[1].y)),
+                                                         as_bf16x8(pf), o[d], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int r = 8 * (i >> 2) + 4 * h + (i & 3);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          const int c = d * 8 + (col >> 2);
+          const float vf = *(const float*)(vt + r * RB + ((c ^ v_key<CPR>(r)) * 16) + (col & 3) * 4);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[i], o[d], 0, 0, 0);
+        }
+      }
+    }
+  };
+
+  int t = split * per + wave, buf = 0;
+  if constexpr (NBUF == 2) {
+    fill(0, t);
+    for (; t < t_end; t += NW) {
+      fill(buf ^ 1, t + NW);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
+      compute(buf, t);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile's reads are done before it is filled again
+      buf ^= 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  } else {
+    for (; t < t_end; t += NW) {
+      fill(0, t);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      compute(0, t);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  }
+
+  // the waves' results: a common maximum, then the sums in wave order
+  l = half_sum(l);
+  if (h == 0) {
+    ml[wave][0][col] = m;
+    ml[wave][1][col] = l;
+  }
+  __syncthreads();
+  float top = ml[0][0][col];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) top = fmaxf(top, ml[w][0][col]);
+  const float use = top == -INFINITY ? 0.0f : top;
+  const float f = exp2_(m - use);
+  float* const os = (float*)lds;  // [wave][DP][32]
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) os[(wave * DP + d * 32 + 8 * (i >> 2) + 4 * h + (i & 3)) * kCols + col] = o[d][i] * f;
+  float total = 0.0f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) total += ml[w][1][col] * exp2_(ml[w][0][col] - use);
+  __syncthreads();
+  if (row >= R) return;
+  // thread = packed row col, columns 8 e .. 8 e + 7 in turn
+  const float inv = lim > 0 ? 1.0f / total : 0.0f;
+  const int i = row / p.group, g = row - i * p.group;
+  const int64_t part = ((int64_t)bh * R + row) * p.splits + split;
+  for (int e = tid >> 5; e * 8 < p.D; e += 2 * NW) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      v[j] = os[(e * 8 + j) * kCols + col];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) v[j] += os[(w * DP + e * 8 + j) * kCols + col];
+    }
+    if (p.splits > 1) {
+      float* out = p.ws + part * p.D + e * 8;
+      *(float4*)out = make_float4(v[0], v[1], v[2], v[3]);
+      *(float4*)(out + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      continue;
+    }
+    // (a row without keys is zero; one whose seen scores are all -inf divides zero by zero, as the softmax does)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = lim > 0 ? v[j] * inv : 0.0f;
+    char* out = (char*)p.y + ((b * (int64_t)p.q_len + i) * p.ldy + (kh * p.group + g) * p.D + e * 8) * ES;
+    if constexpr (BF) {
+      *(uint4*)out = pack8(v);
+    } else {
+      *(float4*)out = make_float4(v[0], v[1], v[2], v[3]);
+      *(float4*)(out + 16) = make_float4(v[4], v[5], v[6], v[7]);
+    }
+  }
+  if (p.splits > 1 && tid < kCols) {
+    float* out = p.ws + (int64_t)p.batch * p.kv_heads * R * p.splits * p.D + part * 2;
+    out[0] = top;
+    out[1] = total;
+  }
+}
+
+// Joins the splits of a packed row: thread = 4 columns.
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p) {
+  const int R = p.q_len * p.group;
+  const int per = p.D / 4;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t pr = at / per;  // (batch, key head, packed row)
+  if (pr >= (int64_t)p.batch * p.kv_heads * R) return;
+  const int c = (int)(at - pr * per) * 4;
+  const int bh = (int)(pr / R), row = (int)(pr - (int64_t)bh * R);
+  const int b = bh / p.kv_heads, kh = bh - b * p.kv_heads;
+  const float* ml = p.ws + (int64_t)p.batch * p.kv_heads * R * p.splits * p.D + pr * p.splits * 2;
+  const float* os = p.ws + pr * p.splits * p.D + c;
+  float top = -INFINITY;
+  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, ml[2 * s]);
+  const float use = top == -INFINITY ? 0.0f : top;
+  float total = 0.0f;
+  float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < p.splits; ++s) {
+    const float f = exp2_(ml[2 * s] - use);
+    const float4 x = *(const float4*)(os + (int64_t)s * p.D);
+    total += ml[2 * s + 1] * f;
+    v[0] += x.x * f, v[1] += x.y * f, v[2] += x.z * f, v[3] += x.w * f;
+  }
+  const bool any = seen_keys(p, batch_len(p, b), row) > 0;
+  const int i = row / p.group, g = row - i * p.group;
+  const int64_t out = (b * (int64_t)p.q_len + i) * p.ldy + (kh * p.group + g) * p.D + c;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = any ? v[j] / total : 0.0f;
+  if (p.f32)
+    *(float4*)((float*)p.y + out) = make_float4(v[0], v[1], v[2], v[3]);
+  else
+    *(uint2*)((bf16_t*)p.y + out) = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
+}
+
+int row_blocks(const AttnParams& p) {
+  return p.batch * p.kv_heads * ceil_div((int64_t)p.q_len * p.group, kCols);
+}
+
+}  // namespace
+
+// Enough workgroups for two on each of the 256 CUs, and 128 keys in each at least.
+void choose_attention(AttnParams& p) {
+  const int want = ceil_div(512, row_blocks(p));
+  p.splits = std::max(1, std::min(std::min(want, ceil_div(p.k_len, 4 * kKeys)), 256));
+}
+
+const char* attention_name(const AttnParams& p) { return p.f32 ? "attention_rows_f32" : "attention_rows"; }
+
+int64_t attn_workspace(const AttnParams& p) {
+  if (p.splits <= 1) return 0;
+  return (int64_t)p.batch * p.kv_heads * p.q_len * p.group * p.splits * (p.D + 2) * 4;
+}
+
+hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
+  if (p.D < 8 || p.D > 256 || p.D % 8 != 0 || p.splits < 1) return hipErrorInvalidValue;
+  const int grid = row_blocks(p) * p.splits;
+  if (p.f32) {
+    if (p.D <= 64) attention_rows_kernel<float, 64, 4><<<grid, 256, 0, s>>>(p);
+    else if (p.D <= 128) attention_rows_kernel<float, 128, 4><<<grid, 256, 0, s>>>(p);
+    else attention_rows_kernel<float, 256, 2><<<grid, 128, 0, s>>>(p);
+  } else {
+    if (p.D <= 64) attention_rows_kernel<bf16_t, 64, 4><<<grid, 256, 0, s>>>(p);
+    else if (p.D <= 128) attention_rows_kernel<bf16_t, 128, 4><<<grid, 256, 0, s>>>(p);
+    else attention_rows_kernel<bf16_t, 256, 2><<<grid, 128, 0, s>>>(p);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_attention_join(const AttnParams& p, hipStream_t s) {
+  const int64_t n = (int64_t)p.batch * p.kv_heads * p.q_len * p.group * (p.D / 4);
+  attention_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace byoc

@@ -32,11 +32,12 @@ constexpr int kKPad = 64;     // packed reduction length is padded to this (the 
 constexpr int kHaloStages = 3;  // halo kernel weight ring: 3 stages of one kernel row (built-in choice)
 
 struct PackJob {
-  enum Kind { ConvW, DwW, DwW32, RowsW32, Vec, Copy, StemW, Host } kind;  // Host: copy blob n, built on the host
+  enum Kind { ConvW, DwW, DwW32, RowsW32, Vec, Copy, StemW, Host, QDenseW } kind;  // Host: copy blob n, built on the host
   int cidx = -1;       // constant index
   int64_t dst = 0;     // byte offset in the weights region
   int K = 0, Cg = 0, R = 0, S = 0, Cp = 0, Kgp = 0, rows = 0;
   int n = 0, n_out = 0;
+  int64_t dst2 = 0;    // QDenseW: the scales
 };
 
 // float32 form of a real rescaling factor of an int8 graph (rounded from
@@ -361,10 +362,12 @@ struct Planner {
   bool i8;                                  // partially quantized (int8) graph
   const byoc_const* consts = nullptr;       // host constants (int8 weights are quantized on the host)
   std::vector<std::vector<uint8_t>> blobs;  // host-built constant blocks (PackJob::Host)
+  std::vector<Launch> quant_of;  // value -> its QuantRows launch, shared by the qdense nodes that read it (x.kind None: none)
 
   Planner(Engine* e_, Graph& g_) : e(e_), g(g_), bf16(g_.compute == DType::BF16), i8(g_.compute == DType::I8) {
     loc.resize(g.values.size());
     cp.assign(g.values.size(), 0);
+    quant_of.resize(g.values.size());
   }
 
   int64_t internal_bytes(int v) const {
@@ -430,6 +433,9 @@ struct Planner {
   void find_ir_blocks();
   void plan_ir(int ci);
   void plan_block_i8(int ci);
+  void plan_qdense(int ni);
+  void plan_rotary(int ni);
+  void plan_attention(int ni);
   Ref slice(int vcat, int channel) const {  // channel slice of a concatenation's buffer
     Ref r = loc[vcat];
     r.off += (int64_t)channel * 2;
@@ -1085,6 +1091,10 @@ Status Planner::plan() {
   for (size_t i = 0; i < g.inputs.size(); ++i) {
     const IoDesc& in = g.inputs[i];
     const int v = in.value;
+    if (in.dtype == DType::I32) {  // positions or lengths, read in place
+      loc[v] = io(Ref::Input, (int)i);
+      continue;
+    }
     const auto& s = g.values[v].shape;
     cp[v] = bf16 ? (int)rup(s[1], 8) : (int)s[1];
     bool fused_stem = false;
@@ -1198,8 +1208,151 @@ Status Planner::plan() {
   return Status::Ok();
 }
 
+// Dense on 8-bit codes: the rows quantized first - once for all the qdense nodes that
+// read a value, such as separate query, key and value projections - then the product.
+void Planner::plan_qdense(int ni) {
+  const Node& n = g.nodes[ni];
+  const auto& xs = g.values[n.data].shape;
+  const auto& ws = g.values[n.weight].shape;
+  const int M = (int)xs[0], K = (int)xs[1], N = (int)ws[0];
+  const int Kq = (int)rup(K, 128), rows = (int)rup(N, kRowPad);
+  Launch& Q = quant_of[n.data];
+  if (Q.x.kind == Ref::None) {
+    Q.op = Launch::QuantRows;
+    Q.info.kind = BYOC_K_QDENSE;
+    Q.info.node = ni;
+    Q.x = loc[n.data];
+    Q.qr_scales = rup((int64_t)M * Kq, 256);
+    Q.y = arena(Q.qr_scales + (int64_t)M * 4);
+    Q.qr.ldx = cp[n.data];
+    Q.qr.M = Q.qr.rows = M, Q.qr.K = K, Q.qr.Kq = Kq;
+    Q.qr.f32 = !bf16;
+    Q.info.bytes = act_bytes(n.data) + (int64_t)M * K + M * 4;
+    name(Q, "quant_rows");
+    e->launches.push_back(Q);
+  }
+  Launch L;
+  L.op = Launch::QDense;
+  L.info.kind = BYOC_K_QDENSE;
+  L.info.node = ni;
+  L.info.flops = 2 * n.macs;
+  L.info.bytes = (int64_t)M * K + M * 4 + (int64_t)N * K + N * 4 + (n.bias >= 0 ? N * 4 : 0) +
+                 act_bytes(n.out) * (n.residual >= 0 ? 2 : 1);
+  L.x = Q.y;
+  L.qr_scales = Q.qr_scales;
+  L.y = loc[n.out];
+  if (n.residual >= 0) L.res = loc[n.residual];
+  const int wc = g.values[n.weight].index;
+  L.w = wslot((int64_t)rows * Kq);
+  L.w2 = wslot((int64_t)rows * 4);
+  PackJob j{PackJob::QDenseW, wc, L.w.off};
+  j.K = N, j.rows = rows, j.Kgp = Kq, j.n = K;
+  j.dst2 = L.w2.off;
+  jobs.push_back(j);
+  if (n.bias >= 0) {
+    L.bias = wslot((int64_t)rows * 4);
+    PackJob b{PackJob::Vec, g.values[n.bias].index, L.bias.off};
+    b.n = N, b.n_out = rows;
+    jobs.push_back(b);
+  }
+  QDenseParams& p = L.qn;
+  p.M = M, p.N = cp[n.out], p.Kq = Kq;
+  p.ldy = cp[n.out];
+  p.ldr = cp[n.out];
+  p.act = (int)n.act;
+  p.alpha = n.alpha;
+  p.f32 = !bf16;
+  L.qt = choose_qdense_tile(p.M, p.N);
+  std::snprintf(L.info.name, sizeof(L.info.name), "qdense_%dx%d", L.qt.bm, L.qt.bn);
+  e->launches.push_back(L);
+}
+
+void Planner::plan_rotary(int ni) {
+  const Node& n = g.nodes[ni];
+  Launch L;
+  L.op = Launch::Rotary;
+  L.info.kind = BYOC_K_ROTARY;
+  L.info.node = ni;
+  L.x = loc[n.data];
+  L.other = loc[n.index];
+  L.y = loc[n.out];
+  RotaryParams& p = L.rot;
+  p.M = (int)g.values[n.data].shape[0];
+  p.ldx = cp[n.data];
+  p.ldy = p.cols_out = cp[n.out];
+  p.heads = n.heads, p.kv_heads = n.kv_heads, p.D = n.head_dim, p.rd = n.rotary_dim;
+  p.interleaved = n.interleaved;
+  p.mag = (float)n.mag;
+  p.eps = (float)n.eps;
+  p.f32 = !bf16;
+  std::vector<uint8_t> turns(n.theta.size() * sizeof(double));
+  for (size_t i = 0; i < n.theta.size(); ++i) {
+    const double t = n.theta[i] / (2.0 * 3.14159265358979323846);
+    std::memcpy(&turns[i * sizeof(double)], &t, sizeof(double));
+  }
+  L.w = host_blob(std::move(turns));
+  auto weight = [&](int v) {
+    if (v < 0) return Ref();
+    const Ref r = wslot((int64_t)n.head_dim * 4);
+    PackJob j{PackJob::Vec, g.values[v].index, r.off};
+    j.n = j.n_out = n.head_dim;
+    jobs.push_back(j);
+    return r;
+  };
+  L.w2 = weight(n.weight);
+  L.w3 = weight(n.weight2);
+  L.info.bytes = 2 * act_bytes(n.out) + (int64_t)p.M * 4;
+  name(L, n.norm ? "qk_norm_rotary" : "rotary");
+  e->launches.push_back(L);
+}
+
+void Planner::plan_attention(int ni) {
+  const Node& n = g.nodes[ni];
+  Launch L;
+  L.op = Launch::Attention;
+  L.info.kind = BYOC_K_ATTENTION;
+  L.info.node = ni;
+  L.x = loc[n.data];
+  L.other = loc[n.key];
+  L.res = loc[n.value];
+  if (n.index >= 0) L.bias = loc[n.index];
+  L.y = loc[n.out];
+  const int64_t es = bf16 ? 2 : 4;
+  L.x.off += n.cols[0] * es;
+  L.other.off += n.cols[1] * es;
+  L.res.off += n.cols[2] * es;
+  AttnParams& p = L.at;
+  p.ldq = cp[n.data], p.ldk = cp[n.key], p.ldv = cp[n.value], p.ldy = cp[n.out];
+  p.batch = n.batch, p.q_len = n.q_len, p.k_len = n.k_len;
+  p.kv_heads = n.kv_heads, p.group = n.heads / n.kv_heads, p.D = n.head_dim;
+  p.causal = n.causal;
+  p.scale = (float)n.scale;
+  p.f32 = !bf16;
+  choose_attention(p);
+  // (every pair of a full context: the lengths are not known yet)
+  L.info.flops = 4 * (int64_t)n.batch * n.heads * n.q_len * n.k_len * n.head_dim;
+  L.info.bytes = 2 * act_bytes(n.out) + 2 * (int64_t)n.batch * n.k_len * n.kv_heads * n.head_dim * es;
+  name(L, attention_name(p));
+  if (p.splits <= 1) {
+    e->launches.push_back(L);
+    return;
+  }
+  L.partial = arena(attn_workspace(p));
+  Launch J = L;
+  L.y = Ref();
+  J.op = Launch::AttentionJoin;
+  J.x = J.other = J.res = Ref();
+  J.info.flops = J.info.bytes = 0;
+  name(J, "attention_join");
+  e->launches.push_back(L);
+  e->launches.push_back(J);
+}
+
 void Planner::plan_node(int ni) {
   const Node& n = g.nodes[ni];
+  if (n.op == OpKind::QDense) return plan_qdense(ni);
+  if (n.op == OpKind::Rotary) return plan_rotary(ni);
+  if (n.op == OpKind::Attention) return plan_attention(ni);
   const auto& xs = g.values[n.data].shape;
   const auto& ys = g.values[n.out].shape;
   Launch L;
@@ -2224,8 +2377,8 @@ struct RunCtx {
   void* ptr(const Ref& r) const {
     switch (r.kind) {
       case Ref::Arena: return (arena ? arena : e->arena) + e->bufs[r.idx].off + r.off;
-      case Ref::Input: return const_cast<void*>(in[r.idx]);
-      case Ref::Output: return out[r.idx];
+      case Ref::Input: return (char*)const_cast<void*>(in[r.idx]) + r.off;
+      case Ref::Output: return (char*)out[r.idx] + r.off;
       case Ref::Weights: return e->weights + r.off;
       default: return nullptr;
     }
@@ -2403,6 +2556,45 @@ hipError_t exec(const Launch& L, const RunCtx& c) {
       p.y = c.ptr(L.y);
       return launch_stem_conv_maxpool(p, c.s);
     }
+    case Launch::QuantRows: {
+      QRowsParams p = L.qr;
+      p.x = c.ptr(L.x);
+      p.q = (int8_t*)c.ptr(L.y);
+      p.scale = (float*)((char*)c.ptr(L.y) + L.qr_scales);
+      return launch_quant_rows(p, c.s);
+    }
+    case Launch::QDense: {
+      QDenseParams p = L.qn;
+      p.x = (const int8_t*)c.ptr(L.x);
+      p.xs = (const float*)((const char*)c.ptr(L.x) + L.qr_scales);
+      p.w = (const int8_t*)c.ptr(L.w);
+      p.ws = (const float*)c.ptr(L.w2);
+      p.bias = (const float*)c.ptr(L.bias);
+      p.res = c.ptr(L.res);
+      p.y = c.ptr(L.y);
+      return launch_qdense(p, L.qt, c.s);
+    }
+    case Launch::Rotary: {
+      RotaryParams p = L.rot;
+      p.x = c.ptr(L.x);
+      p.pos = (const int*)c.ptr(L.other);
+      p.theta = (const double*)c.ptr(L.w);
+      p.wq = (const float*)c.ptr(L.w2);
+      p.wk = (const float*)c.ptr(L.w3);
+      p.y = c.ptr(L.y);
+      return launch_rotary(p, c.s);
+    }
+    case Launch::Attention:
+    case Launch::AttentionJoin: {
+      AttnParams p = L.at;
+      p.q = c.ptr(L.x);
+      p.k = c.ptr(L.other);
+      p.v = c.ptr(L.res);
+      p.lengths = (const int*)c.ptr(L.bias);
+      p.y = c.ptr(L.y);
+      p.ws = (float*)c.ptr(L.partial);
+      return L.op == Launch::Attention ? launch_attention(p, c.s) : launch_attention_join(p, c.s);
+    }
   }
   return hipErrorInvalidValue;
 }
@@ -2510,6 +2702,9 @@ Status build_device_state(Engine* e, Planner& pl, const byoc_const* consts) {
           break;
         case PackJob::StemW:
           err = launch_pack_stem_weights(src, sb, (bf16_t*)dst, j.Cg, j.R, j.S, j.n, nullptr);
+          break;
+        case PackJob::QDenseW:
+          err = launch_quant_rows({src, (int8_t*)dst, (float*)(e->weights + j.dst2), j.n, j.K, j.rows, j.n, j.Kgp, !sb}, nullptr);
           break;
       }
     }
@@ -2633,6 +2828,16 @@ Status engine_create(Graph&& g, const byoc_const* consts, int32_t n_consts, int 
   Planner pl(e, e->graph);
   pl.consts = consts;
   Status st = pl.plan();
+  for (const Launch& L : e->launches) {
+    if (L.op != Launch::QuantRows && L.op != Launch::QDense && L.op != Launch::Rotary && L.op != Launch::Attention &&
+        L.op != Launch::AttentionJoin)
+      continue;
+    for (const Ref* r : {&L.x, &L.bias, &L.res, &L.y, &L.other}) {
+      if (r->kind == Ref::Input)
+        e->in_align.push_back({r->idx, e->graph.inputs[r->idx].dtype == DType::I32 ? 4 : 16});
+      if (r->kind == Ref::Output) e->out_align.push_back({r->idx, 16});
+    }
+  }
   if (st.ok()) {
     int ndev = 0;
     if (hipGetDeviceCount(&ndev) != hipSuccess || ndev == 0)
@@ -3037,6 +3242,15 @@ Status check_run_args(const Engine* e, const void* const* inputs, int32_t n_in, 
     if (!inputs[i]) return Status::Err(BYOC_ERR_INVALID_ARG, "input " + std::to_string(i) + " is NULL");
   for (int i = 0; i < n_out; ++i)
     if (!outputs[i]) return Status::Err(BYOC_ERR_INVALID_ARG, "output " + std::to_string(i) + " is NULL");
+  auto misaligned = [](const void* p, const char* what, const std::pair<int, int>& a) {
+    if ((uintptr_t)p % (unsigned)a.second == 0) return Status::Ok();
+    return Status::Err(BYOC_ERR_INVALID_ARG, std::string(what) + std::to_string(a.first) + " is not aligned to " +
+                                                 std::to_string(a.second) + " bytes");
+  };
+  for (const auto& a : e->in_align)
+    if (Status st = misaligned(inputs[a.first], "input ", a); !st.ok()) return st;
+  for (const auto& a : e->out_align)
+    if (Status st = misaligned(outputs[a.first], "output ", a); !st.ok()) return st;
   return Status::Ok();
 }
 

@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "graph.h"
@@ -26,7 +27,7 @@ struct Launch {
     ConvMfma, SplitReduce, ConvF32, Depthwise, MaxPoolBf16, AvgPoolBf16, MaxPoolF32, AvgPoolF32,
     AddBf16, AddF32, NchwToNhwc, NhwcToNchw, RowsToPadded, PaddedToRows, Cast, StemConvPool, DenseRows,
     ConvI8, MaxPoolI8, AvgPoolI8, AddI8, QuantizeI8, DequantizeI8, AvgPoolWinBf16, CopyChannels, QuantizeIm2colI8,
-    DepthwiseI8, Bottleneck, IrBlock
+    DepthwiseI8, Bottleneck, IrBlock, QuantRows, QDense, Rotary, Attention, AttentionJoin
   } op;
   byoc_launch_info info{};
   Ref x, w, bias, res, y, partial, other;
@@ -49,6 +50,12 @@ struct Launch {
   // in w3 / b3
   IrParams ir{};
   Ref w2, b2, w3, b3, wp, bp;
+  QRowsParams qr{};   // QuantRows: x -> codes in y, scales in y at qr_scales
+  int64_t qr_scales = 0;
+  QDenseParams qn{};  // QDense: codes (and scales) in x, packed codes in w, their scales in w2, bias, res
+  QDenseTile qt{};
+  RotaryParams rot{};  // Rotary: positions in other, angles in w, norm weights in w2 / w3
+  AttnParams at{};     // Attention: queries in x, keys in other, values in res, lengths in bias, split results in partial
   int bnF = 0, bnC = 0, bnCout = 0, bnS = 1;
   int group = 0;      // > 1: this launch and the group - 1 after it go out as one (bf16 convs)
   bool bnI8 = false;  // on int8 codes (w*, b* hold the int8 conv's weights and tables)
@@ -102,6 +109,8 @@ struct Engine {
   std::vector<int> lwait;
   std::vector<hipEvent_t> lev;
   hipEvent_t fork_ev = nullptr, join_ev = nullptr;
+  // inputs and outputs that a kernel addresses 16 bytes (i32: 4) at a time: checked per run
+  std::vector<std::pair<int, int>> in_align, out_align;  // (number, bytes)
 };
 
 // Builds the plan and device state.  On failure releases everything.

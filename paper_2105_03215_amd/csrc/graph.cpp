@@ -2,6 +2,7 @@
 // node (or input / constant) and the field at fault.
 #include "graph.h"
 
+#include <algorithm>
 #include <cmath>
 #include <map>
 #include <sstream>
@@ -119,7 +120,94 @@ struct CompositeName {
   Act act = Act::None;
 };
 
+// Optional integer attribute in [lo, hi].
+Status attr_int(const JsonValue* attrs, const char* key, const std::string& where, int64_t lo, int64_t hi, int* out) {
+  const JsonValue* v = attrs ? attrs->get(key) : nullptr;
+  if (!v) return Status::Ok();
+  if (v->kind != JsonValue::Number || !v->is_integer || v->inum < lo || v->inum > hi)
+    return perr(where + ": attrs." + key + " must be an integer in [" + std::to_string(lo) + ", " +
+                std::to_string(hi) + "]");
+  *out = (int)v->inum;
+  return Status::Ok();
+}
+
+// Optional number attribute, finite and above zero.
+Status attr_positive(const JsonValue* attrs, const char* key, const std::string& where, double* out) {
+  const JsonValue* v = attrs ? attrs->get(key) : nullptr;
+  if (!v) return Status::Ok();
+  if (v->kind != JsonValue::Number || !std::isfinite(v->num) || !(v->num > 0.0))
+    return perr(where + ": attrs." + key + " must be a positive finite number");
+  *out = v->num;
+  return Status::Ok();
+}
+
+constexpr int kMaxHeads = 4096;
+constexpr int64_t kMaxCols = 1 << 22;  // columns of a row that the packed-head kernels address (tiles of 64 rows in 31 bits)
+
+// The angle per position of each pair, and the factor on the rotated values.
+// scaling (for contexts longer than the model was trained on, by `factor`):
+//   linear: theta / factor
+//   ntk:    the base raised to base * factor^(rd / (rd - 2)), which divides the
+//           slowest pair's angle by factor and leaves the fastest alone
+//   yarn:   pairs that turn more than beta_fast times over original_length stay,
+//           those under beta_slow times are divided by factor, a linear ramp
+//           over the pairs between; the values grow by 0.1 ln(factor) + 1
+//           (or attention_factor)
+Status rotary_angles(const JsonValue* attrs, const std::string& where, Node* n) {
+  double base = 10000.0;
+  Status st = attr_positive(attrs, "base", where, &base);
+  if (!st.ok()) return st;
+  if (!(base > 1.0)) return perr(where + ": attrs.base must be above 1");
+  const int rd = n->rotary_dim;
+  const JsonValue* sc = attrs ? attrs->get("scaling") : nullptr;
+  std::string type;
+  double factor = 1.0;
+  if (sc) {
+    if (sc->kind != JsonValue::Object || !get_string(*sc, "type", &type))
+      return perr(where + ": attrs.scaling must be an object with a type");
+    if (type != "linear" && type != "ntk" && type != "yarn")
+      return uerr(where + ": attrs.scaling.type must be \"linear\", \"ntk\" or \"yarn\"");
+    if (!sc->get("factor")) return perr(where + ": attrs.scaling.factor missing");
+    if (!(st = attr_positive(sc, "factor", where, &factor)).ok()) return st;
+    if (factor < 1.0) return perr(where + ": attrs.scaling.factor must be at least 1");
+  }
+  if (type == "ntk" && rd > 2) base *= std::pow(factor, (double)rd / (rd - 2));
+  if (!std::isfinite(base)) return perr(where + ": attrs.base or scaling.factor too large");
+  n->theta.resize(rd / 2);
+  for (int i = 0; i < rd / 2; ++i) n->theta[i] = std::pow(base, -2.0 * i / rd);
+  if (type == "linear")
+    for (double& t : n->theta) t /= factor;
+  if (type == "yarn") {
+    int original = 0;
+    double fast = 32.0, slow = 1.0;
+    if (!sc->get("original_length")) return perr(where + ": attrs.scaling.original_length missing");
+    if (!(st = attr_int(sc, "original_length", where, 1, 1 << 30, &original)).ok()) return st;
+    if (!(st = attr_positive(sc, "beta_fast", where, &fast)).ok()) return st;
+    if (!(st = attr_positive(sc, "beta_slow", where, &slow)).ok()) return st;
+    if (fast <= slow) return perr(where + ": attrs.scaling.beta_fast must be above beta_slow");
+    n->mag = 0.1 * std::log(factor) + 1.0;
+    if (!(st = attr_positive(sc, "attention_factor", where, &n->mag)).ok()) return st;
+    const double pi = 3.14159265358979323846;
+    auto pair_of = [&](double turns) { return rd * std::log(original / (turns * 2.0 * pi)) / (2.0 * std::log(base)); };
+    const double low = std::max(std::floor(pair_of(fast)), 0.0);
+    const double high = std::min(std::ceil(pair_of(slow)), rd - 1.0);
+    for (int i = 0; i < rd / 2; ++i) {
+      const double ramp = std::min(1.0, std::max(0.0, (i - low) / std::max(high - low, 1e-3)));
+      n->theta[i] *= 1.0 - ramp + ramp / factor;
+    }
+  }
+  return Status::Ok();
+}
+
 bool split_composite(const std::string& name, CompositeName* c) {
+  if (name == "rotary" || name == "qk_norm_rotary") {
+    c->op = OpKind::Rotary;
+    return true;
+  }
+  if (name == "attention" || name == "attention_lengths") {
+    c->op = OpKind::Attention;
+    return true;
+  }
   if (name == "max_pool2d") {
     c->op = OpKind::MaxPool;
     return true;
@@ -150,6 +238,7 @@ bool split_composite(const std::string& name, CompositeName* c) {
   size_t i = 0;
   if (parts[0] == "conv2d") c->op = OpKind::Conv;
   else if (parts[0] == "dense") c->op = OpKind::Dense;
+  else if (parts[0] == "qdense") c->op = OpKind::QDense;
   else if (parts[0] == "add") c->op = OpKind::Add;
   else return false;
   ++i;
@@ -219,25 +308,27 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
     where += " (" + v.name + ")";
     if (by_name.count(v.name)) return perr(where + ": duplicate name");
     if (!get_ints(d.get("shape"), &v.shape)) return perr(where + ": shape must be integers");
-    if (v.shape.size() != 2 && v.shape.size() != 4)
-      return uerr(where + ": rank must be 2 or 4, got " + shape_str(v.shape));
+    std::string dt;
+    const bool index = get_string(d, "dtype", &dt) && (dt == "i32" || dt == "int32");
+    if (index ? v.shape.size() != 1 : v.shape.size() != 2 && v.shape.size() != 4)
+      return uerr(where + ": rank must be " + (index ? "1 for i32" : "2 or 4") + ", got " + shape_str(v.shape));
     for (int64_t s : v.shape)
       if (s < 1) return serr(where + ": non-positive extent in " + shape_str(v.shape));
     if (numel(v.shape) > kMaxElems) return uerr(where + ": more than 2^31-1 elements");
-    std::string dt;
-    if (!get_string(d, "dtype", &dt) || !parse_dtype(dt, &v.dtype))
-      return perr(where + ": dtype must be \"f32\" or \"bf16\"");
+    if (index) v.dtype = DType::I32;
+    else if (!parse_dtype(dt, &v.dtype)) return perr(where + ": dtype must be \"f32\", \"bf16\" or \"i32\"");
     IoDesc io;
     io.dtype = v.dtype;
     std::string lay;
     io.layout = v.shape.size() == 4 ? BYOC_NCHW : BYOC_ROWMAJOR;
     if (get_string(d, "layout", &lay)) {
-      if ((v.shape.size() == 4 && lay != "NCHW") || (v.shape.size() == 2 && lay != "ROWMAJOR"))
+      if ((v.shape.size() == 4 && lay != "NCHW") || (v.shape.size() != 4 && lay != "ROWMAJOR"))
         return uerr(where + ": layout " + lay + " not supported for rank " +
                     std::to_string(v.shape.size()));
     }
     Status qs = parse_quant(d, where, &v);
     if (!qs.ok()) return qs;
+    if (index && v.has_q) return uerr(where + ": quant parameters on an i32 input");
     v.source = Value::Input;
     v.index = (int)i;
     io.value = add_value(v);
@@ -338,7 +429,13 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
 
     size_t want = 0;
     switch (n.op) {
+      case OpKind::Rotary:
+        n.norm = n.composite == "qk_norm_rotary";
+        want = n.norm ? (args.size() == 3 ? 3 : 4) : 2;  // (no key heads: no key weight)
+        break;
+      case OpKind::Attention: want = n.composite == "attention" ? 3 : 4; break;
       case OpKind::Conv:
+      case OpKind::QDense:
       case OpKind::Dense: want = 2 + (n.has_bias ? 1 : 0) + (n.has_add ? 1 : 0); break;
       case OpKind::MaxPool:
       case OpKind::AvgPool:
@@ -350,8 +447,12 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
       return perr(where + ": expects " + std::to_string(want) + " inputs, got " +
                   std::to_string(args.size()));
     for (size_t k = 0; k < args.size(); ++k) {
-      bool weight_slot = (n.op == OpKind::Conv || n.op == OpKind::Dense) &&
+      bool weight_slot = (n.op == OpKind::Conv || n.op == OpKind::Dense || n.op == OpKind::QDense) &&
                          (k == 1 || (k == 2 && n.has_bias));
+      if (n.op == OpKind::Rotary) weight_slot = k > 0 && k + 1 < args.size();
+      const bool index_slot = (n.op == OpKind::Rotary && k + 1 == args.size()) || (n.op == OpKind::Attention && k == 3);
+      if (index_slot != (g.values[args[k]].dtype == DType::I32))
+        return serr(where + ": input " + std::to_string(k) + (index_slot ? " must be an i32 input" : " must not be i32"));
       if (weight_slot && !is_const(args[k]))
         return uerr(where + ": input " + std::to_string(k) + " must be a constant");
       if (!weight_slot && is_const(args[k]))
@@ -359,7 +460,7 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
                     g.values[args[k]].name + "'");
     }
     n.data = args[0];
-    if (n.op == OpKind::Conv || n.op == OpKind::Dense) {
+    if (n.op == OpKind::Conv || n.op == OpKind::Dense || n.op == OpKind::QDense) {
       n.weight = args[1];
       size_t k = 2;
       if (n.has_bias) n.bias = args[k++];
@@ -368,7 +469,17 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
       n.other = args[1];
     } else if (n.op == OpKind::Concat) {
       n.cat = args;
+    } else if (n.op == OpKind::Rotary) {
+      n.index = args.back();
+      if (n.norm) n.weight = args[1];
+      if (args.size() == 4) n.weight2 = args[2];
+    } else if (n.op == OpKind::Attention) {
+      n.key = args[1];
+      n.value = args[2];
+      if (args.size() == 4) n.index = args[3];
     }
+    if ((n.op == OpKind::QDense || n.op == OpKind::Rotary || n.op == OpKind::Attention) && out_dtype == DType::I8)
+      return uerr(where + ": " + n.composite + " only in bf16 and f32 graphs");
     const auto& xs = shp(n.data);
     if (n.act == Act::Leaky && attrs && attrs->get("alpha")) {
       const JsonValue* av = attrs->get("alpha");
@@ -414,7 +525,85 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
       if (n.has_bias && shp(n.bias) != std::vector<int64_t>{K})
         return serr(where + ": bias shape " + shape_str(shp(n.bias)) + " != [" + std::to_string(K) + "]");
       n.macs = xs[0] * K * P * Q * (C / n.groups) * R * S;
-    } else if (n.op == OpKind::Dense) {
+    } else if (n.op == OpKind::Rotary) {
+      if (xs.size() != 2) return serr(where + ": data must be 2-D, got " + shape_str(xs));
+      Status st = attr_int(attrs, "heads", where, 1, kMaxHeads, &n.heads);
+      if (st.ok()) st = attr_int(attrs, "kv_heads", where, 0, kMaxHeads, &n.kv_heads);
+      if (st.ok()) st = attr_int(attrs, "head_dim", where, 2, 512, &n.head_dim);
+      if (!st.ok()) return st;
+      if (!n.heads || !n.head_dim) return perr(where + ": attrs.heads and attrs.head_dim are required");
+      if (n.head_dim % 2) return uerr(where + ": attrs.head_dim must be even");
+      n.rotary_dim = n.head_dim;
+      st = attr_int(attrs, "rotary_dim", where, 2, n.head_dim, &n.rotary_dim);
+      if (st.ok()) st = attr_positive(attrs, "eps", where, &n.eps);
+      if (!st.ok()) return st;
+      if (n.rotary_dim % 2) return uerr(where + ": attrs.rotary_dim must be even");
+      std::string lay = "half";
+      if (attrs && attrs->get("layout") && !get_string(*attrs, "layout", &lay)) lay.clear();
+      if (lay != "half" && lay != "interleaved")
+        return perr(where + ": attrs.layout must be \"half\" or \"interleaved\"");
+      n.interleaved = lay == "interleaved";
+      st = rotary_angles(attrs, where, &n);
+      if (!st.ok()) return st;
+      const int64_t cols = (int64_t)(n.heads + n.kv_heads) * n.head_dim;
+      if (cols > xs[1])
+        return serr(where + ": " + std::to_string(n.heads + n.kv_heads) + " heads of " + std::to_string(n.head_dim) +
+                    " do not fit the rows of " + shape_str(xs));
+      if (n.norm && (n.weight2 >= 0) != (n.kv_heads > 0))
+        return perr(where + ": expects a weight for the query heads and, with kv_heads, one for the key heads");
+      for (int w : {n.weight, n.weight2})
+        if (w >= 0 && shp(w) != std::vector<int64_t>{n.head_dim})
+          return serr(where + ": norm weight shape " + shape_str(shp(w)) + " != [" + std::to_string(n.head_dim) + "]");
+      if (shp(n.index) != std::vector<int64_t>{xs[0]})
+        return serr(where + ": positions shape " + shape_str(shp(n.index)) + " != [" + std::to_string(xs[0]) + "]");
+      oshape = {xs[0], cols};
+    } else if (n.op == OpKind::Attention) {
+      const auto& ks = shp(n.key);
+      const auto& vs = shp(n.value);
+      if (xs.size() != 2 || ks.size() != 2 || vs.size() != 2) return serr(where + ": queries, keys and values must be 2-D");
+      n.batch = 0;
+      Status st = attr_int(attrs, "batch", where, 1, 1 << 20, &n.batch);
+      if (st.ok()) st = attr_int(attrs, "heads", where, 1, kMaxHeads, &n.heads);
+      n.kv_heads = n.heads;
+      if (st.ok()) st = attr_int(attrs, "kv_heads", where, 1, kMaxHeads, &n.kv_heads);
+      if (st.ok()) st = attr_int(attrs, "head_dim", where, 8, 256, &n.head_dim);
+      if (!st.ok()) return st;
+      if (!n.batch || !n.heads || !n.head_dim)
+        return perr(where + ": attrs.batch, attrs.heads and attrs.head_dim are required");
+      if (n.head_dim % 8) return uerr(where + ": attrs.head_dim must be a multiple of 8");
+      if (n.heads % n.kv_heads) return serr(where + ": attrs.heads is not a multiple of attrs.kv_heads");
+      n.scale = 1.0 / std::sqrt((double)n.head_dim);
+      if (!(st = attr_positive(attrs, "scale", where, &n.scale)).ok()) return st;
+      if (n.scale < 1e-30 || n.scale > 1e30) return uerr(where + ": attrs.scale outside [1e-30, 1e30]");
+      if (const JsonValue* cv = attrs->get("causal")) {
+        if (cv->kind != JsonValue::Bool) return perr(where + ": attrs.causal must be a boolean");
+        n.causal = cv->b;
+      }
+      const char* col_names[3] = {"q_col", "k_col", "v_col"};
+      const std::vector<int64_t>* shapes[3] = {&xs, &ks, &vs};
+      for (int i = 0; i < 3; ++i) {
+        if (!(st = attr_int(attrs, col_names[i], where, 0, kMaxCols, &n.cols[i])).ok()) return st;
+        if (n.cols[i] % 8) return uerr(where + ": attrs." + col_names[i] + " must be a multiple of 8");
+        const int64_t cols = (*shapes[i])[1];
+        if (n.cols[i] + (int64_t)(i ? n.kv_heads : n.heads) * n.head_dim > cols)
+          return serr(where + ": the heads from attrs." + col_names[i] + " on do not fit the rows of " +
+                      shape_str(*shapes[i]));
+        if (cols > kMaxCols) return uerr(where + ": rows of more than " + std::to_string(kMaxCols) + " columns");
+        if (out_dtype == DType::F32 && cols % 4)
+          return uerr(where + ": f32 rows need a multiple of 4 columns, got " + shape_str(*shapes[i]));
+      }
+      if (xs[0] % n.batch || ks[0] % n.batch)
+        return serr(where + ": rows of " + shape_str(xs) + " or " + shape_str(ks) + " are not a multiple of attrs.batch");
+      if (vs[0] != ks[0]) return serr(where + ": keys " + shape_str(ks) + " and values " + shape_str(vs) + " differ in rows");
+      n.q_len = (int)(xs[0] / n.batch);
+      n.k_len = (int)(ks[0] / n.batch);
+      if (n.index >= 0 && shp(n.index) != std::vector<int64_t>{n.batch})
+        return serr(where + ": lengths shape " + shape_str(shp(n.index)) + " != [" + std::to_string(n.batch) + "]");
+      // packed rows, workgroups and split results are counted in 31 bits
+      if ((int64_t)n.q_len * (n.heads / n.kv_heads) > kMaxElems / 64 || xs[0] * n.heads > kMaxElems / 64)
+        return uerr(where + ": too many query rows");
+      oshape = {xs[0], (int64_t)n.heads * n.head_dim};
+    } else if (n.op == OpKind::Dense || n.op == OpKind::QDense) {
       if (xs.size() != 2) return serr(where + ": data must be 2-D [M,K], got " + shape_str(xs));
       const auto& ws = shp(n.weight);
       if (ws.size() != 2 || ws[1] != xs[1])
@@ -424,6 +613,8 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
         return serr(where + ": bias shape " + shape_str(shp(n.bias)) + " != [" +
                     std::to_string(ws[0]) + "]");
       n.macs = xs[0] * ws[0] * xs[1];
+      if (n.op == OpKind::QDense && xs[1] > 131072)  // 127^2 K stays under 2^31
+        return uerr(where + ": reduction of more than 131072 elements on 8-bit codes");
     } else if (n.op == OpKind::MaxPool) {
       if (xs.size() != 4) return serr(where + ": data must be 4-D NCHW, got " + shape_str(xs));
       if (!attrs || !attrs->get("pool_size")) return perr(where + ": attrs.pool_size missing");
@@ -554,6 +745,8 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
     if (it == by_name.end()) return perr(where + ": unknown value '" + name + "'");
     if (g.values[it->second].source == Value::Const)
       return uerr(where + ": a constant cannot be a subgraph output");
+    if (g.values[it->second].dtype == DType::I32)
+      return uerr(where + ": an i32 input cannot be a subgraph output");
     IoDesc io;
     io.value = it->second;
     const auto& s = g.values[io.value].shape;

@@ -26,10 +26,11 @@ struct Status {
 
 // I8: the compute type of a partially quantized graph (int8 codes with an
 // affine scale and zero point per tensor); never an external dtype.
-enum class DType { F32 = BYOC_F32, BF16 = BYOC_BF16, I8 = 2 };
+// I32: an index input (token positions, sequence lengths).
+enum class DType { F32 = BYOC_F32, BF16 = BYOC_BF16, I8 = 2, I32 = BYOC_I32 };
 enum class Act { None = 0, Relu = 1, Relu6 = 2, Gelu = 3, Leaky = 4 };
 // AvgPool: global average pool; AvgPoolWin: windowed average pool.
-enum class OpKind { Conv, Dense, MaxPool, AvgPool, Add, AvgPoolWin, Concat };
+enum class OpKind { Conv, Dense, MaxPool, AvgPool, Add, AvgPoolWin, Concat, QDense, Rotary, Attention };
 
 // A named tensor of the graph: a subgraph input, a constant or a node output.
 struct Value {
@@ -61,6 +62,20 @@ struct Node {
   bool depthwise = false;
   bool count_include_pad = false;  // AvgPoolWin
   std::vector<int> cat;            // Concat: the joined values, in channel order
+  // Rotary, Attention: packed heads (data: the rotated rows, or the queries)
+  int index = -1;                  // value id of the positions or lengths (i32 input, -1: none)
+  int key = -1, value = -1;        // Attention: value ids of keys and values
+  int weight2 = -1;                // Rotary with norm: the key heads' weight (weight: the query heads')
+  int heads = 0, kv_heads = 0, head_dim = 0;
+  int batch = 1, q_len = 0, k_len = 0;
+  int cols[3] = {0, 0, 0};         // Attention: first column of the queries, keys and values
+  double scale = 0.0;              // Attention: of the scores
+  bool causal = false;
+  bool norm = false, interleaved = false;
+  int rotary_dim = 0;
+  double eps = 1e-6;
+  std::vector<double> theta;       // Rotary: angle per position of each pair
+  double mag = 1.0;                // factor on the rotated values
   int64_t macs = 0;
 };
 

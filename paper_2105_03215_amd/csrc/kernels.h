@@ -438,4 +438,86 @@ hipError_t launch_pack_dw_weights_f32(const void* src, bool src_bf16, float* dst
 hipError_t launch_pack_vector_f32(const void* src, bool src_bf16, float* dst, int K, int n_out,
                                   hipStream_t s);
 
+// ---- transformer-layer composites -------------------------------------------
+
+// Rows of activations (or weights) -> symmetric 8-bit codes with a scale for
+// each row: a = max|x|, code = rint(127 x / a), scale = a / 127; an all-zero
+// row has zero codes and scale, a row with an infinity or a NaN zero codes and
+// a NaN scale.  `rows` rows of Kq codes are written (Kq a multiple of 128), zero
+// past row M and column K.
+struct QRowsParams {
+  const void* x;  // [M][ldx], bf16 or f32
+  int8_t* q;      // [rows][Kq]
+  float* scale;   // [rows]
+  int64_t ldx;
+  int M, rows, K, Kq;
+  int f32;
+};
+hipError_t launch_quant_rows(const QRowsParams& p, hipStream_t s);
+
+// y[m][n] = act((sum_k x[m][k] w[n][k]) xs[m] ws[n] + bias[n] (+ res[m][n])) on
+// 8-bit codes, the sum exact in int32.
+struct QDenseParams {
+  const int8_t* x;    // [M][Kq]
+  const float* xs;    // [M]
+  const int8_t* w;    // [rows of a multiple of 256][Kq], zero past the channels
+  const float* ws;    // [as many], zero past the channels
+  const float* bias;  // [as many] or nullptr
+  const void* res;    // [M][ldr], the type of y, or nullptr
+  void* y;            // [M][ldy], bf16 or f32
+  int64_t ldy, ldr;
+  int M, N, Kq;       // N: columns written
+  int act;
+  float alpha;
+  int f32;
+  int py;             // tile grid partition over the XCDs (set by the launcher)
+};
+struct QDenseTile {
+  int bm, bn;
+};
+QDenseTile choose_qdense_tile(int64_t M, int64_t N);
+hipError_t launch_qdense(const QDenseParams& p, QDenseTile t, hipStream_t s);
+
+// Position rotation of the leading `heads + kv_heads` heads of each row, after
+// an optional RMS norm of each head.  theta: turns (angle / 2 pi) per position
+// of each of the rd / 2 pairs.
+struct RotaryParams {
+  const void* x;      // [M][ldx], bf16 or f32
+  const int* pos;     // [M]
+  const double* theta;
+  const float* wq;    // [D] or nullptr (no norm)
+  const float* wk;
+  void* y;            // [M][ldy], the type of x
+  int64_t ldx, ldy;
+  int M, heads, kv_heads, D, rd;
+  int cols_out;       // columns written: (heads + kv_heads) D, zeros up to here
+  int interleaved;
+  float mag, eps;
+  int f32;
+};
+hipError_t launch_rotary(const RotaryParams& p, hipStream_t s);
+
+// Softmax attention.  Query row i of batch b and head h reads head h / group of
+// the keys and values; key j is seen while j < len_b and, causal, while
+// j < len_b - q_len + i + 1; a row that sees none is zero.
+struct AttnParams {
+  const void* q;       // [batch * q_len][ldq], head h at column h D
+  const void* k;       // [batch * k_len][ldk], head at column (h / group) D
+  const void* v;
+  const int* lengths;  // [batch] or nullptr (k_len)
+  void* y;             // [batch * q_len][ldy]
+  float* ws;           // attn_workspace() bytes when splits > 1
+  int64_t ldq, ldk, ldv, ldy;
+  int batch, q_len, k_len, kv_heads, group, D;
+  int causal;
+  int splits;
+  float scale;
+  int f32;
+};
+void choose_attention(AttnParams& p);  // the split of the key axis
+const char* attention_name(const AttnParams& p);
+int64_t attn_workspace(const AttnParams& p);
+hipError_t launch_attention(const AttnParams& p, hipStream_t s);
+hipError_t launch_attention_join(const AttnParams& p, hipStream_t s);
+
 }  // namespace byoc

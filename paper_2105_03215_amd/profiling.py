@@ -291,7 +291,7 @@ def run_workload(name, batch, runs, warmup, autotune=True):
 
     from . import capi, runtime, workloads
 
-    wl = workloads.build(name, **({("batch" if name == "bert_ffn" else "n"): batch} if batch else {}))
+    wl = workloads.build(name, **({("batch" if name in ("bert_ffn", "decoder_layer") else "n"): batch} if batch else {}))
     sg = capi.Subgraph(wl.graph, wl.consts, device=0)
     try:
         dev = "cuda:0"

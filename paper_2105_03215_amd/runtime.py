@@ -9,12 +9,15 @@ from .capi import Subgraph  # noqa: F401
 
 
 def torch_dtype(name):
-    return torch.bfloat16 if name == "bf16" else torch.float32
+    return {"bf16": torch.bfloat16, "i32": torch.int32}.get(name, torch.float32)
 
 
 def to_device(arr, dtype_name, device):
-    """Host float array -> device tensor of the declared dtype.  bf16-declared
-    arrays must hold bf16-representable values (the conversion is exact)."""
+    """Host array -> device tensor of the declared dtype.  bf16-declared
+    arrays must hold bf16-representable values (the conversion is exact);
+    i32-declared ones hold whole numbers."""
+    if dtype_name == "i32":
+        return torch.from_numpy(np.ascontiguousarray(arr, dtype=np.int32)).to(device)
     t = torch.from_numpy(np.ascontiguousarray(arr, dtype=np.float32))
     return t.to(device=device, dtype=torch_dtype(dtype_name)).contiguous()
 

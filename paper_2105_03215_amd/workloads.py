@@ -33,6 +33,7 @@ CONFIG_IDS = {
     "vgg19": 5,
     "darknet53": 6,
     "inception_v3": 7,
+    "decoder_layer": 8,
 }
 
 _BN_EPS = 1e-5
@@ -154,6 +155,14 @@ class GraphBuilder:
         self.mu[name] = 0.5 if dist == "uniform" else 0.0
         return name
 
+    def index_input(self, name, values):
+        """Positions or lengths: a vector of whole numbers, given."""
+        a = np.ascontiguousarray(values, dtype=np.int32)
+        self.inputs.append({"name": name, "shape": list(a.shape), "dtype": "i32", "layout": "ROWMAJOR"})
+        self.input_arrays.append(a)
+        self.shapes[name] = list(a.shape)
+        return name
+
     def _after_add_act(self, m2_stream, m2_branch, act):
         if not act:
             return m2_stream + m2_branch
@@ -224,7 +233,7 @@ class GraphBuilder:
         self.conv_macs += macs
         return name
 
-    def dense(self, x, n_out, act=None, residual=None, w_std=None, b_std=0.01, name=None):
+    def dense(self, x, n_out, act=None, residual=None, w_std=None, b_std=0.01, name=None, op="dense"):
         m, kin = self.shapes[x]
         tid = self.next_tensor
         self.next_tensor += 2
@@ -233,7 +242,7 @@ class GraphBuilder:
         b = self.rng(tid + 1).normal(0.0, b_std, size=n_out)
         name = name or "n%d" % len(self.nodes)
         ins = [x, self._const(name + ".w", wt, "OI"), self._const(name + ".b", b, "O")]
-        comp = "dense_bias"
+        comp = op + "_bias"
         m2 = kin * std * std * self.m2[x] + b_std * b_std
         if residual is not None:
             ins.append(residual)
@@ -248,6 +257,40 @@ class GraphBuilder:
         self.shapes[name] = [m, n_out]
         self.m2[name] = m2
         self.macs += m * n_out * kin
+        return name
+
+    def qdense(self, x, n_out, **kw):
+        """Dense composite on 8-bit codes with a scale for each row and each output channel."""
+        return self.dense(x, n_out, op="qdense", **kw)
+
+    def rotary(self, x, positions, heads, kv_heads, head_dim, norm=False, name=None, **attrs):
+        """Rotation of the leading heads of each row, with norm after an RMS norm of each head."""
+        name = name or "n%d" % len(self.nodes)
+        ins = [x]
+        if norm:
+            for part in ("q", "k")[:2 if kv_heads else 1]:
+                w = 1.0 + self.rng(self.next_tensor).normal(0.0, 0.1, size=head_dim)
+                self.next_tensor += 1
+                ins.append(self._const("%s.%s" % (name, part), w, "O"))
+        self.nodes.append({"name": name, "composite": "qk_norm_rotary" if norm else "rotary",
+                           "inputs": ins + [positions],
+                           "attrs": dict({"heads": heads, "kv_heads": kv_heads, "head_dim": head_dim}, **attrs),
+                           "out_dtype": self.dtype})
+        self.shapes[name] = [self.shapes[x][0], (heads + kv_heads) * head_dim]
+        self.m2[name] = 1.0 if norm else self.m2[x]
+        return name
+
+    def attention(self, q, k, v, batch, heads, head_dim, lengths=None, name=None, **attrs):
+        """Attention of the heads in q's rows over those of k and v."""
+        name = name or "n%d" % len(self.nodes)
+        self.nodes.append({"name": name, "composite": "attention_lengths" if lengths else "attention",
+                           "inputs": [q, k, v] + ([lengths] if lengths else []),
+                           "attrs": dict({"batch": batch, "heads": heads, "head_dim": head_dim}, **attrs),
+                           "out_dtype": self.dtype})
+        self.shapes[name] = [self.shapes[q][0], heads * head_dim]
+        # the mean of n values weighted by a softmax of scores of variance 1 keeps about e / n of
+        # their mean square (causal rows see n / 2 on average); the first rows keep all of it
+        self.m2[name] = self.m2[v] * min(1.0, 2.0 * math.e * batch / self.shapes[k][0])
         return name
 
     def max_pool(self, x, size=3, stride=2, pad=1, name=None, gain=None):
@@ -436,6 +479,34 @@ def bert_ffn(batch=8, seq=128, hidden=768, ffn=3072, layers=12):
     return g.finish({"batch": batch, "seq": seq})
 
 
+def decoder_layer(batch=8, tokens=128, encoder_tokens=200, hidden=768, heads=12, kv_heads=4, ffn=3072, start=0):
+    """One decoder layer of an encoder-decoder transformer on 8-bit weights, on
+    the token rows of the BERT FFN stack: causal self attention with
+    normed and rotated queries and keys, cross attention to the encoder's
+    states, whose lengths differ, and the feed-forward block, each with its
+    residual.  Tokens stand at positions start, start + 1, ...; x N(0,1), W
+    N(0, 0.02) as there, the three branches' output projections N(0, 0.01)."""
+    g = GraphBuilder("decoder_layer", CONFIG_IDS["decoder_layer"])
+    d = hidden // heads
+    qk, kv = (heads + kv_heads) * d, kv_heads * d
+    x = g.input("x", [batch * tokens, hidden], "normal")
+    enc = g.input("encoder", [batch * encoder_tokens, hidden], "normal")
+    pos = g.index_input("positions", np.tile(np.arange(start, start + tokens), batch))
+    lens = g.index_input("lengths", [max(1, encoder_tokens * (3 + 5 * i % 8) // 10) for i in range(batch)])
+    qkv = g.qdense(x, qk + kv, w_std=0.02, b_std=0.02, name="self.qkv")
+    rot = g.rotary(qkv, pos, heads, kv_heads, d, norm=True, name="self.rotary")
+    a = g.attention(rot, rot, qkv, batch, heads, d, kv_heads=kv_heads, causal=True, k_col=heads * d, v_col=qk,
+                    name="self.attention")
+    x = g.qdense(a, hidden, residual=x, w_std=0.01, b_std=0.02, name="self.out")
+    q = g.qdense(x, hidden, w_std=0.02, b_std=0.02, name="cross.q")
+    ekv = g.qdense(enc, 2 * kv, w_std=0.02, b_std=0.02, name="cross.kv")
+    a = g.attention(q, ekv, ekv, batch, heads, d, lengths=lens, kv_heads=kv_heads, v_col=kv, name="cross.attention")
+    x = g.qdense(a, hidden, residual=x, w_std=0.01, b_std=0.02, name="cross.out")
+    h = g.qdense(x, ffn, act="gelu", w_std=0.02, b_std=0.02, name="ffn1")
+    g.output(g.qdense(h, hidden, residual=x, w_std=0.01, b_std=0.02, name="ffn2"))
+    return g.finish({"batch": batch, "tokens": tokens})
+
+
 _VGG19 = [64, 64, "M", 128, 128, "M", 256, 256, 256, 256, "M", 512, 512, 512, 512, "M",
           512, 512, 512, 512, "M"]
 
@@ -592,7 +663,8 @@ def inception_v3(n=1, hw=299, input_dtype="bf16", num_classes=1000):
 
 def build(name, **kw):
     """Build a workload by name: conv_f32, resnet18_block, resnet50_v1,
-    resnet50_v1b, mobilenet_v2, bert_ffn, vgg19, darknet53, inception_v3."""
+    resnet50_v1b, mobilenet_v2, bert_ffn, vgg19, darknet53, inception_v3,
+    decoder_layer."""
     if name == "conv_f32":
         return conv_f32(**kw)
     if name == "resnet18_block":
@@ -611,4 +683,6 @@ def build(name, **kw):
         return darknet53(**kw)
     if name == "inception_v3":
         return inception_v3(**kw)
+    if name == "decoder_layer":
+        return decoder_layer(**kw)
     raise ValueError("unknown workload %r" % name)
