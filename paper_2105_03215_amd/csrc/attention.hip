@@ -69,6 +69,29 @@ __device__ __forceinline__ int v_key(int row) {
   return CPR == 8 ? ((row >> 1) & 1) << 2 : ((row & 3) << 2) | ((row >> 2) & 3);
 }
 
+// Weights of 16 keys of one register group, rounded to bf16 for the matrix cores (a
+// relative 2^-8 each at most, as the values' own rounding).
+__device__ __forceinline__ uint4 pack_weights(const f32x16& s, int ks) {
+  return make_uint4(pack2_bf16(s[8 * ks + 0], s[8 * ks + 1]), pack2_bf16(s[8 * ks + 2], s[8 * ks + 3]),
+                    pack2_bf16(s[8 * ks + 4], s[8 * ks + 5]), pack2_bf16(s[8 * ks + 6], s[8 * ks + 7]));
+}
+
+// V^T of 16 keys (row0 ..) and 32 columns (block d): the left operand of O^T = V^T P^T,
+// keys in the order that pack_weights leaves them in.
+template <int CPR>
+__device__ __forceinline__ uint4 load_vt(const char* vt, int row0, int d, int lane) {
+  const int h = lane >> 5;
+  uint2 vf[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int r = row0 + 8 * j + 4 * h + ((lane & 15) >> 2);
+    const int c = d * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    const char* at = vt + r * (CPR * 16) + ((c ^ v_key<CPR>(r)) * 16) + (lane & 1) * 8;
+    vf[j] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at));
+  }
+  return make_uint4(vf[0].x, vf[0].y, vf[1].x, vf[1].y);
+}
+
 // A workgroup takes 32 packed query rows of one (batch, key head) and a share of
 // its keys; its waves take tiles of 32 keys in turn, each through its own LDS
 // tiles, without a barrier until their results meet at the end.
@@ -185,25 +208,11 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
     if constexpr (BF) {
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
-        // (weights rounded to bf16 for the matrix cores: relative 2^-9 each, as the values' own)
-        uint4 pf;
-        pf.x = pack2_bf16(s[8 * ks + 0], s[8 * ks + 1]);
-        pf.y = pack2_bf16(s[8 * ks + 2], s[8 * ks + 3]);
-        pf.z = pack2_bf16(s[8 * ks + 4], s[8 * ks + 5]);
-        pf.w = pack2_bf16(s[8 * ks + 6], s[8 * ks + 7]);
+        const uint4 pf = pack_weights(s, ks);
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          uint2 vf[2];
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int r = ks * 16 + 8 * j + 4 * h + ((lane & 15) >> 2);
-            const int c = d * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-            const char* at = vt + r * RB + ((c ^ v_key<CPR>(r)) * 16) + (lane & 1) * 8;
-            vf[j] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at));
-          }
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(make_uint4(vf[0].x, vf[0].y, vf[1].x, vf[1].y)),
-                                                         as_bf16x8(pf), o[d], 0, 0, 0);
-        }
+        for (int d = 0; d < DB; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(load_vt<CPR>(vt, ks * 16, d, lane)), as_bf16x8(pf),
+                                                         o[d], 0, 0, 0);
       }
     } else {
 #pragma unroll
@@ -297,6 +306,194 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   }
 }
 
+// Many rows, bf16: four waves of 32 packed rows each share tiles of 64 keys and
+// values, double-buffered in LDS; a tile's loads run while the one before is
+// multiplied, with one barrier a tile.  Two such workgroups fit a CU (D <= 128), so
+// that one's softmax runs beside the other's products.
+//
+// The running maximum moves only when a tile's exceeds it by more than 2^8 (kSlack):
+// the weights then stay under 2^8, far from overflow, and the 16 x D / 32 products
+// that rescale the output are left out of almost every tile.
+constexpr int kTileKeys = 64;
+constexpr float kSlack = 8.0f;
+
+template <int DP>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel(AttnParams p) {
+  constexpr int NW = 4;
+  constexpr int RB = DP * 2, CPR = RB / 16;
+  constexpr int TILE = kTileKeys * RB;
+  constexpr int NI = TILE / (NW * 1024);  // loads of a tile per lane
+  constexpr int DB = DP / 32, QS = CPR / 2, KB = kTileKeys / 32;
+  __shared__ __align__(16) char lds[4 * TILE];
+  static_assert(sizeof(lds) <= kLdsLimit, "LDS");
+
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int R = p.q_len * p.group;
+  const int nh = p.batch * p.kv_heads;
+  const int nt = (R + 32 * NW - 1) / (32 * NW);
+  // Head fastest: with a multiple of 8 heads each XCD (workgroup b runs on XCD b % 8) keeps to its own
+  // heads' keys and values; the last rows first, which see the most keys under a causal mask.
+  int bid = blockIdx.x;
+  const int bh = bid % nh;
+  bid /= nh;
+  const int split = bid % p.splits;
+  const int tile = nt - 1 - bid / p.splits;
+  const int b = bh / p.kv_heads, kh = bh - b * p.kv_heads;
+  const int len = batch_len(p, b);
+  const int row0 = tile * 32 * NW + wave * 32, row = row0 + col;
+  const int lim = seen_keys(p, len, row);
+  const int lim_lo = seen_keys(p, len, min(row0, R - 1));            // (rows see more keys further down)
+  const int lim_hi = row0 < R ? seen_keys(p, len, min(row0 + 32, R) - 1) : 0;
+  const int kend = seen_keys(p, len, min((tile + 1) * 32 * NW, R) - 1);
+  const int tiles = (kend + kTileKeys - 1) / kTileKeys;
+  const int per = (tiles + p.splits - 1) / p.splits;
+  const int t0 = split * per, t_end = min(t0 + per, tiles);
+
+  uint4 qf[QS];
+  const int i = row / p.group, g = row - i * p.group;
+  {
+    const char* qp = (const char*)p.q + ((b * (int64_t)p.q_len + i) * p.ldq + (kh * p.group + g) * p.D) * 2;
+#pragma unroll
+    for (int st = 0; st < QS; ++st) {
+      const int c = 2 * st + h;
+      qf[st] = row < R && c * 8 < p.D ? *(const uint4*)(qp + c * 16) : make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+
+  const int64_t sk = p.ldk * 2, sv = p.ldv * 2;
+  const char* kb = (const char*)p.k + (int64_t)b * p.k_len * sk + kh * p.D * 2;
+  const char* vb = (const char*)p.v + (int64_t)b * p.k_len * sv + kh * p.D * 2;
+  uint32_t ko[NI], vo[NI];
+#pragma unroll
+  for (int n = 0; n < NI; ++n) {
+    const int at = (n * NW + wave) * 64 + lane, r = at / CPR, s = at % CPR;
+    const int ck = s ^ k_key<CPR>(r), cv = s ^ v_key<CPR>(r);
+    ko[n] = ck * 8 < p.D ? (uint32_t)(r * (int)sk + ck * 16) : kOOB;
+    vo[n] = cv * 8 < p.D ? (uint32_t)(r * (int)sv + cv * 16) : kOOB;
+  }
+  auto fill = [&](int buf, int t) {
+    const int k0 = t * kTileKeys;
+    const int n = min(kTileKeys, len - k0);  // rows past the length read as zeros, whatever they hold
+    const i32x4 kr = buffer_rsrc(kb + (int64_t)k0 * sk, (n - 1) * (int)sk + p.D * 2);
+    const i32x4 vr = buffer_rsrc(vb + (int64_t)k0 * sv, (n - 1) * (int)sv + p.D * 2);
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(lds + buf * 2 * TILE)) + wave * 1024;
+#pragma unroll
+    for (int n = 0; n < NI; ++n) lds_fill16(kr, at + n * NW * 1024, ko[n]);
+#pragma unroll
+    for (int n = 0; n < NI; ++n) lds_fill16(vr, at + TILE + n * NW * 1024, vo[n]);
+  };
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) o[d] = f32x16{};
+  float m = -INFINITY, l = 0.0f;
+  const float c2 = p.scale * 1.44269504088896340736f;
+
+  if (t0 < t_end) fill(0, t0);
+  for (int t = t0; t < t_end; ++t) {
+    const int buf = (t - t0) & 1;
+    // this tile has landed for every wave, and every wave is done with the one before
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t + 1 < t_end) fill(buf ^ 1, t + 1);
+    const int k0 = t * kTileKeys;
+    if (k0 >= lim_hi) continue;  // nothing here for this wave's rows
+    const char* kt = lds + buf * 2 * TILE;
+    const char* vt = kt + TILE;
+    f32x16 s[KB];
+#pragma unroll
+    for (int n = 0; n < KB; ++n) s[n] = f32x16{};
+#pragma unroll
+    for (int st = 0; st < QS; ++st)
+#pragma unroll
+      for (int n = 0; n < KB; ++n) {
+        const int r = n * 32 + col;
+        const uint4 a = *(const uint4*)(kt + r * RB + (((2 * st + h) ^ k_key<CPR>(r)) * 16));
+        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(qf[st]), s[n], 0, 0, 0);
+      }
+    if (k0 + kTileKeys > lim_lo) {
+#pragma unroll
+      for (int n = 0; n < KB; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (k0 + n * 32 + 8 * (e >> 2) + 4 * h + (e & 3) >= lim) s[n][e] = -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < KB; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[n][e]);
+    top = half_max(top) * c2;
+    if (__any(top > m + kSlack)) {  // (m = -inf before the first seen key)
+      const float mn = fmaxf(m, top);
+      const float keep = exp2_(m - (mn == -INFINITY ? 0.0f : mn));
+      m = mn;
+      l *= keep;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d] *= keep;
+    }
+    const float use = m == -INFINITY ? 0.0f : m;
+    float sum = 0.0f;
+#pragma unroll
+    for (int n = 0; n < KB; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[n][e] = exp2_(__builtin_fmaf(s[n][e], c2, -use));
+        sum += s[n][e];
+      }
+    l += sum;
+#pragma unroll
+    for (int n = 0; n < KB; ++n)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const uint4 pf = pack_weights(s[n], ks);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(load_vt<CPR>(vt, n * 32 + ks * 16, d, lane)),
+                                                         as_bf16x8(pf), o[d], 0, 0, 0);
+      }
+  }
+  if (row >= R) return;
+  l = half_sum(l);
+  if (p.splits > 1) {
+    const int64_t part = ((int64_t)bh * R + row) * p.splits + split;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = d * 32 + 8 * e + 4 * h;
+        if (c < p.D) *(float4*)(p.ws + part * p.D + c) = make_float4(o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]);
+      }
+    if (h == 0) {
+      float* out = p.ws + (int64_t)nh * R * p.splits * p.D + part * 2;
+      out[0] = m;
+      out[1] = l;
+    }
+    return;
+  }
+  // (a row without keys is zero; one whose seen scores are all -inf divides zero by zero, as the softmax does)
+  const float inv = 1.0f / l;
+  bf16_t* y = (bf16_t*)p.y + (b * (int64_t)p.q_len + i) * p.ldy + (kh * p.group + g) * p.D;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+      // columns 8 e + 4 h .. + 3 and 8 (e + 1) + 4 h .. + 3 of this lane become 8 (e + h) .. + 7
+      uint32_t w[2][2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int at = 4 * (e + k) + 2 * j;
+          w[k][j] = lim > 0 ? pack2_bf16(o[d][at] * inv, o[d][at + 1] * inv) : 0u;
+        }
+      const u32x2 lo = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+      const u32x2 hi = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+      const int c = d * 32 + 8 * (e + h);
+      if (c < p.D) *(uint4*)(y + c) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+    }
+}
+
 // Joins the splits of a packed row: thread = 4 columns.
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p) {
   const int R = p.q_len * p.group;
@@ -331,19 +528,26 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p) {
     *(uint2*)((bf16_t*)p.y + out) = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
 }
 
-int row_blocks(const AttnParams& p) {
-  return p.batch * p.kv_heads * ceil_div((int64_t)p.q_len * p.group, kCols);
+int row_blocks(const AttnParams& p, int rows) {
+  return p.batch * p.kv_heads * ceil_div((int64_t)p.q_len * p.group, rows);
 }
+
+// Whether the rows go through the shared tiles: with 32 packed rows or fewer three of
+// its four waves would idle, and fp32 products are bound by the matrix cores either way.
+bool tiled(const AttnParams& p) { return !p.f32 && p.q_len * (int64_t)p.group > 32; }
 
 }  // namespace
 
-// Enough workgroups for two on each of the 256 CUs, and 128 keys in each at least.
+// Enough workgroups for two on each of the 256 CUs, and 128 keys (tiles: 512) in each at least.
 void choose_attention(AttnParams& p) {
-  const int want = ceil_div(512, row_blocks(p));
-  p.splits = std::max(1, std::min(std::min(want, ceil_div(p.k_len, 4 * kKeys)), 256));
+  const bool t = tiled(p);
+  const int want = ceil_div(512, row_blocks(p, t ? 128 : kCols));
+  p.splits = std::max(1, std::min(std::min(want, ceil_div(p.k_len, t ? 512 : 4 * kKeys)), 256));
 }
 
-const char* attention_name(const AttnParams& p) { return p.f32 ? "attention_rows_f32" : "attention_rows"; }
+const char* attention_name(const AttnParams& p) {
+  return p.f32 ? "attention_rows_f32" : tiled(p) ? "attention_tiles" : "attention_rows";
+}
 
 int64_t attn_workspace(const AttnParams& p) {
   if (p.splits <= 1) return 0;
@@ -352,7 +556,14 @@ int64_t attn_workspace(const AttnParams& p) {
 
 hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
   if (p.D < 8 || p.D > 256 || p.D % 8 != 0 || p.splits < 1) return hipErrorInvalidValue;
-  const int grid = row_blocks(p) * p.splits;
+  if (tiled(p)) {
+    const int grid = row_blocks(p, 128) * p.splits;
+    if (p.D <= 64) attention_tiles_kernel<64><<<grid, 256, 0, s>>>(p);
+    else if (p.D <= 128) attention_tiles_kernel<128><<<grid, 256, 0, s>>>(p);
+    else attention_tiles_kernel<256><<<grid, 256, 0, s>>>(p);
+    return hipGetLastError();
+  }
+  const int grid = row_blocks(p, kCols) * p.splits;
   if (p.f32) {
     if (p.D <= 64) attention_rows_kernel<float, 64, 4><<<grid, 256, 0, s>>>(p);
     else if (p.D <= 128) attention_rows_kernel<float, 128, 4><<<grid, 256, 0, s>>>(p);
