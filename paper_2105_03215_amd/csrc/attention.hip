@@ -541,7 +541,8 @@ bool tiled(const AttnParams& p) { return !p.f32 && p.q_len * (int64_t)p.group > 
 // Enough workgroups for two on each of the 256 CUs, and 128 keys (tiles: 512) in each at least.
 void choose_attention(AttnParams& p) {
   const bool t = tiled(p);
-  const int want = ceil_div(512, row_blocks(p, t ? 128 : kCols));
+  const int blocks = row_blocks(p, t ? 128 : kCols);
+  const int want = t ? (blocks >= 256 ? 1 : 512 / blocks) : ceil_div(512, blocks);
   p.splits = std::max(1, std::min(std::min(want, ceil_div(p.k_len, t ? 512 : 4 * kKeys)), 256));
 }
 
