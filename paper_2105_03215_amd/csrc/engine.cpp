@@ -1216,6 +1216,7 @@ void Planner::plan_qdense(int ni) {
   const auto& ws = g.values[n.weight].shape;
   const int M = (int)xs[0], K = (int)xs[1], N = (int)ws[0];
   const int Kq = (int)rup(K, 128), rows = (int)rup(N, kRowPad);
+  const bool fused = qdense_fuses_rows(M, Kq);
   Launch& Q = quant_of[n.data];
   if (Q.x.kind == Ref::None) {
     Q.op = Launch::QuantRows;
@@ -1223,13 +1224,13 @@ void Planner::plan_qdense(int ni) {
     Q.info.node = ni;
     Q.x = loc[n.data];
     Q.qr_scales = rup((int64_t)M * Kq, 256);
-    Q.y = arena(Q.qr_scales + (int64_t)M * 4);
+    if (!fused) Q.y = arena(Q.qr_scales + (int64_t)M * 4);
     Q.qr.ldx = cp[n.data];
     Q.qr.M = Q.qr.rows = M, Q.qr.K = K, Q.qr.Kq = Kq;
     Q.qr.f32 = !bf16;
     Q.info.bytes = act_bytes(n.data) + (int64_t)M * K + M * 4;
     name(Q, "quant_rows");
-    e->launches.push_back(Q);
+    if (!fused) e->launches.push_back(Q);
   }
   Launch L;
   L.op = Launch::QDense;
@@ -1238,7 +1239,9 @@ void Planner::plan_qdense(int ni) {
   L.info.flops = 2 * n.macs;
   L.info.bytes = (int64_t)M * K + M * 4 + (int64_t)N * K + N * 4 + (n.bias >= 0 ? N * 4 : 0) +
                  act_bytes(n.out) * (n.residual >= 0 ? 2 : 1);
-  L.x = Q.y;
+  L.fused = fused;
+  L.x = fused ? Q.x : Q.y;
+  L.qr = Q.qr;
   L.qr_scales = Q.qr_scales;
   L.y = loc[n.out];
   if (n.residual >= 0) L.res = loc[n.residual];
@@ -1262,8 +1265,9 @@ void Planner::plan_qdense(int ni) {
   p.act = (int)n.act;
   p.alpha = n.alpha;
   p.f32 = !bf16;
-  L.qt = choose_qdense_tile(p.M, p.N);
-  std::snprintf(L.info.name, sizeof(L.info.name), "qdense_%dx%d", L.qt.bm, L.qt.bn);
+  L.qt = choose_qdense_tile(p.M, p.N, Kq);
+  if (L.qt.id == kQDenseRows) std::snprintf(L.info.name, sizeof(L.info.name), "qdense_rows_m%d%s", M, fused ? "_fused" : "");
+  else std::snprintf(L.info.name, sizeof(L.info.name), "qdense_%dx%d", L.qt.bm, L.qt.bn);
   e->launches.push_back(L);
 }
 
@@ -2565,13 +2569,20 @@ hipError_t exec(const Launch& L, const RunCtx& c) {
     }
     case Launch::QDense: {
       QDenseParams p = L.qn;
-      p.x = (const int8_t*)c.ptr(L.x);
-      p.xs = (const float*)((const char*)c.ptr(L.x) + L.qr_scales);
+      if (!L.fused) {
+        p.x = (const int8_t*)c.ptr(L.x);
+        p.xs = (const float*)((const char*)c.ptr(L.x) + L.qr_scales);
+      }
       p.w = (const int8_t*)c.ptr(L.w);
       p.ws = (const float*)c.ptr(L.w2);
       p.bias = (const float*)c.ptr(L.bias);
       p.res = c.ptr(L.res);
       p.y = c.ptr(L.y);
+      if (L.fused) {
+        QRowsParams q = L.qr;
+        q.x = c.ptr(L.x);
+        return launch_qdense_fused(p, q, c.s);
+      }
       return launch_qdense(p, L.qt, c.s);
     }
     case Launch::Rotary: {

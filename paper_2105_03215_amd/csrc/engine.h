@@ -53,7 +53,8 @@ struct Launch {
   QRowsParams qr{};   // QuantRows: x -> codes in y, scales in y at qr_scales
   int64_t qr_scales = 0;
   QDenseParams qn{};  // QDense: codes (and scales) in x, packed codes in w, their scales in w2, bias, res
-  QDenseTile qt{};
+  QDenseTile qt{};    //   (x: the rows themselves, described in qr, where the product quantizes them: fused)
+  bool fused = false;
   RotaryParams rot{};  // Rotary: positions in other, angles in w, norm weights in w2 / w3
   AttnParams at{};     // Attention: queries in x, keys in other, values in res, lengths in bias, split results in partial
   int bnF = 0, bnC = 0, bnCout = 0, bnS = 1;

@@ -472,10 +472,14 @@ struct QDenseParams {
   int f32;
   int py;             // tile grid partition over the XCDs (set by the launcher)
 };
+constexpr int kQDenseRows = -1;  // QDenseTile::id of the kernel of few rows
 struct QDenseTile {
-  int bm, bn;
+  int id, bm, bn;
 };
-QDenseTile choose_qdense_tile(int64_t M, int64_t N);
+QDenseTile choose_qdense_tile(int64_t M, int64_t N, int64_t Kq);
+// Few enough rows for the product's workgroups to quantize them for themselves (q: the rows; p.x and p.xs unused).
+bool qdense_fuses_rows(int64_t M, int64_t Kq);
+hipError_t launch_qdense_fused(const QDenseParams& p, const QRowsParams& q, hipStream_t s);
 hipError_t launch_qdense(const QDenseParams& p, QDenseTile t, hipStream_t s);
 
 // Position rotation of the leading `heads + kv_heads` heads of each row, after

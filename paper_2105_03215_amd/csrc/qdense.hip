@@ -7,6 +7,8 @@
 //
 // with r, b the same of the weight rows, formed once at engine creation by the
 // same kernel.
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "lds_dma.h"
@@ -16,15 +18,18 @@ namespace {
 
 using namespace dma;
 
-// 8 consecutive values of a row, zero from column K on.  f32 rows need not be
-// 16-byte aligned (their stride is any number of columns); bf16 rows are, but for
-// constants of other widths (`vec` false).
+// 8 consecutive values of a row as they are stored, zero from column K on.  f32 rows
+// need not be 16-byte aligned (their stride is any number of columns); bf16 rows
+// are, but for constants of other widths (`vec` false).
 struct __attribute__((packed, aligned(4))) F32x4u {
   float v[4];
 };
 template <bool F32>
-__device__ __forceinline__ void load8(const void* x, int64_t row, int col, int K, bool vec, float* v) {
-  if constexpr (F32) {
+struct Chunk;
+template <>
+struct Chunk<true> {
+  float v[8];
+  __device__ __forceinline__ void load(const void* x, int64_t row, int col, int K, bool) {
     const float* p = (const float*)x + row + col;
     if (col + 8 <= K) {
       const F32x4u a = *(const F32x4u*)p, b = *(const F32x4u*)(p + 4);
@@ -34,20 +39,28 @@ __device__ __forceinline__ void load8(const void* x, int64_t row, int col, int K
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = col + e < K ? p[e] : 0.0f;
     }
-  } else {
-    if (!vec) {
+  }
+  __device__ __forceinline__ void get(float* f) const {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = col + e < K ? bf16_to_f32(((const bf16_t*)x)[row + col + e]) : 0.0f;
-    } else if (col < K) {
-      unpack8(*(const uint4*)((const bf16_t*)x + row + col), v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = col + e < K ? v[e] : 0.0f;
+    for (int e = 0; e < 8; ++e) f[e] = v[e];
+  }
+};
+template <>
+struct Chunk<false> {
+  uint4 u;
+  __device__ __forceinline__ void load(const void* x, int64_t row, int col, int K, bool vec) {
+    const bf16_t* p = (const bf16_t*)x + row + col;
+    if (vec && col + 8 <= K) {
+      u = *(const uint4*)p;
     } else {
+      uint32_t w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+      for (int e = 0; e < 8; ++e) w[e] = col + e < K ? p[e] : 0u;
+      u = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
     }
   }
-}
+  __device__ __forceinline__ void get(float* f) const { unpack8(u, f); }
+};
 
 // A row's scale, and what its codes are formed with.  The magnitudes are compared
 // as integers, which orders NaN above infinity above every number.
@@ -90,8 +103,10 @@ __device__ __forceinline__ uint32_t pack_codes(const float* y) {
   return w ^ kU8ToCode;
 }
 
-// WPR waves per row; NC > 0: the row's chunks of 8 stay in registers between the
-// maximum and the codes (at most NC per lane), NC = 0: they are read twice.
+// WPR waves per row; NC > 0: the row's chunks of 8 stay in registers as they came
+// between the maximum and the codes (at most NC per lane), NC = 0: they are read
+// twice.  HBM bound: 8192 rows of 4096 bf16, 101 MB, in 19.9 us (5.1 TB/s;
+// 21.8 with a wave per row).
 template <bool F32, int WPR, int NC>
 __global__ __launch_bounds__(256) void quant_rows_kernel(QRowsParams p) {
   constexpr int LANES = 64 * WPR;
@@ -100,38 +115,43 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QRowsParams p) {
   const int row = blockIdx.x * (4 / WPR) + tid / LANES;
   const int lane = tid % LANES;
   const int chunks = p.Kq / 8;
-  const bool live = row < p.M, vec = p.ldx % 8 == 0;
+  const bool vec = p.ldx % 8 == 0;
+  const int K = row < p.M ? p.K : 0;
   const int64_t at = (int64_t)row * p.ldx;
   uint32_t top = 0;
-  float v[NC > 0 ? NC : 1][8];
-  auto widen = [&](const float* f) {
+  Chunk<F32> v[NC > 0 ? NC : 1];
+  auto widen = [&](const Chunk<F32>& c) {
+    float f[8];
+    c.get(f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
   };
   if constexpr (NC > 0) {
 #pragma unroll
-    for (int i = 0; i < NC; ++i) load8<F32>(p.x, at, (i * LANES + lane) * 8, live ? p.K : 0, vec, v[i]);
+    for (int i = 0; i < NC; ++i) v[i].load(p.x, at, (i * LANES + lane) * 8, K, vec);
 #pragma unroll
     for (int i = 0; i < NC; ++i) widen(v[i]);
   } else {
     for (int c = lane; c < chunks; c += LANES) {
-      load8<F32>(p.x, at, c * 8, live ? p.K : 0, vec, v[0]);
+      v[0].load(p.x, at, c * 8, K, vec);
       widen(v[0]);
     }
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
-  if constexpr (WPR == 4) {
+  if constexpr (WPR > 1) {
     if ((tid & 63) == 0) tops[wave] = top;
     __syncthreads();
-    top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+#pragma unroll
+    for (int w = 0; w < WPR; ++w) top = max(top, tops[wave / WPR * WPR + w]);
   }
   if (row >= p.rows) return;
   const RowScale r = row_scale(top);
   if (lane == 0) p.scale[row] = r.scale;
   int8_t* q = p.q + (int64_t)row * p.Kq;
-  auto write = [&](int c, const float* f) {
-    float y[8];
+  auto write = [&](int c, const Chunk<F32>& x) {
+    float f[8], y[8];
+    x.get(f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = code_of<F32>(f[e], r);
     *(uint2*)(q + c * 8) = make_uint2(pack_codes(y), pack_codes(y + 4));
@@ -144,21 +164,24 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QRowsParams p) {
     }
   } else {
     for (int c = lane; c < chunks; c += LANES) {
-      load8<F32>(p.x, at, c * 8, live ? p.K : 0, vec, v[0]);
+      v[0].load(p.x, at, c * 8, K, vec);
       write(c, v[0]);
     }
   }
 }
 
+template <bool F32, int WPR, int NC>
+void quant_rows_as(const QRowsParams& p, hipStream_t s) {
+  quant_rows_kernel<F32, WPR, NC><<<(p.rows + 4 / WPR - 1) / (4 / WPR), 256, 0, s>>>(p);
+}
 template <bool F32>
 void quant_rows(const QRowsParams& p, hipStream_t s) {
-  const int rows4 = (p.rows + 3) / 4;
   const int c = p.Kq / 8;  // chunks of a row
-  if (c <= 64) quant_rows_kernel<F32, 1, 1><<<rows4, 256, 0, s>>>(p);
-  else if (c <= 128) quant_rows_kernel<F32, 1, 2><<<rows4, 256, 0, s>>>(p);
-  else if (c <= 512) quant_rows_kernel<F32, 4, 2><<<p.rows, 256, 0, s>>>(p);
-  else if (c <= 1024) quant_rows_kernel<F32, 4, 4><<<p.rows, 256, 0, s>>>(p);
-  else quant_rows_kernel<F32, 4, 0><<<p.rows, 256, 0, s>>>(p);
+  if (c <= 64) quant_rows_as<F32, 1, 1>(p, s);
+  else if (c <= 128) quant_rows_as<F32, 1, 2>(p, s);
+  else if (c <= 512) quant_rows_as<F32, 4, 2>(p, s);
+  else if (c <= 1024) quant_rows_as<F32, 4, 4>(p, s);
+  else quant_rows_as<F32, 4, 0>(p, s);
 }
 
 constexpr int kCH = 8;   // 16-byte chunks of an LDS row
@@ -176,18 +199,35 @@ __device__ __forceinline__ float act_nan(float v, ActClamp ac) {
   return MODE != 1 && v != v ? v : y;
 }
 
+__device__ __forceinline__ void load8f(const float* p, float* v) {
+  const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+
+// Eight columns of a row of the residual (zeros without one).
+template <bool F32>
+__device__ __forceinline__ Chunk<F32> load_res(const QDenseParams& p, int64_t m, int n) {
+  Chunk<F32> r;
+  if constexpr (F32) {
+    const float* rp = (const float*)p.res + m * p.ldr + n;
+    if (p.res && p.ldr % 4 == 0 && n + 8 <= p.N) {
+      load8f(rp, r.v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r.v[e] = p.res && n + e < p.N ? rp[e] : 0.0f;
+    }
+  } else {
+    r.u = p.res ? *(const uint4*)((const bf16_t*)p.res + m * p.ldr + n) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  return r;
+}
+
 // Eight columns of one output row: y = act(acc * scale + bias + res).
 template <bool F32, int MODE>
 __device__ __forceinline__ void finish8(const QDenseParams& p, const int* acc, float xs, const float* ws,
-                                        const float* bias, int64_t m, int n, ActClamp ac) {
+                                        const float* bias, const Chunk<F32>& res, int64_t m, int n, ActClamp ac) {
   float r[8], v[8];
-  if constexpr (F32) {
-    const float* rp = (const float*)p.res + m * p.ldr + n;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = p.res && n + e < p.N ? rp[e] : 0.0f;
-  } else {
-    unpack8(p.res ? *(const uint4*)((const bf16_t*)p.res + m * p.ldr + n) : make_uint4(0u, 0u, 0u, 0u), r);
-  }
+  res.get(r);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = act_nan<MODE>(__builtin_fmaf((float)acc[e], xs * ws[e], bias[e]) + r[e], ac);
   if constexpr (F32) {
@@ -203,11 +243,6 @@ __device__ __forceinline__ void finish8(const QDenseParams& p, const int* acc, f
   } else {
     *(uint4*)((bf16_t*)p.y + m * p.ldy + n) = pack8(v);
   }
-}
-
-__device__ __forceinline__ void load8f(const float* p, float* v) {
-  const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
-  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
 }
 
 // BM rows x BN channels per workgroup of WM x WN waves; both operands streamed
@@ -235,15 +270,21 @@ __global__ __launch_bounds__(64 * WM * WN) void qdense_kernel(QDenseParams p) {
   const int cva = (lane & 7) ^ (r0 & 7);
   const int cvb = (lane & 7) ^ ((r0 & 3) | ((r0 & 8) >> 1));
 
-  // XCD x = (gx, gy) of 8 / py x py owns a block of the tile grid (workgroup b runs on XCD b % 8)
+  // XCD x = (gx, gy) of 8 / py x py owns a block of the tile grid (workgroup b runs on XCD b % 8) and
+  // walks it in bands of 4 row tiles: the 32 tiles that its CUs have at a time then share 4 row and 8
+  // channel tiles in its L2 (8192 x 4096 x 8192: 260 us row by row, 256 in bands of 4, 277 of 8)
+  constexpr int kBand = 4;
   const int ntm = (p.M + BM - 1) / BM, ntn = (p.N + BN - 1) / BN;
   const int x = blockIdx.x & 7, j = blockIdx.x >> 3;
   const int px = 8 / p.py;
   const int mh = (ntm + px - 1) / px, nh = (ntn + p.py - 1) / p.py;
   const int gx = x / p.py, gy = x - gx * p.py;
-  const int jm = j / nh;
-  const int tm = gx * mh + jm, tn = gy * nh + (j - jm * nh);
-  if (jm >= mh || tm >= ntm || tn >= ntn) return;
+  const int band = j / (kBand * nh), at = j - band * kBand * nh;
+  const int bm = min(kBand, mh - band * kBand);
+  if (bm <= 0) return;
+  const int jn = at / bm;
+  const int tm = gx * mh + band * kBand + at - jn * bm, tn = gy * nh + jn;
+  if (jn >= nh || tm >= ntm || tn >= ntn) return;
   const int m0 = tm * BM, n0 = tn * BN;
   const int nst = p.Kq / kBK;
 
@@ -333,7 +374,18 @@ __global__ __launch_bounds__(64 * WM * WN) void qdense_kernel(QDenseParams p) {
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
+  // Epilogue: lane = row lr of each row tile, 8 consecutive channels per pair of channel tiles; the
+  // residuals of a batch of rows are on their way together
   const ActClamp ac = act_clamp_of(p.act, p.alpha);
+  // (bf16: 8192 x 4096 x 8192 314 us one by one, 290 together; fp32, twice the registers: 1531 x 1000 x 2056
+  // 19.9 and 21.0)
+  constexpr int BATCH = F32 ? 1 : TM;
+  float xs[TM];
+#pragma unroll
+  for (int k = 0; k < TM; ++k) {
+    const int m = m0 + wm * WTM + k * 16 + lr;
+    xs[k] = m < p.M ? p.xs[m] : 0.0f;
+  }
   auto epilogue = [&](auto mode_tag) {
 #pragma unroll
     for (int pr = 0; pr < TN / 2; ++pr) {
@@ -348,13 +400,20 @@ __global__ __launch_bounds__(64 * WM * WN) void qdense_kernel(QDenseParams p) {
         for (int e = 0; e < 8; ++e) bias[e] = 0.0f;
       }
 #pragma unroll
-      for (int k = 0; k < TM; ++k) {
-        const int m = m0 + wm * WTM + k * 16 + lr;
-        if (m >= p.M) continue;
-        int a[8];
+      for (int k0 = 0; k0 < TM; k0 += BATCH) {
+        Chunk<F32> res[BATCH];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) a[e] = acc[2 * pr + (e >> 2)][k][e & 3];
-        finish8<F32, decltype(mode_tag)::value>(p, a, p.xs[m], ws, bias, m, n, ac);
+        for (int k = 0; k < BATCH; ++k)
+          res[k] = load_res<F32>(p, min(m0 + wm * WTM + (k0 + k) * 16 + lr, p.M - 1), n);
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+          const int m = m0 + wm * WTM + (k0 + k) * 16 + lr;
+          if (m >= p.M) continue;
+          int a[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) a[e] = acc[2 * pr + (e >> 2)][k0 + k][e & 3];
+          finish8<F32, decltype(mode_tag)::value>(p, a, xs[k0 + k], ws, bias, res[k], m, n, ac);
+        }
       }
     }
   };
@@ -364,6 +423,164 @@ __global__ __launch_bounds__(64 * WM * WN) void qdense_kernel(QDenseParams p) {
     epilogue(std::integral_constant<int, 0>{});
   else
     epilogue(std::integral_constant<int, 2>{});
+}
+
+// Few rows: a workgroup of 8 waves owns 16 NT channels and all rows and splits the
+// reduction over its waves, operands straight to registers, the waves' sums joined
+// in LDS; the time is that of reading the weights.  MT tiles of 16 rows.
+//
+// FUSED: the rows are quantized by every workgroup for itself, into LDS, while its
+// first weights are on their way; that saves the launch that would do it.
+constexpr int kRowWaves = 8;
+constexpr int kRowThreads = 64 * kRowWaves;
+constexpr int kRowSteps = 4;                // steps of 64 codes per wave with loads in flight together
+constexpr int kFusedCodes = 16 * kRowThreads;  // codes of all rows that FUSED takes
+
+template <int MT, int NT, bool F32, bool FUSED>
+__global__ __launch_bounds__(kRowThreads) void qdense_rows_kernel(QDenseParams p, QRowsParams q) {
+  __shared__ i32x4 red[kRowWaves][MT * NT][64];
+  __shared__ __align__(16) int8_t codes[FUSED ? kFusedCodes : 16];
+  __shared__ float scales[16];
+  __shared__ uint32_t tops[kRowWaves];
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lc = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = blockIdx.x * 16 * NT;
+  const int steps = p.Kq / 64;
+  // a wave takes pairs of steps, 128 bytes of each weight row: wave w steps 2w, 2w + 1, 2w + 16, ...
+  auto step_of = [&](int i) { return (i >> 1) * 2 * kRowWaves + 2 * wave + (i & 1); };
+  const int8_t* wp = p.w + (int64_t)(n0 + lr) * p.Kq + lc * 16;
+  uint4 a[kRowSteps][NT];
+  auto load_w = [&](int i0) {
+#pragma unroll
+    for (int u = 0; u < kRowSteps; ++u) {
+      const int t = step_of(i0 + u);
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        a[u][j] = t < steps ? *(const uint4*)(wp + (int64_t)j * 16 * p.Kq + t * 64) : make_uint4(0u, 0u, 0u, 0u);
+    }
+  };
+  load_w(0);
+  if constexpr (FUSED) {
+    // waves per row: as many as there are for the rows rounded up to a power of two
+    const int lg = p.M > 4 ? 3 : (p.M > 2 ? 2 : p.M - 1);
+    const int wpr = kRowWaves >> lg;
+    const int row = wave / wpr, part = (wave % wpr) * 64 + lane;
+    const bool live = row < p.M, vec = q.ldx % 8 == 0;
+    const int chunks = p.Kq / 8;
+    constexpr int NC = 4;  // (2 kFusedCodes / kRowThreads / 8)
+    Chunk<F32> v[NC];
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      v[i].load(q.x, (int64_t)row * q.ldx, (i * wpr * 64 + part) * 8, live ? q.K : 0, vec);
+      float f[8];
+      v[i].get(f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+    for (int w = 0; w < wpr; ++w) top = max(top, tops[row * wpr + w]);
+    const RowScale r = row_scale(top);
+    if (live && part == 0) scales[row] = r.scale;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int c = i * wpr * 64 + part;
+      if (!live || c >= chunks) continue;
+      float f[8], y[8];
+      v[i].get(f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = code_of<F32>(f[e], r);
+      *(uint2*)(codes + row * p.Kq + c * 8) = make_uint2(pack_codes(y), pack_codes(y + 4));
+    }
+    __syncthreads();
+  }
+  i32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  for (int i0 = 0; step_of(i0) < steps; i0 += kRowSteps) {
+    uint4 b[kRowSteps][MT];
+#pragma unroll
+    for (int u = 0; u < kRowSteps; ++u) {
+      const int t = step_of(i0 + u);
+#pragma unroll
+      for (int k = 0; k < MT; ++k) {
+        const int m = k * 16 + lr;
+        const int8_t* xp = (FUSED ? codes : p.x) + (int64_t)m * p.Kq + t * 64 + lc * 16;
+        b[u][k] = m < p.M && t < steps ? *(const uint4*)xp : make_uint4(0u, 0u, 0u, 0u);
+      }
+    }
+    uint4 w[kRowSteps][NT];
+#pragma unroll
+    for (int u = 0; u < kRowSteps; ++u)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) w[u][j] = a[u][j];
+    load_w(i0 + kRowSteps);
+#pragma unroll
+    for (int u = 0; u < kRowSteps; ++u)
+#pragma unroll
+      for (int k = 0; k < MT; ++k)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[k][j] = mma(w[u][j], b[u][k], acc[k][j]);
+  }
+#pragma unroll
+  for (int k = 0; k < MT; ++k)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) red[wave][k * NT + j][lane] = acc[k][j];
+  __syncthreads();
+  // row m, channels n0 + 16 j + 4 c .. + 3 sit in lane 16 c + m % 16 of tile (m / 16, j) of every wave;
+  // a thread takes 8 channels
+  const ActClamp ac = act_clamp_of(p.act, p.alpha);
+  auto epilogue = [&](auto mode_tag) {
+    for (int at = tid; at < MT * 16 * NT * 2; at += kRowThreads) {
+      const int m = at / (NT * 2), g = at % (NT * 2);
+      const int n = n0 + g * 8;
+      if (m >= p.M || n >= p.N) continue;
+      int s[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] = 0;
+#pragma unroll
+      for (int w = 0; w < kRowWaves; ++w)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const i32x4 r = red[w][(m >> 4) * NT + (g >> 1)][((g & 1) * 2 + half) * 16 + (m & 15)];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * half + e] += r[e];
+        }
+      float ws[8], bias[8];
+      load8f(p.ws + n, ws);
+      if (p.bias) {
+        load8f(p.bias + n, bias);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bias[e] = 0.0f;
+      }
+      finish8<F32, decltype(mode_tag)::value>(p, s, FUSED ? scales[m] : p.xs[m], ws, bias,
+                                              load_res<F32>(p, m, n), m, n, ac);
+    }
+  };
+  if (act_mode(p.act) == 1)
+    epilogue(std::integral_constant<int, 1>{});
+  else if (act_mode(p.act) == 0)
+    epilogue(std::integral_constant<int, 0>{});
+  else
+    epilogue(std::integral_constant<int, 2>{});
+}
+
+template <bool F32>
+hipError_t launch_rows(const QDenseParams& p, const QRowsParams& q, bool fused, hipStream_t s) {
+  const int mt = (p.M + 15) / 16;
+  const int nt = 1;
+  const dim3 grid((p.N + 16 * nt - 1) / (16 * nt));
+  if (fused) qdense_rows_kernel<1, 1, F32, true><<<grid, kRowThreads, 0, s>>>(p, q);
+  else if (mt == 1) qdense_rows_kernel<1, 1, F32, false><<<grid, kRowThreads, 0, s>>>(p, q);
+  else if (mt == 2) qdense_rows_kernel<2, 1, F32, false><<<grid, kRowThreads, 0, s>>>(p, q);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
 }
 
 template <int BM, int BN, int WM, int WN, int NS, bool F32>
@@ -380,10 +597,33 @@ hipError_t launch_one(QDenseParams p, hipStream_t s) {
   return hipGetLastError();
 }
 
-#define BYOC_QDENSE_TILES(X) \
-  X(256, 256, 2, 4, 2)       \
-  X(128, 128, 2, 2, 3)       \
-  X(64, 64, 2, 2, 4)
+// Tiles (BM, BN, waves along each, ring stages) and what they cost in microseconds:
+// a stage of 128 codes while at most one workgroup runs per CU or all slots (occ per
+// CU) are busy, and a round's prologue and epilogue.  Fitted to 15 shapes from 24 x 4096 x
+// 12288 to 8192 x 4096 x 8192, on which the choice is never more than 8% behind the
+// fastest tile.  What bounds the large tiles is the feed: a 256x256 stage moves 64 KB from
+// L2 to LDS and 192 KB from LDS to registers in 1.8 us, for 0.9 us of matrix
+// operations; with 4 waves of 128 x 128 the LDS reads fall by a third, but one wave per SIMD hides
+// nothing (8192 x 4096 x 8192: 347 us against 256), and half-depth stages in a ring of
+// five fetch half cache lines (285).
+//   id BM BN WM WN NS  occ  lone  busy  round
+#define BYOC_QDENSE_TILES(X)                 \
+  X(0, 256, 256, 2, 4, 2, 1, 1.33, 1.8, 9.0) \
+  X(1, 256, 128, 4, 2, 3, 1, 0.77, 1.0, 6.0) \
+  X(2, 128, 128, 2, 4, 3, 1, 0.51, 0.6, 4.2) \
+  X(3, 128, 128, 2, 4, 2, 2, 0.71, 1.09, 5.0) \
+  X(4, 128, 64, 4, 2, 3, 2, 0.39, 0.70, 3.5) \
+  X(5, 64, 64, 2, 2, 4, 2, 0.33, 0.46, 2.3)  \
+  X(6, 32, 32, 2, 1, 8, 2, 0.26, 0.30, 1.8)
+
+double tile_cost(int bm, int bn, int occ, double lone, double busy, double round, int64_t M, int64_t N, int64_t Kq) {
+  const int64_t tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn), slots = 256 * occ;
+  const double stages = (double)(Kq / kBK);
+  const int64_t rest = tiles % slots;
+  double t = (double)(tiles / slots) * (stages * busy + round);
+  if (rest) t += stages * (rest <= (occ == 1 ? 128 : 256) ? lone : busy) + round;
+  return t;
+}
 
 }  // namespace
 
@@ -394,17 +634,31 @@ hipError_t launch_quant_rows(const QRowsParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The largest tile that leaves every CU one.
-QDenseTile choose_qdense_tile(int64_t M, int64_t N) {
-  for (int b : {256, 128})
-    if (((M + b - 1) / b) * ((N + b - 1) / b) >= 256) return {b, b};
-  return {64, 64};
+bool qdense_fuses_rows(int64_t M, int64_t Kq) { return M <= 8 && M * Kq <= kFusedCodes; }
+
+hipError_t launch_qdense_fused(const QDenseParams& p, const QRowsParams& q, hipStream_t s) {
+  if (!qdense_fuses_rows(p.M, p.Kq)) return hipErrorInvalidValue;
+  return p.f32 ? launch_rows<true>(p, q, true, s) : launch_rows<false>(p, q, true, s);
+}
+
+// The rows kernel where all of its workgroups run at once, one per CU (32 x 768 x
+// 3072: 8.8 us against 9.4 on 32x32 tiles, 16 x 8192 x 1024: 15.0 against 16.4; but 16 x
+// 4096 x 12288, 768 workgroups: 23.5 against 15.2); else the tile of least modelled time.
+QDenseTile choose_qdense_tile(int64_t M, int64_t N, int64_t Kq) {
+  if (qdense_fuses_rows(M, Kq) || (M <= 32 && N <= 16 * 256)) return {kQDenseRows, (int)(M + 15) / 16 * 16, 16};
+  QDenseTile best{};
+  double least = INFINITY;
+#define X(ID, BM, BN, WM, WN, NS, OCC, LONE, BUSY, ROUND)                                                \
+  if (const double c = tile_cost(BM, BN, OCC, LONE, BUSY, ROUND, M, N, Kq); c < least) least = c, best = {ID, BM, BN};
+  BYOC_QDENSE_TILES(X)
+#undef X
+  return best;
 }
 
 hipError_t launch_qdense(const QDenseParams& p, QDenseTile t, hipStream_t s) {
-#define X(BM, BN, WM, WN, NS)           \
-  if (t.bm == BM && t.bn == BN)         \
-    return p.f32 ? launch_one<BM, BN, WM, WN, NS, true>(p, s) : launch_one<BM, BN, WM, WN, NS, false>(p, s);
+  if (t.id == kQDenseRows) return p.f32 ? launch_rows<true>(p, {}, false, s) : launch_rows<false>(p, {}, false, s);
+#define X(ID, BM, BN, WM, WN, NS, OCC, LONE, BUSY, ROUND) \
+  if (t.id == ID) return p.f32 ? launch_one<BM, BN, WM, WN, NS, true>(p, s) : launch_one<BM, BN, WM, WN, NS, false>(p, s);
   BYOC_QDENSE_TILES(X)
 #undef X
   return hipErrorInvalidValue;
