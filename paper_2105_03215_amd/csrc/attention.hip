@@ -33,6 +33,7 @@ typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 
 constexpr int kKeys = 32;   // keys of a tile
 constexpr int kCols = 32;   // packed query rows of a tile
+constexpr int kPitch = 33;  // of the waves' results in LDS: free of bank conflicts along either axis
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -55,6 +56,70 @@ __device__ __forceinline__ int seen_keys(const AttnParams& p, int len, int r) {
 
 __device__ __forceinline__ int batch_len(const AttnParams& p, int b) {
   return p.lengths ? min(max(p.lengths[b], 0), p.k_len) : p.k_len;
+}
+
+// The key axis of few rows is split into p.chunks chunks, shared by the sequences in
+// proportion to their lengths, which only the device knows: chunks of `size` tiles each,
+// the first of sequence b number `first`, `count` of them.  With size = ceil(tiles of all /
+// (chunks - batch)) they never need more than p.chunks.  More than 64 sequences
+// (lanes) get the same number each.  chunks == batch: a sequence each.
+// (floats of the workspace's head, a multiple of 4 so that the sums can be written 16 bytes at a time)
+__host__ __device__ __forceinline__ int64_t head_floats(const AttnParams& p) { return (2 * (int64_t)p.batch + 3) / 4 * 4; }
+struct Chunks {
+  int first, count, size;
+};
+__device__ __forceinline__ Chunks lane_chunks(const AttnParams& p) {
+  const int lane = threadIdx.x & 63;
+  const int mine = lane < p.batch ? (batch_len(p, lane) + p.tile_keys - 1) / p.tile_keys : 0;
+  int total = mine;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d, 64);
+  Chunks c;
+  const int spare = p.chunks - p.batch;
+  c.size = max(1, (total + spare - 1) / spare);
+  c.count = (mine + c.size - 1) / c.size;
+  c.first = c.count;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int x = __shfl_up(c.first, d, 64);
+    if (lane >= d) c.first += x;
+  }
+  c.first -= c.count;
+  return c;
+}
+__device__ __forceinline__ Chunks uniform_chunks(const AttnParams& p, int b) {
+  const int per = p.chunks / p.batch;
+  const int tiles = (p.k_len + p.tile_keys - 1) / p.tile_keys;
+  return Chunks{b * per, per, (tiles + per - 1) / per};
+}
+// The sequence of chunk q, -1 if no sequence needs it.
+__device__ __forceinline__ int chunk_batch(const AttnParams& p, int q, Chunks* out) {
+  if (p.batch > 64 || p.chunks == p.batch) {
+    const int b = q / (p.chunks / p.batch);
+    *out = uniform_chunks(p, b);
+    return b;
+  }
+  const Chunks c = lane_chunks(p);
+  const unsigned long long at = __ballot(q >= c.first && q < c.first + c.count);
+  if (at == 0) return -1;
+  const int b = __builtin_ctzll(at);
+  *out = Chunks{__builtin_amdgcn_readlane(c.first, b), __builtin_amdgcn_readlane(c.count, b), c.size};
+  return b;
+}
+// The workspace: for each sequence the first of its chunks and their number (written by that chunk's
+// workgroup, so that the join need not count them again; a sequence without keys has none), then the
+// sums, then the maxima and weights.
+__device__ __forceinline__ void note_chunks(const AttnParams& p, int b, int q, const Chunks& c) {
+  if (q == c.first && threadIdx.x == 0) ((int2*)p.ws)[b] = make_int2(c.first, c.count);
+}
+// Where the result of chunk q of packed row `row` of key head kh stands: D sums, and its maximum and weight.
+__device__ __forceinline__ float* part_sums(const AttnParams& p, int kh, int row, int q) {
+  const int64_t rows = (int64_t)p.q_len * p.group;
+  return p.ws + head_floats(p) + ((kh * rows + row) * p.chunks + q) * p.D;
+}
+__device__ __forceinline__ float* part_scale(const AttnParams& p, int kh, int row, int q) {
+  const int64_t rows = (int64_t)p.q_len * p.group;
+  return p.ws + head_floats(p) + (p.kv_heads * rows * p.D + (kh * rows + row) * 2) * p.chunks + q * 2;
 }
 
 // Swizzle keys of the LDS tiles, on 16-byte chunks of a row: key rows are read 16
@@ -108,24 +173,26 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   __shared__ __align__(16) char lds[NW * NBUF * 2 * TILE];
   __shared__ float ml[NW][2][kCols];
   static_assert(sizeof(lds) + sizeof(ml) <= kLdsLimit, "LDS");
-  static_assert(NW * NBUF * 2 * TILE >= NW * DP * kCols * 4, "the waves' results take the tiles' place");
+  static_assert(NW * NBUF * 2 * TILE >= NW * DP * kPitch * 4, "the waves' results take the tiles' place");
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int R = p.q_len * p.group;
   const int ncb = (R + kCols - 1) / kCols;
-  int bid = blockIdx.x;
-  const int bh = bid % (p.batch * p.kv_heads);
-  bid /= p.batch * p.kv_heads;
-  const int cb = bid % ncb, split = bid / ncb;
-  const int b = bh / p.kv_heads, kh = bh - b * p.kv_heads;
+  const int kh = blockIdx.x % p.kv_heads;
+  const int rest = blockIdx.x / p.kv_heads;
+  const int cb = rest % ncb, chunk = rest / ncb;
+  const bool joined = p.chunks > p.batch;
+  Chunks ck;
+  const int b = __builtin_amdgcn_readfirstlane(chunk_batch(p, chunk, &ck));
+  if (b < 0) return;
+  if (joined && cb == 0 && kh == 0) note_chunks(p, b, chunk, ck);
   const int len = batch_len(p, b);
   const int row = cb * kCols + col;
   const int lim = seen_keys(p, len, row);
   const int kend = seen_keys(p, len, min(cb * kCols + kCols, R) - 1);  // (rows see more keys further down)
-  const int tiles = (kend + kKeys - 1) / kKeys;
-  const int per = (tiles + p.splits - 1) / p.splits;
-  const int t_end = min(split * per + per, tiles);
+  const int t0 = (chunk - ck.first) * ck.size;
+  const int t_end = min(t0 + ck.size, (kend + kKeys - 1) / kKeys);
 
   // this lane's part of its query row: 16-byte chunks 2 st + h
   constexpr int QS = CPR / 2;
@@ -144,25 +211,23 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   const char* kb = (const char*)p.k + (int64_t)b * p.k_len * sk + kh * p.D * ES;
   const char* vb = (const char*)p.v + (int64_t)b * p.k_len * sv + kh * p.D * ES;
   char* mine = lds + wave * (NBUF * 2 * TILE);
-  auto fill = [&](int buf, int t) {
+  // keys or values of a tile; rows past the length (and tiles past the end) read as zeros, whatever stands there
+  auto fill = [&](int buf, int t, auto values_tag) {
+    constexpr bool VALUES = decltype(values_tag)::value;
     const int k0 = t * kKeys;
-    const int n = t < t_end ? min(kKeys, len - k0) : 0;  // rows past the length read as zeros, whatever they hold
-    const i32x4 kr = buffer_rsrc(kb + (int64_t)k0 * sk, n > 0 ? (n - 1) * (int)sk + p.D * ES : 0);
-    const i32x4 vr = buffer_rsrc(vb + (int64_t)k0 * sv, n > 0 ? (n - 1) * (int)sv + p.D * ES : 0);
-    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(mine + buf * 2 * TILE));
+    const int n = t < t_end ? min(kKeys, len - k0) : 0;
+    const int64_t stride = VALUES ? sv : sk;
+    const i32x4 r4 = buffer_rsrc((VALUES ? vb : kb) + (int64_t)k0 * stride, n > 0 ? (n - 1) * (int)stride + p.D * ES : 0);
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(mine + (buf * 2 + VALUES) * TILE));
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int r = (i * 64 + lane) / CPR, s = (i * 64 + lane) % CPR;
-      const int c = s ^ k_key<CPR>(r);
-      lds_fill16(kr, at + i * 1024, c * 16 < p.D * ES ? (uint32_t)(r * (int)sk + c * 16) : kOOB);
-    }
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int r = (i * 64 + lane) / CPR, s = (i * 64 + lane) % CPR;
-      const int c = s ^ v_key<CPR>(r);
-      lds_fill16(vr, at + TILE + i * 1024, c * 16 < p.D * ES ? (uint32_t)(r * (int)sv + c * 16) : kOOB);
+      const int c = s ^ (VALUES ? v_key<CPR>(r) : k_key<CPR>(r));
+      lds_fill16(r4, at + i * 1024, c * 16 < p.D * ES ? (uint32_t)(r * (int)stride + c * 16) : kOOB);
     }
   };
+  constexpr std::integral_constant<bool, false> keys{};
+  constexpr std::integral_constant<bool, true> values{};
 
   f32x16 o[DB];
 #pragma unroll
@@ -170,9 +235,13 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   float m = -INFINITY, l = 0.0f;
   const float c2 = p.scale * 1.44269504088896340736f;
 
+  // Loads of 2 NBUF half tiles are in flight: a half is filled again as soon as it has been read.
+  auto landed = [] { asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * NBUF - 1) * NI) : "memory"); };
+  auto read = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
   auto compute = [&](int buf, int t) {
     const char* kt = mine + buf * 2 * TILE;
     const char* vt = kt + TILE;
+    landed();
     f32x16 s{};
 #pragma unroll
     for (int st = 0; st < QS; ++st) {
@@ -185,6 +254,8 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
         for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(af[e], bf[e], s, 0, 0, 0);
       }
     }
+    read();
+    fill(buf, t + NBUF * NW, keys);
     const int k0 = t * kKeys + 4 * h;
     float top = -INFINITY;
 #pragma unroll
@@ -205,6 +276,7 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
     l = l * keep + sum;
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] *= keep;
+    landed();
     if constexpr (BF) {
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
@@ -228,25 +300,19 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
     }
   };
 
-  int t = split * per + wave, buf = 0;
-  if constexpr (NBUF == 2) {
-    fill(0, t);
-    for (; t < t_end; t += NW) {
-      fill(buf ^ 1, t + NW);
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
-      compute(buf, t);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tile's reads are done before it is filled again
-      buf ^= 1;
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  } else {
-    for (; t < t_end; t += NW) {
-      fill(0, t);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      compute(0, t);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
+#pragma unroll
+  for (int n = 0; n < NBUF; ++n) {
+    fill(n, t0 + wave + n * NW, keys);
+    fill(n, t0 + wave + n * NW, values);
   }
+  int buf = 0;
+  for (int t = t0 + wave; t < t_end; t += NW) {
+    compute(buf, t);
+    read();
+    fill(buf, t + NBUF * NW, values);
+    buf = NBUF == 2 ? buf ^ 1 : 0;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
   // the waves' results: a common maximum, then the sums in wave order
   l = half_sum(l);
@@ -260,49 +326,54 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   for (int w = 1; w < NW; ++w) top = fmaxf(top, ml[w][0][col]);
   const float use = top == -INFINITY ? 0.0f : top;
   const float f = exp2_(m - use);
-  float* const os = (float*)lds;  // [wave][DP][32]
+  float* const os = (float*)lds;  // [wave][column][packed row]
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) os[(wave * DP + d * 32 + 8 * (i >> 2) + 4 * h + (i & 3)) * kCols + col] = o[d][i] * f;
+    for (int i = 0; i < 16; ++i) os[(wave * DP + d * 32 + 8 * (i >> 2) + 4 * h + (i & 3)) * kPitch + col] = o[d][i] * f;
   float total = 0.0f;
 #pragma unroll
   for (int w = 0; w < NW; ++w) total += ml[w][1][col] * exp2_(ml[w][0][col] - use);
   __syncthreads();
-  if (row >= R) return;
-  // thread = packed row col, columns 8 e .. 8 e + 7 in turn
-  const float inv = lim > 0 ? 1.0f / total : 0.0f;
-  const int i = row / p.group, g = row - i * p.group;
-  const int64_t part = ((int64_t)bh * R + row) * p.splits + split;
-  for (int e = tid >> 5; e * 8 < p.D; e += 2 * NW) {
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[j] = os[(e * 8 + j) * kCols + col];
-#pragma unroll
-      for (int w = 1; w < NW; ++w) v[j] += os[(w * DP + e * 8 + j) * kCols + col];
-    }
-    if (p.splits > 1) {
-      float* out = p.ws + part * p.D + e * 8;
-      *(float4*)out = make_float4(v[0], v[1], v[2], v[3]);
-      *(float4*)(out + 4) = make_float4(v[4], v[5], v[6], v[7]);
-      continue;
-    }
-    // (a row without keys is zero; one whose seen scores are all -inf divides zero by zero, as the softmax does)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = lim > 0 ? v[j] * inv : 0.0f;
-    char* out = (char*)p.y + ((b * (int64_t)p.q_len + i) * p.ldy + (kh * p.group + g) * p.D + e * 8) * ES;
-    if constexpr (BF) {
-      *(uint4*)out = pack8(v);
-    } else {
-      *(float4*)out = make_float4(v[0], v[1], v[2], v[3]);
-      *(float4*)(out + 16) = make_float4(v[4], v[5], v[6], v[7]);
+  if (wave == 0 && h == 0) {
+    // the joined weight, where the outputs' threads find it; a row without keys is zero, one whose
+    // seen scores are all -inf divides zero by zero, as the softmax does
+    if (!joined) ml[0][1][col] = total;
+    else if (row < R) {
+      float* out = part_scale(p, kh, row, chunk);
+      out[0] = top;
+      out[1] = total;
     }
   }
-  if (p.splits > 1 && tid < kCols) {
-    float* out = p.ws + (int64_t)p.batch * p.kv_heads * R * p.splits * p.D + part * 2;
-    out[0] = top;
-    out[1] = total;
+  if (!joined) __syncthreads();
+  // thread = 4 columns of a packed row, rows in turn
+  const int rows = min(kCols, R - cb * kCols);
+  for (int at = tid; at < rows * (DP / 4); at += 64 * NW) {
+    const int c = at / (DP / 4), e = at % (DP / 4) * 4;
+    if (e >= p.D) continue;
+    float v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[j] = os[(e + j) * kPitch + c];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) v[j] += os[(w * DP + e + j) * kPitch + c];
+    }
+    const int r = cb * kCols + c;
+    if (joined) {
+      *(float4*)(part_sums(p, kh, r, chunk) + e) = make_float4(v[0], v[1], v[2], v[3]);
+      continue;
+    }
+    const float sum = ml[0][1][c];
+    const bool any = seen_keys(p, len, r) > 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = any ? v[j] / sum : 0.0f;
+    const int i = r / p.group, g = r - i * p.group;
+    T* out = (T*)p.y + (b * (int64_t)p.q_len + i) * p.ldy + (kh * p.group + g) * p.D + e;
+    if constexpr (BF) {
+      *(uint2*)out = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
+    } else {
+      *(float4*)out = make_float4(v[0], v[1], v[2], v[3]);
+    }
   }
 }
 
@@ -330,25 +401,26 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int R = p.q_len * p.group;
-  const int nh = p.batch * p.kv_heads;
+  const int nh = p.chunks * p.kv_heads;
   const int nt = (R + 32 * NW - 1) / (32 * NW);
   // Head fastest: with a multiple of 8 heads each XCD (workgroup b runs on XCD b % 8) keeps to its own
   // heads' keys and values; the last rows first, which see the most keys under a causal mask.
-  int bid = blockIdx.x;
-  const int bh = bid % nh;
-  bid /= nh;
-  const int split = bid % p.splits;
-  const int tile = nt - 1 - bid / p.splits;
-  const int b = bh / p.kv_heads, kh = bh - b * p.kv_heads;
+  const int bh = blockIdx.x % nh;
+  const int tile = nt - 1 - blockIdx.x / nh;
+  const int chunk = bh / p.kv_heads, kh = bh - chunk * p.kv_heads;
+  const bool joined = p.chunks > p.batch;
+  Chunks ck;
+  const int b = __builtin_amdgcn_readfirstlane(chunk_batch(p, chunk, &ck));
+  if (b < 0) return;
+  if (joined && tile == 0 && kh == 0) note_chunks(p, b, chunk, ck);
   const int len = batch_len(p, b);
   const int row0 = tile * 32 * NW + wave * 32, row = row0 + col;
   const int lim = seen_keys(p, len, row);
   const int lim_lo = seen_keys(p, len, min(row0, R - 1));            // (rows see more keys further down)
   const int lim_hi = row0 < R ? seen_keys(p, len, min(row0 + 32, R) - 1) : 0;
   const int kend = seen_keys(p, len, min((tile + 1) * 32 * NW, R) - 1);
-  const int tiles = (kend + kTileKeys - 1) / kTileKeys;
-  const int per = (tiles + p.splits - 1) / p.splits;
-  const int t0 = split * per, t_end = min(t0 + per, tiles);
+  const int t0 = (chunk - ck.first) * ck.size;
+  const int t_end = min(t0 + ck.size, (kend + kTileKeys - 1) / kTileKeys);
 
   uint4 qf[QS];
   const int i = row / p.group, g = row - i * p.group;
@@ -455,17 +527,17 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
   }
   if (row >= R) return;
   l = half_sum(l);
-  if (p.splits > 1) {
-    const int64_t part = ((int64_t)bh * R + row) * p.splits + split;
+  if (joined) {
+    float* const sums = part_sums(p, kh, row, chunk);
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int c = d * 32 + 8 * e + 4 * h;
-        if (c < p.D) *(float4*)(p.ws + part * p.D + c) = make_float4(o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]);
+        if (c < p.D) *(float4*)(sums + c) = make_float4(o[d][4 * e], o[d][4 * e + 1], o[d][4 * e + 2], o[d][4 * e + 3]);
       }
     if (h == 0) {
-      float* out = p.ws + (int64_t)nh * R * p.splits * p.D + part * 2;
+      float* out = part_scale(p, kh, row, chunk);
       out[0] = m;
       out[1] = l;
     }
@@ -494,30 +566,49 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
     }
 }
 
-// Joins the splits of a packed row: thread = 4 columns.
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p) {
+// Joins the chunks of a packed row: a group of D / 4 lanes (of 64 / 32 / 16 lanes), 4 columns each.
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p, int lanes) {
   const int R = p.q_len * p.group;
-  const int per = p.D / 4;
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t pr = at / per;  // (batch, key head, packed row)
-  if (pr >= (int64_t)p.batch * p.kv_heads * R) return;
-  const int c = (int)(at - pr * per) * 4;
-  const int bh = (int)(pr / R), row = (int)(pr - (int64_t)bh * R);
-  const int b = bh / p.kv_heads, kh = bh - b * p.kv_heads;
-  const float* ml = p.ws + (int64_t)p.batch * p.kv_heads * R * p.splits * p.D + pr * p.splits * 2;
-  const float* os = p.ws + pr * p.splits * p.D + c;
-  float top = -INFINITY;
-  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, ml[2 * s]);
-  const float use = top == -INFINITY ? 0.0f : top;
-  float total = 0.0f;
+  // rows of one sequence per workgroup row (blockIdx.y), so that a wave has one set of chunks
+  const int b = blockIdx.y;
+  const int len = batch_len(p, b);
+  const int2 ck = len > 0 ? ((const int2*)p.ws)[b] : make_int2(0, 0);  // first chunk, count
+  const int at = blockIdx.x * (256 / lanes) + threadIdx.x / lanes;  // (key head, packed row)
+  const int c = threadIdx.x % lanes * 4;
+  if (at >= p.kv_heads * R || c >= p.D) return;
+  const int kh = at / R, row = at - kh * R;
+  const float* ml = part_scale(p, kh, row, ck.x);
+  const float* os = part_sums(p, kh, row, ck.x) + c;
+  // eight chunks at a time, their loads on the way together
+  float top = -INFINITY, total = 0.0f;
   float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < p.splits; ++s) {
-    const float f = exp2_(ml[2 * s] - use);
-    const float4 x = *(const float4*)(os + (int64_t)s * p.D);
-    total += ml[2 * s + 1] * f;
-    v[0] += x.x * f, v[1] += x.y * f, v[2] += x.z * f, v[3] += x.w * f;
+  for (int s0 = 0; s0 < ck.y; s0 += 8) {
+    float2 m[8];
+    float4 x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int s = min(s0 + k, ck.y - 1);
+      m[k] = *(const float2*)(ml + 2 * s);
+      x[k] = *(const float4*)(os + (int64_t)s * p.D);
+    }
+    float most = top;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) most = fmaxf(most, m[k].x);
+    const float use = most == -INFINITY ? 0.0f : most;
+    const float keep = exp2_(top - use);
+    top = most;
+    total *= keep;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] *= keep;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (s0 + k >= ck.y) break;
+      const float f = exp2_(m[k].x - use);
+      total += m[k].y * f;
+      v[0] += x[k].x * f, v[1] += x[k].y * f, v[2] += x[k].z * f, v[3] += x[k].w * f;
+    }
   }
-  const bool any = seen_keys(p, batch_len(p, b), row) > 0;
+  const bool any = seen_keys(p, len, row) > 0;
   const int i = row / p.group, g = row - i * p.group;
   const int64_t out = (b * (int64_t)p.q_len + i) * p.ldy + (kh * p.group + g) * p.D + c;
 #pragma unroll
@@ -528,49 +619,58 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p) {
     *(uint2*)((bf16_t*)p.y + out) = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
 }
 
-int row_blocks(const AttnParams& p, int rows) {
-  return p.batch * p.kv_heads * ceil_div((int64_t)p.q_len * p.group, rows);
-}
+// waves of a workgroup of the rows kernel: as many as the LDS has tiles for
+int row_waves(const AttnParams& p) { return p.D > 128 ? 2 : p.D > 64 || p.f32 ? 4 : 8; }
 
-// Whether the rows go through the shared tiles: with 32 packed rows or fewer three of
-// its four waves would idle, and fp32 products are bound by the matrix cores either way.
-bool tiled(const AttnParams& p) { return !p.f32 && p.q_len * (int64_t)p.group > 32; }
+// workgroups along the rows
+int row_blocks(const AttnParams& p) {
+  return ceil_div((int64_t)p.q_len * p.group, p.tile_rows);
+}
 
 }  // namespace
 
-// Enough workgroups for two on each of the 256 CUs, and 128 keys (tiles: 512) in each at least.
+// The kernel and the split.  The shared tiles take more than 32 packed rows (with fewer three
+// of their four waves would idle; fp32 products are bound by the matrix cores either way).
 void choose_attention(AttnParams& p) {
-  const bool t = tiled(p);
-  const int blocks = row_blocks(p, t ? 128 : kCols);
-  const int want = t ? (blocks >= 256 ? 1 : 512 / blocks) : ceil_div(512, blocks);
-  p.splits = std::max(1, std::min(std::min(want, ceil_div(p.k_len, t ? 512 : 4 * kKeys)), 256));
+  const bool tiled = !p.f32 && p.q_len * (int64_t)p.group > 32;
+  p.tile_rows = tiled ? 128 : kCols;
+  p.tile_keys = tiled ? kTileKeys : kKeys;
+  const int64_t blocks = (int64_t)p.batch * p.kv_heads * row_blocks(p);
+  // Tiles: a split fills the two workgroups that a CU has room for where there is less than one.
+  int64_t most = blocks >= 256 ? 1 : std::min<int64_t>(512 / blocks, ceil_div(p.k_len, 512));
+  if (!tiled) {
+    // Rows: one workgroup has a CU to itself; three rounds of its waves in each at least, which take as
+    // long as the join
+    const int round = kKeys * row_waves(p);
+    most = std::min<int64_t>(256 / std::min<int64_t>(blocks, 256), ceil_div(p.k_len, round) / 3);
+  }
+  p.chunks = p.batch * (int)std::max<int64_t>(1, std::min<int64_t>(most, 256));
 }
 
 const char* attention_name(const AttnParams& p) {
-  return p.f32 ? "attention_rows_f32" : tiled(p) ? "attention_tiles" : "attention_rows";
+  return p.f32 ? "attention_rows_f32" : p.tile_rows > kCols ? "attention_tiles" : "attention_rows";
 }
 
 int64_t attn_workspace(const AttnParams& p) {
-  if (p.splits <= 1) return 0;
-  return (int64_t)p.batch * p.kv_heads * p.q_len * p.group * p.splits * (p.D + 2) * 4;
+  if (p.chunks <= p.batch) return 0;
+  return (head_floats(p) + (int64_t)p.kv_heads * p.q_len * p.group * p.chunks * (p.D + 2)) * 4;
 }
 
 hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
-  if (p.D < 8 || p.D > 256 || p.D % 8 != 0 || p.splits < 1) return hipErrorInvalidValue;
-  if (tiled(p)) {
-    const int grid = row_blocks(p, 128) * p.splits;
+  if (p.D < 8 || p.D > 256 || p.D % 8 != 0 || p.chunks < p.batch) return hipErrorInvalidValue;
+  const int grid = p.chunks * p.kv_heads * row_blocks(p);
+  if (p.tile_rows > kCols) {
     if (p.D <= 64) attention_tiles_kernel<64><<<grid, 256, 0, s>>>(p);
     else if (p.D <= 128) attention_tiles_kernel<128><<<grid, 256, 0, s>>>(p);
     else attention_tiles_kernel<256><<<grid, 256, 0, s>>>(p);
     return hipGetLastError();
   }
-  const int grid = row_blocks(p, kCols) * p.splits;
   if (p.f32) {
     if (p.D <= 64) attention_rows_kernel<float, 64, 4><<<grid, 256, 0, s>>>(p);
     else if (p.D <= 128) attention_rows_kernel<float, 128, 4><<<grid, 256, 0, s>>>(p);
     else attention_rows_kernel<float, 256, 2><<<grid, 128, 0, s>>>(p);
   } else {
-    if (p.D <= 64) attention_rows_kernel<bf16_t, 64, 4><<<grid, 256, 0, s>>>(p);
+    if (p.D <= 64) attention_rows_kernel<bf16_t, 64, 8><<<grid, 512, 0, s>>>(p);
     else if (p.D <= 128) attention_rows_kernel<bf16_t, 128, 4><<<grid, 256, 0, s>>>(p);
     else attention_rows_kernel<bf16_t, 256, 2><<<grid, 128, 0, s>>>(p);
   }
@@ -578,8 +678,9 @@ hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
 }
 
 hipError_t launch_attention_join(const AttnParams& p, hipStream_t s) {
-  const int64_t n = (int64_t)p.batch * p.kv_heads * p.q_len * p.group * (p.D / 4);
-  attention_join_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(p);
+  const int lanes = p.D <= 64 ? 16 : p.D <= 128 ? 32 : 64;
+  const dim3 grid(ceil_div((int64_t)p.kv_heads * p.q_len * p.group, 256 / lanes), p.batch);
+  attention_join_kernel<<<grid, 256, 0, s>>>(p, lanes);
   return hipGetLastError();
 }
 

@@ -1337,7 +1337,7 @@ void Planner::plan_attention(int ni) {
   L.info.flops = 4 * (int64_t)n.batch * n.heads * n.q_len * n.k_len * n.head_dim;
   L.info.bytes = 2 * act_bytes(n.out) + 2 * (int64_t)n.batch * n.k_len * n.kv_heads * n.head_dim * es;
   name(L, attention_name(p));
-  if (p.splits <= 1) {
+  if (p.chunks <= p.batch) {
     e->launches.push_back(L);
     return;
   }

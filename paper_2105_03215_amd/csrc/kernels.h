@@ -510,15 +510,16 @@ struct AttnParams {
   const void* v;
   const int* lengths;  // [batch] or nullptr (k_len)
   void* y;             // [batch * q_len][ldy]
-  float* ws;           // attn_workspace() bytes when splits > 1
+  float* ws;           // attn_workspace() bytes when chunks > batch
   int64_t ldq, ldk, ldv, ldy;
   int batch, q_len, k_len, kv_heads, group, D;
   int causal;
-  int splits;
+  int tile_rows, tile_keys;  // packed query rows and keys of a tile (set with chunks by choose_attention)
+  int chunks;                // of the key axes of all sequences; batch: one each, no join
   float scale;
   int f32;
 };
-void choose_attention(AttnParams& p);  // the split of the key axis
+void choose_attention(AttnParams& p);  // the kernel and the split of the key axes
 const char* attention_name(const AttnParams& p);
 int64_t attn_workspace(const AttnParams& p);
 hipError_t launch_attention(const AttnParams& p, hipStream_t s);
