@@ -54,6 +54,9 @@ __device__ __forceinline__ int seen_keys(const AttnParams& p, int len, int r) {
   return min(max(len - p.q_len + r / p.group + 1, 0), len);
 }
 
+// (a value that is the same in all lanes, said to the compiler: what is computed from it stays in scalar registers)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 __device__ __forceinline__ int batch_len(const AttnParams& p, int b) {
   return p.lengths ? min(max(p.lengths[b], 0), p.k_len) : p.k_len;
 }
@@ -103,7 +106,7 @@ __device__ __forceinline__ int chunk_batch(const AttnParams& p, int q, Chunks* o
   const unsigned long long at = __ballot(q >= c.first && q < c.first + c.count);
   if (at == 0) return -1;
   const int b = __builtin_ctzll(at);
-  *out = Chunks{__builtin_amdgcn_readlane(c.first, b), __builtin_amdgcn_readlane(c.count, b), c.size};
+  *out = Chunks{__builtin_amdgcn_readlane(c.first, b), __builtin_amdgcn_readlane(c.count, b), uniform(c.size)};
   return b;
 }
 // The workspace: for each sequence the first of its chunks and their number (written by that chunk's
@@ -176,7 +179,7 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   static_assert(NW * NBUF * 2 * TILE >= NW * DP * kPitch * 4, "the waves' results take the tiles' place");
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = uniform(tid >> 6);
   const int R = p.q_len * p.group;
   const int ncb = (R + kCols - 1) / kCols;
   const int kh = blockIdx.x % p.kv_heads;
@@ -184,13 +187,13 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   const int cb = rest % ncb, chunk = rest / ncb;
   const bool joined = p.chunks > p.batch;
   Chunks ck;
-  const int b = __builtin_amdgcn_readfirstlane(chunk_batch(p, chunk, &ck));
+  const int b = uniform(chunk_batch(p, chunk, &ck));
   if (b < 0) return;
   if (joined && cb == 0 && kh == 0) note_chunks(p, b, chunk, ck);
-  const int len = batch_len(p, b);
+  const int len = uniform(batch_len(p, b));
   const int row = cb * kCols + col;
   const int lim = seen_keys(p, len, row);
-  const int kend = seen_keys(p, len, min(cb * kCols + kCols, R) - 1);  // (rows see more keys further down)
+  const int kend = uniform(seen_keys(p, len, min(cb * kCols + kCols, R) - 1));  // (rows see more keys further down)
   const int t0 = (chunk - ck.first) * ck.size;
   const int t_end = min(t0 + ck.size, (kend + kKeys - 1) / kKeys);
 
@@ -395,11 +398,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
   constexpr int TILE = kTileKeys * RB;
   constexpr int NI = TILE / (NW * 1024);  // loads of a tile per lane
   constexpr int DB = DP / 32, QS = CPR / 2, KB = kTileKeys / 32;
-  __shared__ __align__(16) char lds[4 * TILE];
+  __shared__ __align__(1024) char lds[4 * TILE];
   static_assert(sizeof(lds) <= kLdsLimit, "LDS");
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = uniform(tid >> 6);
   const int R = p.q_len * p.group;
   const int nh = p.chunks * p.kv_heads;
   const int nt = (R + 32 * NW - 1) / (32 * NW);
@@ -410,15 +413,15 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
   const int chunk = bh / p.kv_heads, kh = bh - chunk * p.kv_heads;
   const bool joined = p.chunks > p.batch;
   Chunks ck;
-  const int b = __builtin_amdgcn_readfirstlane(chunk_batch(p, chunk, &ck));
+  const int b = uniform(chunk_batch(p, chunk, &ck));
   if (b < 0) return;
   if (joined && tile == 0 && kh == 0) note_chunks(p, b, chunk, ck);
-  const int len = batch_len(p, b);
+  const int len = uniform(batch_len(p, b));
   const int row0 = tile * 32 * NW + wave * 32, row = row0 + col;
   const int lim = seen_keys(p, len, row);
-  const int lim_lo = seen_keys(p, len, min(row0, R - 1));            // (rows see more keys further down)
-  const int lim_hi = row0 < R ? seen_keys(p, len, min(row0 + 32, R) - 1) : 0;
-  const int kend = seen_keys(p, len, min((tile + 1) * 32 * NW, R) - 1);
+  const int lim_lo = uniform(seen_keys(p, len, min(row0, R - 1)));  // (rows see more keys further down)
+  const int lim_hi = uniform(row0 < R ? seen_keys(p, len, min(row0 + 32, R) - 1) : 0);
+  const int kend = uniform(seen_keys(p, len, min((tile + 1) * 32 * NW, R) - 1));
   const int t0 = (chunk - ck.first) * ck.size;
   const int t_end = min(t0 + ck.size, (kend + kTileKeys - 1) / kTileKeys);
 
@@ -436,53 +439,102 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
   const int64_t sk = p.ldk * 2, sv = p.ldv * 2;
   const char* kb = (const char*)p.k + (int64_t)b * p.k_len * sk + kh * p.D * 2;
   const char* vb = (const char*)p.v + (int64_t)b * p.k_len * sv + kh * p.D * 2;
-  uint32_t ko[NI], vo[NI];
+  // The loads of a lane are STEP rows apart, over which the swizzle repeats (every second load where
+  // STEP is 8), so that one offset serves all of them from a moving base.
+  constexpr int STEP = NW * 64 / CPR, NO = STEP % 16 == 0 ? 1 : 2;
+  uint32_t ko[NO], vo[NO];
 #pragma unroll
-  for (int n = 0; n < NI; ++n) {
-    const int at = (n * NW + wave) * 64 + lane, r = at / CPR, s = at % CPR;
+  for (int n = 0; n < NO; ++n) {
+    const int at = wave * 64 + lane, r = n * STEP + at / CPR, s = at % CPR;
     const int ck = s ^ k_key<CPR>(r), cv = s ^ v_key<CPR>(r);
-    ko[n] = ck * 8 < p.D ? (uint32_t)(r * (int)sk + ck * 16) : kOOB;
-    vo[n] = cv * 8 < p.D ? (uint32_t)(r * (int)sv + cv * 16) : kOOB;
+    ko[n] = ck * 8 < p.D ? (uint32_t)(at / CPR * (int)sk + ck * 16) : kOOB;
+    vo[n] = cv * 8 < p.D ? (uint32_t)(at / CPR * (int)sv + cv * 16) : kOOB;
   }
-  auto fill = [&](int buf, int t) {
+  // rows past the length (and tiles past the end) read as zeros, whatever stands there
+  auto fill = [&](int t, const char* base, int64_t stride, const uint32_t* off, char* dst) {
     const int k0 = t * kTileKeys;
-    const int n = min(kTileKeys, len - k0);  // rows past the length read as zeros, whatever they hold
-    const i32x4 kr = buffer_rsrc(kb + (int64_t)k0 * sk, (n - 1) * (int)sk + p.D * 2);
-    const i32x4 vr = buffer_rsrc(vb + (int64_t)k0 * sv, (n - 1) * (int)sv + p.D * 2);
-    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(lds + buf * 2 * TILE)) + wave * 1024;
+    const int valid = t < t_end ? min(kTileKeys, len - k0) : 0;
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(dst)) + wave * 1024;
 #pragma unroll
-    for (int n = 0; n < NI; ++n) lds_fill16(kr, at + n * NW * 1024, ko[n]);
-#pragma unroll
-    for (int n = 0; n < NI; ++n) lds_fill16(vr, at + TILE + n * NW * 1024, vo[n]);
+    for (int n = 0; n < NI; ++n) {
+      const int left = valid - n * STEP;
+      const i32x4 r4 = buffer_rsrc(base + (int64_t)(k0 + n * STEP) * stride, left > 0 ? (left - 1) * (int)stride + p.D * 2 : 0);
+      lds_fill16(r4, at + n * NW * 1024, off[n % NO]);
+    }
   };
+  char* const kt = lds;             // two tiles of keys
+  char* const vt = lds + 2 * TILE;  // and of values
+  auto fill_k = [&](int t) { fill(t, kb, sk, ko, kt + ((t - t0) & 1) * TILE); };
+  auto fill_v = [&](int t) { fill(t, vb, sv, vo, vt + ((t - t0) & 1) * TILE); };
 
   f32x16 o[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) o[d] = f32x16{};
   float m = -INFINITY, l = 0.0f;
   const float c2 = p.scale * 1.44269504088896340736f;
+  const int t_wave = min(t_end, (lim_hi + kTileKeys - 1) / kTileKeys);  // tiles that this wave's rows see
 
-  if (t0 < t_end) fill(0, t0);
-  for (int t = t0; t < t_end; ++t) {
-    const int buf = (t - t0) & 1;
-    // this tile has landed for every wave, and every wave is done with the one before
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (t + 1 < t_end) fill(buf ^ 1, t + 1);
+  // LDS offsets of this lane's operands in a tile: its key row at chunk h, whose other chunks are an XOR
+  // away (chunk 2 st + h at st << 5); and its part of V^T for 32-column block d, key group j
+  const uint32_t ka = col * RB + ((h ^ k_key<CPR>(col)) << 4);
+  uint32_t va[DB][2];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int r = 8 * j + 4 * h + ((lane & 15) >> 2);
+      const int c = d * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      va[d][j] = r * RB + ((c ^ v_key<CPR>(r)) << 4) + (lane & 1) * 8;
+    }
+  struct KFrag {
+    uint4 a[KB];
+  };
+  struct VFrag {
+    uint2 a[DB][2];
+  };
+  auto read_k = [&](auto par_tag, auto st_tag) {
+    constexpr int par = decltype(par_tag)::value, st = decltype(st_tag)::value;
+    KFrag f;
+#pragma unroll
+    for (int n = 0; n < KB; ++n) f.a[n] = *(const uint4*)(kt + (ka ^ (st << 5)) + par * TILE + n * 32 * RB);
+    return f;
+  };
+  auto read_v = [&](auto par_tag, auto ks_tag) {
+    constexpr int par = decltype(par_tag)::value, ks = decltype(ks_tag)::value;
+    VFrag f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        f.a[d][j] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                  (lds_s16x4)(vt + va[d][j] + par * TILE + ks * 16 * RB)));
+    return f;
+  };
+  auto mul_k = [&](const KFrag& f, auto st_tag, f32x16* s) {
+    constexpr int st = decltype(st_tag)::value;
+#pragma unroll
+    for (int n = 0; n < KB; ++n)
+      s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(f.a[n]), as_bf16x8(qf[st]), s[n], 0, 0, 0);
+  };
+  auto mul_v = [&](const VFrag& f, uint4 w) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+      o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          as_bf16x8(make_uint4(f.a[d][0].x, f.a[d][0].y, f.a[d][1].x, f.a[d][1].y)), as_bf16x8(w), o[d], 0, 0, 0);
+  };
+
+  // Tile t, in the LDS places of its parity: its scores s are there.  While the matrix cores form the next
+  // tile's, the vector ALU turns these into weights, a slice per step; operands are read two steps ahead.
+  // Then the values are weighted.  (Past the last tile the next scores are of whatever the place holds, and
+  // not used.)
+  auto step = [&](int t, auto par_tag, f32x16* s, f32x16* next) {
+    constexpr std::integral_constant<int, 1 - decltype(par_tag)::value> other{};
+    constexpr std::integral_constant<int, 0> c0{};
+    constexpr std::integral_constant<int, 1> c1{};
+    KFrag kf[3];
+    kf[0] = read_k(other, c0);
+    kf[1] = read_k(other, c1);
     const int k0 = t * kTileKeys;
-    if (k0 >= lim_hi) continue;  // nothing here for this wave's rows
-    const char* kt = lds + buf * 2 * TILE;
-    const char* vt = kt + TILE;
-    f32x16 s[KB];
-#pragma unroll
-    for (int n = 0; n < KB; ++n) s[n] = f32x16{};
-#pragma unroll
-    for (int st = 0; st < QS; ++st)
-#pragma unroll
-      for (int n = 0; n < KB; ++n) {
-        const int r = n * 32 + col;
-        const uint4 a = *(const uint4*)(kt + r * RB + (((2 * st + h) ^ k_key<CPR>(r)) * 16));
-        s[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(qf[st]), s[n], 0, 0, 0);
-      }
     if (k0 + kTileKeys > lim_lo) {
 #pragma unroll
       for (int n = 0; n < KB; ++n)
@@ -490,12 +542,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
         for (int e = 0; e < 16; ++e)
           if (k0 + n * 32 + 8 * (e >> 2) + 4 * h + (e & 3) >= lim) s[n][e] = -INFINITY;
     }
-    float top = -INFINITY;
+    float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
     for (int n = 0; n < KB; ++n)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[n][e]);
-    top = half_max(top) * c2;
+      for (int e = 0; e < 16; ++e) tops[e & 3] = fmaxf(tops[e & 3], s[n][e]);
+    const float top = half_max(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))) * c2;
     if (__any(top > m + kSlack)) {  // (m = -inf before the first seen key)
       const float mn = fmaxf(m, top);
       const float keep = exp2_(m - (mn == -INFINITY ? 0.0f : mn));
@@ -505,26 +557,64 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
       for (int d = 0; d < DB; ++d) o[d] *= keep;
     }
     const float use = m == -INFINITY ? 0.0f : m;
-    float sum = 0.0f;
 #pragma unroll
-    for (int n = 0; n < KB; ++n)
+    for (int n = 0; n < KB; ++n) next[n] = f32x16{};
+    float sums[2] = {0.0f, 0.0f};
+    uint4 pf[2 * KB];
+    VFrag vf[2];
+    constexpr int SL = 16 * KB / QS;  // weights of a slice
+    static_for<0, QS>([&](auto st) {
+      constexpr int i = decltype(st)::value;
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (i + 2 < QS) kf[(i + 2) % 3] = read_k(other, std::integral_constant<int, i + 2>{});
+      if constexpr (i == QS - 1) vf[0] = read_v(par_tag, c0);
+      mul_k(kf[i % 3], st, next);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[n][e] = exp2_(__builtin_fmaf(s[n][e], c2, -use));
-        sum += s[n][e];
+      for (int e = i * SL; e < (i + 1) * SL; ++e) {
+        const float w = exp2_(__builtin_fmaf(s[e >> 4][e & 15], c2, -use));
+        s[e >> 4][e & 15] = w;
+        sums[e & 1] += w;
       }
-    l += sum;
+      if constexpr ((i + 1) * SL % 8 == 0) {
 #pragma unroll
-    for (int n = 0; n < KB; ++n)
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const uint4 pf = pack_weights(s[n], ks);
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(load_vt<CPR>(vt, n * 32 + ks * 16, d, lane)),
-                                                         as_bf16x8(pf), o[d], 0, 0, 0);
+        for (int ks = i * SL / 8; ks < (i + 1) * SL / 8; ++ks) pf[ks] = pack_weights(s[ks >> 1], ks & 1);
       }
+    });
+    l += sums[0] + sums[1];
+    static_for<0, 2 * KB>([&](auto ks) {
+      constexpr int i = decltype(ks)::value;
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (i + 1 < 2 * KB) vf[(i + 1) & 1] = read_v(par_tag, std::integral_constant<int, i + 1>{});
+      mul_v(vf[i & 1], pf[i]);
+    });
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // Tiles t of values and t + 1 of keys have landed for every wave, and every wave is done with those
+  // before, whose places the next take.
+  auto turn = [&](int t) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    fill_k(t + 2);
+    fill_v(t + 1);
+  };
+  constexpr std::integral_constant<int, 0> even{};
+  constexpr std::integral_constant<int, 1> odd{};
+  f32x16 sa[KB], sb[KB];
+  fill_k(t0);
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  fill_k(t0 + 1);
+  fill_v(t0);
+#pragma unroll
+  for (int n = 0; n < KB; ++n) sa[n] = f32x16{};
+  static_for<0, QS>([&](auto st) { mul_k(read_k(even, st), st, sa); });
+  for (int t = t0; t < t_end; t += 2) {
+    turn(t);
+    if (t < t_wave) step(t, even, sa, sb);
+    if (t + 1 >= t_end) break;
+    turn(t + 1);
+    if (t + 1 < t_wave) step(t + 1, odd, sb, sa);
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if (row >= R) return;
   l = half_sum(l);
   if (joined) {
