@@ -439,33 +439,32 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
   const int64_t sk = p.ldk * 2, sv = p.ldv * 2;
   const char* kb = (const char*)p.k + (int64_t)b * p.k_len * sk + kh * p.D * 2;
   const char* vb = (const char*)p.v + (int64_t)b * p.k_len * sv + kh * p.D * 2;
-  // The loads of a lane are STEP rows apart, over which the swizzle repeats (every second load where
-  // STEP is 8), so that one offset serves all of them from a moving base.
-  constexpr int STEP = NW * 64 / CPR, NO = STEP % 16 == 0 ? 1 : 2;
-  uint32_t ko[NO], vo[NO];
+  uint32_t ko[NI], vo[NI];
 #pragma unroll
-  for (int n = 0; n < NO; ++n) {
-    const int at = wave * 64 + lane, r = n * STEP + at / CPR, s = at % CPR;
-    const int ck = s ^ k_key<CPR>(r), cv = s ^ v_key<CPR>(r);
-    ko[n] = ck * 8 < p.D ? (uint32_t)(at / CPR * (int)sk + ck * 16) : kOOB;
-    vo[n] = cv * 8 < p.D ? (uint32_t)(at / CPR * (int)sv + cv * 16) : kOOB;
+  for (int n = 0; n < NI; ++n) {
+    const int at = (n * NW + wave) * 64 + lane, r = at / CPR, x = at % CPR;
+    const int ck = x ^ k_key<CPR>(r), cv = x ^ v_key<CPR>(r);
+    ko[n] = ck * 8 < p.D ? (uint32_t)(r * (int)sk + ck * 16) : kOOB;
+    vo[n] = cv * 8 < p.D ? (uint32_t)(r * (int)sv + cv * 16) : kOOB;
   }
-  // rows past the length (and tiles past the end) read as zeros, whatever stands there
-  auto fill = [&](int t, const char* base, int64_t stride, const uint32_t* off, char* dst) {
-    const int k0 = t * kTileKeys;
-    const int valid = t < t_end ? min(kTileKeys, len - k0) : 0;
-    const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(dst)) + wave * 1024;
-#pragma unroll
-    for (int n = 0; n < NI; ++n) {
-      const int left = valid - n * STEP;
-      const i32x4 r4 = buffer_rsrc(base + (int64_t)(k0 + n * STEP) * stride, left > 0 ? (left - 1) * (int)stride + p.D * 2 : 0);
-      lds_fill16(r4, at + n * NW * 1024, off[n % NO]);
-    }
-  };
+  // Fills of successive tiles, the base moving along (few scalar instructions: they are not hidden); rows past
+  // the length (and tiles past the end) read as zeros, whatever stands there
   char* const kt = lds;             // two tiles of keys
   char* const vt = lds + 2 * TILE;  // and of values
-  auto fill_k = [&](int t) { fill(t, kb, sk, ko, kt + ((t - t0) & 1) * TILE); };
-  auto fill_v = [&](int t) { fill(t, vb, sv, vo, vt + ((t - t0) & 1) * TILE); };
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds)) + wave * 1024;
+  auto fill = [&](const char*& base, int64_t stride, int& left, const uint32_t* off, uint32_t at) {
+    const int valid = min(kTileKeys, left);
+    const i32x4 r4 = buffer_rsrc(base, valid > 0 ? (valid - 1) * (int)stride + p.D * 2 : 0);
+#pragma unroll
+    for (int n = 0; n < NI; ++n) lds_fill16(r4, at + n * NW * 1024, off[n]);
+    base += kTileKeys * stride;
+    left -= kTileKeys;
+  };
+  const char *kp = kb + (int64_t)t0 * kTileKeys * sk, *vp = vb + (int64_t)t0 * kTileKeys * sv;
+  const int rest = t_end > t0 ? min(len, t_end * kTileKeys) - t0 * kTileKeys : 0;  // keys from t0 on
+  int k_left = rest, v_left = rest;
+  auto fill_k = [&](auto par_tag) { fill(kp, sk, k_left, ko, lds0 + decltype(par_tag)::value * TILE); };
+  auto fill_v = [&](auto par_tag) { fill(vp, sv, v_left, vo, lds0 + (2 + decltype(par_tag)::value) * TILE); };
 
   f32x16 o[DB];
 #pragma unroll
@@ -590,28 +589,28 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  // Tiles t of values and t + 1 of keys have landed for every wave, and every wave is done with those
-  // before, whose places the next take.
-  auto turn = [&](int t) {
+  // Before step t: its values and the keys of t + 1 have landed for every wave, and every wave is done with
+  // the tiles before, whose places keys t + 2 (that of t) and values t + 1 take.
+  auto turn = [&](auto same, auto other) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    fill_k(t + 2);
-    fill_v(t + 1);
+    fill_k(same);
+    fill_v(other);
   };
   constexpr std::integral_constant<int, 0> even{};
   constexpr std::integral_constant<int, 1> odd{};
   f32x16 sa[KB], sb[KB];
-  fill_k(t0);
+  fill_k(even);
   asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-  fill_k(t0 + 1);
-  fill_v(t0);
+  fill_k(odd);
+  fill_v(even);
 #pragma unroll
   for (int n = 0; n < KB; ++n) sa[n] = f32x16{};
   static_for<0, QS>([&](auto st) { mul_k(read_k(even, st), st, sa); });
   for (int t = t0; t < t_end; t += 2) {
-    turn(t);
+    turn(even, odd);
     if (t < t_wave) step(t, even, sa, sb);
     if (t + 1 >= t_end) break;
-    turn(t + 1);
+    turn(odd, even);
     if (t + 1 < t_wave) step(t + 1, odd, sb, sa);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
