@@ -3325,12 +3325,18 @@ Status engine_run(Engine* e, const void* const* inputs, int32_t n_in, void* cons
   if (stream != nullptr) HIP_TRY(hipStreamIsCapturing(stream, &cs), "hipStreamIsCapturing");
   if ((e->options & BYOC_OPT_GRAPH_REPLAY) && !prof && stream != nullptr && cs == hipStreamCaptureStatusNone) {
     Status st = run_graph(e, c, n_in, n_out);
-    if (st.ok()) HIP_TRY(hipEventRecord(e->done, stream), "hipEventRecord");
+    if (st.ok()) {
+      e->done_on_null = false;
+      HIP_TRY(hipEventRecord(e->done, stream), "hipEventRecord");
+    }
     return st;
   }
   Status st = launch_all(e, c, prof);
   // completion marker for destroy (not inside a capture of the caller's)
-  if (st.ok() && cs == hipStreamCaptureStatusNone) HIP_TRY(hipEventRecord(e->done, stream), "hipEventRecord");
+  if (st.ok() && cs == hipStreamCaptureStatusNone) {
+    e->done_on_null = stream == nullptr;
+    if (stream != nullptr) HIP_TRY(hipEventRecord(e->done, stream), "hipEventRecord");
+  }
   return st;
 }
 
@@ -3421,7 +3427,8 @@ Status engine_destroy(Engine* e) {
     DeviceGuard guard(e->device);
     // the last run enqueued through run() (the event completes at once when
     // there was none); runs of run_static are the caller's to synchronise
-    hipError_t err = e->done ? hipEventSynchronize(e->done) : hipSuccess;
+    hipError_t err = e->done && e->done_on_null ? hipEventRecord(e->done, nullptr) : hipSuccess;
+    if (err == hipSuccess && e->done) err = hipEventSynchronize(e->done);
     if (err != hipSuccess) st = Status::Err(BYOC_ERR_DEVICE, std::string("destroy: ") + hipGetErrorString(err));
     release(e);
   }

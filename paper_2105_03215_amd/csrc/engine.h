@@ -98,8 +98,11 @@ struct Engine {
   int prof_max_runs = 0;
   int prof_runs = 0;
   hipStream_t prof_last_stream = nullptr;
-  // marks the end of the last run() on its stream; destroy waits for it
+  // marks the end of the last run() on its stream; destroy waits for it.  After a run on
+  // the null stream, which outlives every engine, it is recorded by destroy instead
+  // (done_on_null): an event a run costs the GPU 2 us between small kernels.
   hipEvent_t done = nullptr;
+  bool done_on_null = false;
   // two-stream execution: launch i runs on the caller's stream (lstream 0)
   // or on the engine's side stream (1) and first waits for the event of
   // launch lwait[i] (>= 0) on the other stream; lrecord[i]: an event is
