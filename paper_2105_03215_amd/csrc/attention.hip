@@ -391,18 +391,18 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
 constexpr int kTileKeys = 64;
 constexpr float kSlack = 8.0f;
 
-template <int DP>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel(AttnParams p) {
-  constexpr int NW = 4;
+template <int DP, int KS>
+__global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_kernel(AttnParams p) {
+  constexpr int NW = 4 / KS;  // waves along the rows
   constexpr int RB = DP * 2, CPR = RB / 16;
   constexpr int TILE = kTileKeys * RB;
   constexpr int NI = TILE / (NW * 1024);  // loads of a tile per lane
   constexpr int DB = DP / 32, QS = CPR / 2, KB = kTileKeys / 32;
-  __shared__ __align__(1024) char lds[4 * TILE];
+  __shared__ __align__(1024) char lds[KS * 4 * TILE];
   static_assert(sizeof(lds) <= kLdsLimit, "LDS");
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
-  const int wave = uniform(tid >> 6);
+  const int wave = uniform((tid >> 6) % NW), kg = uniform((tid >> 6) / NW);  // place among the rows; key group
   const int R = p.q_len * p.group;
   const int nh = p.chunks * p.kv_heads;
   const int nt = (R + 32 * NW - 1) / (32 * NW);
@@ -449,19 +449,20 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
   }
   // Fills of successive tiles, the base moving along (few scalar instructions: they are not hidden); rows past
   // the length (and tiles past the end) read as zeros, whatever stands there
-  char* const kt = lds;             // two tiles of keys
-  char* const vt = lds + 2 * TILE;  // and of values
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(lds)) + wave * 1024;
+  char* const kt = lds + kg * 4 * TILE;  // two tiles of keys
+  char* const vt = kt + 2 * TILE;        // and of values
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(kt)) + wave * 1024;
   auto fill = [&](const char*& base, int64_t stride, int& left, const uint32_t* off, uint32_t at) {
     const int valid = min(kTileKeys, left);
     const i32x4 r4 = buffer_rsrc(base, valid > 0 ? (valid - 1) * (int)stride + p.D * 2 : 0);
 #pragma unroll
     for (int n = 0; n < NI; ++n) lds_fill16(r4, at + n * NW * 1024, off[n]);
-    base += kTileKeys * stride;
-    left -= kTileKeys;
+    base += KS * kTileKeys * stride;
+    left -= KS * kTileKeys;
   };
-  const char *kp = kb + (int64_t)t0 * kTileKeys * sk, *vp = vb + (int64_t)t0 * kTileKeys * sv;
-  const int rest = t_end > t0 ? min(len, t_end * kTileKeys) - t0 * kTileKeys : 0;  // keys from t0 on
+  const int first = t0 + kg;  // this group's tiles: first, first + KS, ...
+  const char *kp = kb + (int64_t)first * kTileKeys * sk, *vp = vb + (int64_t)first * kTileKeys * sv;
+  const int rest = t_end > first ? min(len, t_end * kTileKeys) - first * kTileKeys : 0;  // keys from there on
   int k_left = rest, v_left = rest;
   auto fill_k = [&](auto par_tag) { fill(kp, sk, k_left, ko, lds0 + decltype(par_tag)::value * TILE); };
   auto fill_v = [&](auto par_tag) { fill(vp, sv, v_left, vo, lds0 + (2 + decltype(par_tag)::value) * TILE); };
@@ -606,16 +607,41 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_kernel
 #pragma unroll
   for (int n = 0; n < KB; ++n) sa[n] = f32x16{};
   static_for<0, QS>([&](auto st) { mul_k(read_k(even, st), st, sa); });
-  for (int t = t0; t < t_end; t += 2) {
+  for (int t = t0; t < t_end; t += 2 * KS) {
     turn(even, odd);
-    if (t < t_wave) step(t, even, sa, sb);
-    if (t + 1 >= t_end) break;
+    if (t + kg < t_wave) step(t + kg, even, sa, sb);
+    if (t + KS >= t_end) break;
     turn(odd, even);
-    if (t + 1 < t_wave) step(t + 1, odd, sb, sa);
+    if (t + KS + kg < t_wave) step(t + KS + kg, odd, sb, sa);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  if (row >= R) return;
   l = half_sum(l);
+  if constexpr (KS > 1) {
+    // the second key group hands its results over, lane by lane, in the place of the tiles
+    static_assert(KS == 2 && NW * 64 * (16 * DB + 2) * 4 <= (int)sizeof(lds), "the results' place");
+    float* const ex = (float*)lds + wave * 64 * (16 * DB + 2) + lane;
+    __syncthreads();
+    if (kg == 1) {
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) ex[(d * 16 + e) * 64] = o[d][e];
+      ex[16 * DB * 64] = m;
+      ex[(16 * DB + 1) * 64] = l;
+    }
+    __syncthreads();
+    if (kg == 1) return;
+    const float m1 = ex[16 * DB * 64], l1 = ex[(16 * DB + 1) * 64];
+    const float top = fmaxf(m, m1), use = top == -INFINITY ? 0.0f : top;
+    const float f0 = exp2_(m - use), f1 = exp2_(m1 - use);
+    m = top;
+    l = l * f0 + l1 * f1;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[d][e] = o[d][e] * f0 + ex[(d * 16 + e) * 64] * f1;
+  }
+  if (row >= R) return;
   if (joined) {
     float* const sums = part_sums(p, kh, row, chunk);
 #pragma unroll
@@ -722,7 +748,11 @@ int row_blocks(const AttnParams& p) {
 // of their four waves would idle; fp32 products are bound by the matrix cores either way).
 void choose_attention(AttnParams& p) {
   const bool tiled = !p.f32 && p.q_len * (int64_t)p.group > 32;
-  p.tile_rows = tiled ? 128 : kCols;
+  // Up to 64 columns a head, two waves along the rows and two along the keys where 128-row workgroups would
+  // not fill the chip twice: causal 1 x 2048, 16 heads of 64: 30.5 us as 256 workgroups of 128 rows, 21.4 as
+  // 512 of 64; 128 columns need the LDS of a CU for that and lose (1 x 1024, 32 over 8 of 128: 25.1, 29.1).
+  const bool halves = tiled && p.D <= 64 && (int64_t)p.batch * p.kv_heads * ceil_div((int64_t)p.q_len * p.group, 128) <= 320;
+  p.tile_rows = tiled ? (halves ? 64 : 128) : kCols;
   p.tile_keys = tiled ? kTileKeys : kKeys;
   const int64_t blocks = (int64_t)p.batch * p.kv_heads * row_blocks(p);
   // Tiles: a split fills the two workgroups that a CU has room for where there is less than one.
@@ -749,9 +779,13 @@ hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
   if (p.D < 8 || p.D > 256 || p.D % 8 != 0 || p.chunks < p.batch) return hipErrorInvalidValue;
   const int grid = p.chunks * p.kv_heads * row_blocks(p);
   if (p.tile_rows > kCols) {
-    if (p.D <= 64) attention_tiles_kernel<64><<<grid, 256, 0, s>>>(p);
-    else if (p.D <= 128) attention_tiles_kernel<128><<<grid, 256, 0, s>>>(p);
-    else attention_tiles_kernel<256><<<grid, 256, 0, s>>>(p);
+    if (p.tile_rows == 64) {
+      attention_tiles_kernel<64, 2><<<grid, 256, 0, s>>>(p);
+    } else {
+      if (p.D <= 64) attention_tiles_kernel<64, 1><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 128) attention_tiles_kernel<128, 1><<<grid, 256, 0, s>>>(p);
+      else attention_tiles_kernel<256, 1><<<grid, 256, 0, s>>>(p);
+    }
     return hipGetLastError();
   }
   if (p.f32) {
