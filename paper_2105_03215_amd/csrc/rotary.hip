@@ -8,8 +8,11 @@
 // integer part), exact enough for every 32-bit position, before the float32 sine
 // and cosine; in float32 a position of 10^5 would lose 2^-8 of a radian.
 //
-// HBM bound: every row is read and written once.  A row's angles are formed once by
-// its workgroup, into LDS, for all of its heads.
+// HBM bound: every row is read and written once.  What a row's columns are multiplied
+// with is formed once by its workgroup, into LDS, for all of its heads.  8192 rows of 40
+// normed heads of 128, bf16 (168 MB): 38 us, 4.4 TB/s, where a copy of as many bytes
+// runs at 4.8; 52 us with the norm weights in registers, the partner's columns loaded
+// again and one head of a lane at a time.
 #include <algorithm>
 
 #include "device_common.h"
@@ -56,73 +59,158 @@ __device__ __forceinline__ void angles(const RotaryParams& p, int row0, int rows
   __syncthreads();
 }
 
+// 8 columns as they are stored.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<bf16_t> {
+  uint4 u;
+  __device__ __forceinline__ void load(const bf16_t* p) { u = *(const uint4*)p; }
+  __device__ __forceinline__ void get(float* f) const { unpack8(u, f); }
+  __device__ __forceinline__ Raw across(int d) const {
+    Raw r;
+    r.u = make_uint4(__shfl_xor((int)u.x, d, 64), __shfl_xor((int)u.y, d, 64), __shfl_xor((int)u.z, d, 64),
+                     __shfl_xor((int)u.w, d, 64));
+    return r;
+  }
+};
+template <>
+struct Raw<float> {
+  float v[8];
+  __device__ __forceinline__ void load(const float* p) { load8(p, v); }
+  __device__ __forceinline__ void get(float* f) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = v[e];
+  }
+  __device__ __forceinline__ Raw across(int d) const {
+    Raw r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.v[e] = __shfl_xor(v[e], d, 64);
+    return r;
+  }
+};
+
+// What each column of `rows` rows is multiplied with: y = (x A + partner B) / rms, with
+// A = weight cos, B = -+ partner's weight sin (times mag; past the turning columns weight
+// and 0), so that the norm weights cost a lane nothing.  With NORM a table each for the
+// query and the key heads.  Column 8 c + e of D / 8 chunks stands at ((e / 2) chunks + c)
+// float4 + e % 2 float2: lanes of consecutive chunks read consecutive 16 bytes.
+template <bool NORM, bool INTER>
+__device__ __forceinline__ void coefficients(const RotaryParams& p, int row0, int rows, float2* cs) {
+  const int half = p.rd / 2, chunks = p.D / 8;
+  const int tables = NORM && p.kv_heads > 0 ? 2 : 1;
+  auto put = [&](int r, int t, int col, float a, float b) {
+    cs[(r * tables + t) * p.D + (((col & 7) >> 1) * chunks + (col >> 3)) * 2 + (col & 1)] = make_float2(a, b);
+  };
+  for (int i = threadIdx.x; i < rows * half; i += kThreads) {
+    const int r = i / half, k = i - r * half;
+    const double turns = (double)p.pos[row0 + r] * p.theta[k];
+    float s, c;
+    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+    s *= p.mag, c *= p.mag;
+    const int e1 = INTER ? 2 * k : k, e2 = INTER ? 2 * k + 1 : k + half;
+    for (int t = 0; t < tables; ++t) {
+      const float* w = t ? p.wk : p.wq;
+      const float w1 = NORM ? w[e1] : 1.0f, w2 = NORM ? w[e2] : 1.0f;
+      put(r, t, e1, w1 * c, -w2 * s);
+      put(r, t, e2, w2 * c, w1 * s);
+    }
+  }
+  if constexpr (!NORM) {  // (the other columns are copied)
+    __syncthreads();
+    return;
+  }
+  const int rest = p.D - p.rd;
+  for (int i = threadIdx.x; i < rows * rest; i += kThreads) {
+    const int r = i / rest, col = p.rd + i - r * rest;
+    for (int t = 0; t < tables; ++t) put(r, t, col, (t ? p.wk : p.wq)[col], 0.0f);
+  }
+  __syncthreads();
+}
+
 // LH lanes per head, 8 consecutive columns each (D <= 8 LH); RB rows per workgroup,
-// hb heads per workgroup.
-template <typename T, int LH, bool NORM, bool INTER>
+// hb heads per workgroup; U heads of a lane on their way together.  In the half
+// layout a lane needs its partner's columns too: from the lane that has them where
+// the whole head turns and fills its lanes (ACROSS), else read again.
+template <typename T, int LH, bool NORM, bool INTER, bool ACROSS, int U>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int RB, int hb) {
-  extern __shared__ float2 cs[];
+  extern __shared__ __align__(16) float2 cs[];
   constexpr int SLOTS = kThreads / LH;
   const int row0 = blockIdx.x * RB;
   const int rows = min(RB, p.M - row0);
-  angles(p, row0, rows, cs);
   const int H = p.heads + p.kv_heads;
   const int h0 = blockIdx.y * hb, nh = min(hb, H - h0);
   const int slot = threadIdx.x / LH, c = threadIdx.x % LH;
-  const int half = p.rd / 2;
+  const int half = p.rd / 2, chunks = p.D / 8;
+  const int tables = NORM && p.kv_heads > 0 ? 2 : 1;
   const int e0 = c * 8;
   const bool live = e0 < p.D;
-  // columns of this lane that turn, and in the half layout its partner's
-  const bool turn = live && e0 < p.rd;
-  const bool second = !INTER && e0 >= half;
-  const int pe = second ? e0 - half : e0 + half;  // the partner's first column
-  const int pair = INTER ? e0 / 2 : (second ? e0 - half : e0);
-  float w[2][8], pw[2][8];
-  if constexpr (NORM) {
+  const bool turn = live && e0 < p.rd;                 // (whole chunks turn or stay)
+  const int pe = e0 >= half ? e0 - half : e0 + half;  // half layout: the partner's first column
+  const T* const x0 = (const T*)p.x + (int64_t)row0 * p.ldx + (int64_t)h0 * p.D;
+  T* const y0 = (T*)p.y + (int64_t)row0 * p.ldy + (int64_t)h0 * p.D;
+  // item it: row it / nh, head it % nh of this workgroup; a lane's first and its next
+  const int items = rows * nh;
+  int r = slot / nh, h = slot - r * nh;
+  const int dr = SLOTS / nh, dh = SLOTS - dr * nh;
+  Raw<T> v[U], o[U];
+  int rr[U], hh[U];
+  auto fetch = [&](int it) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const float* g = k == 0 ? p.wq : (p.wk ? p.wk : p.wq);
-      if (live) load8(g + e0, w[k]);
-      if (!INTER && turn) load8(g + pe, pw[k]);
-    }
-  }
-  for (int it = slot; it < rows * nh; it += SLOTS) {
-    const int r = it / nh, h = h0 + it - r * nh;
-    const T* x = (const T*)p.x + (int64_t)(row0 + r) * p.ldx + (int64_t)h * p.D;
-    T* y = (T*)p.y + (int64_t)(row0 + r) * p.ldy + (int64_t)h * p.D;
-    float v[8], o[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = o[e] = 0.0f;
-    if (live) load8(x + e0, v);
-    if (!INTER && turn) load8(x + pe, o);
-    if constexpr (NORM) {
-      float sum = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(v[e], v[e], sum);
-#pragma unroll
-      for (int d = LH / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-      const float inv = 1.0f / sqrtf(sum / (float)p.D + p.eps);
-      const bool key = h >= p.heads;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[e] *= inv * (key ? w[1][e] : w[0][e]);
-        if (!INTER) o[e] *= inv * (key ? pw[1][e] : pw[0][e]);
+    for (int u = 0; u < U; ++u) {
+      rr[u] = r, hh[u] = h;
+      if (it + u * SLOTS < items) {
+        const T* x = x0 + (int64_t)r * p.ldx + h * p.D;
+        if (live) v[u].load(x + e0);
+        if (!INTER && !ACROSS && turn) o[u].load(x + pe);
       }
+      r += dr, h += dh;
+      if (h >= nh) h -= nh, ++r;
     }
-    if (turn) {
-      const float2* t = cs + r * half + pair;
-      if constexpr (INTER) {
+  };
+  fetch(slot);  // (the first heads are on their way while the coefficients are formed)
+  coefficients<NORM, INTER>(p, row0, rows, cs);
+  for (int it = slot; it < items; it += U * SLOTS) {
+    float f[U][8], q[U][8];
+    int fr[U], fh[U];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float a = v[2 * e], b = v[2 * e + 1];
-          v[2 * e] = a * t[e].x - b * t[e].y;
-          v[2 * e + 1] = b * t[e].x + a * t[e].y;
-        }
-      } else {
+    for (int u = 0; u < U; ++u) {
+      v[u].get(f[u]);
+      if constexpr (!INTER) (ACROSS ? v[u].across(LH / 2) : o[u]).get(q[u]);
+      fr[u] = rr[u], fh[u] = hh[u];
+    }
+    fetch(it + U * SLOTS);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = v[e] * t[e].x + (second ? o[e] : -o[e]) * t[e].y;
+    for (int u = 0; u < U; ++u) {
+      float inv = 1.0f;
+      if constexpr (NORM) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(f[u][e], f[u][e], sum);
+        sum = live ? sum : 0.0f;
+#pragma unroll
+        for (int d = LH / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+        inv = 1.0f / sqrtf(sum / (float)p.D + p.eps);
       }
+      if (it + u * SLOTS >= items || !live) continue;
+      T* const out = y0 + (int64_t)fr[u] * p.ldy + fh[u] * p.D + e0;
+      if (!NORM && !turn) {
+        store8(out, f[u]);
+        continue;
+      }
+      const int t = tables == 2 && h0 + fh[u] >= p.heads ? 1 : 0;
+      const float4* k = (const float4*)(cs + (fr[u] * tables + t) * p.D) + c;
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float4 ab = k[(e >> 1) * chunks];
+        const float q0 = INTER ? f[u][e + 1] : q[u][e], q1 = INTER ? f[u][e] : q[u][e + 1];
+        y[e] = turn ? __builtin_fmaf(q0, ab.y, f[u][e] * ab.x) : f[u][e] * ab.x;
+        y[e + 1] = turn ? __builtin_fmaf(q1, ab.w, f[u][e + 1] * ab.z) : f[u][e + 1] * ab.z;
+        if constexpr (NORM) y[e] *= inv, y[e + 1] *= inv;
+      }
+      store8(out, y);
     }
-    if (live) store8(y + e0, v);
   }
 }
 
@@ -179,9 +267,9 @@ template <typename T>
 hipError_t launch(const RotaryParams& p, hipStream_t s) {
   const int H = p.heads + p.kv_heads;
   const int half = p.rd / 2;
-  // Rows per workgroup: four share the angles' latency once there are enough of them for the chip;
-  // few rows are spread over the heads instead.
-  const int RB = p.M >= 2048 ? 4 : 1;
+  // Rows per workgroup: up to four share the latency of forming their coefficients while that leaves 1024
+  // workgroups (8192 rows: 41 us alone, 38 by four, 40 by eight); few rows are spread over the heads instead.
+  const int RB = std::min(4, std::max(1, p.M / 1024));
   int lh = 1;
   while (lh * 8 < p.D) lh *= 2;
   const bool fast = p.D % 8 == 0 && lh <= 64 && (p.interleaved ? p.rd : half) % 8 == 0 &&
@@ -189,19 +277,23 @@ hipError_t launch(const RotaryParams& p, hipStream_t s) {
   const int slots = fast ? kThreads / lh : kThreads / 64;
   const int hb = p.M >= 1024 ? H : std::min(H, slots);
   const dim3 grid((p.M + RB - 1) / RB, (H + hb - 1) / hb);
-  const size_t lds = (size_t)RB * half * sizeof(float2);
   if (!fast) {
+    const size_t lds = (size_t)RB * half * sizeof(float2);
     rotary_any_kernel<T><<<grid, kThreads, lds, s>>>(p, RB, hb);
     return hipGetLastError();
   }
-#define BYOC_ROTARY(LH)                                                                              \
-  case LH:                                                                                           \
-    if (p.wq)                                                                                        \
-      p.interleaved ? rotary_kernel<T, LH, true, true><<<grid, kThreads, lds, s>>>(p, RB, hb)        \
-                    : rotary_kernel<T, LH, true, false><<<grid, kThreads, lds, s>>>(p, RB, hb);      \
-    else                                                                                             \
-      p.interleaved ? rotary_kernel<T, LH, false, true><<<grid, kThreads, lds, s>>>(p, RB, hb)       \
-                    : rotary_kernel<T, LH, false, false><<<grid, kThreads, lds, s>>>(p, RB, hb);     \
+  const size_t lds = (size_t)RB * p.D * (p.wq && p.kv_heads > 0 ? 2 : 1) * sizeof(float2);
+  const bool across = !p.interleaved && p.rd == p.D && p.D == 8 * lh && lh > 1;
+#define BYOC_ROTARY_AS(LH, NORM, INTER, ACROSS) \
+  rotary_kernel<T, LH, NORM, INTER, ACROSS, ACROSS ? 2 : 1><<<grid, kThreads, lds, s>>>(p, RB, hb)
+#define BYOC_ROTARY(LH)                                                                      \
+  case LH:                                                                                   \
+    if (p.wq)                                                                                \
+      p.interleaved ? BYOC_ROTARY_AS(LH, true, true, false)                                  \
+                    : across ? BYOC_ROTARY_AS(LH, true, false, true) : BYOC_ROTARY_AS(LH, true, false, false);   \
+    else                                                                                     \
+      p.interleaved ? BYOC_ROTARY_AS(LH, false, true, false)                                 \
+                    : across ? BYOC_ROTARY_AS(LH, false, false, true) : BYOC_ROTARY_AS(LH, false, false, false); \
     break;
   switch (lh) {
     BYOC_ROTARY(1)
@@ -213,6 +305,7 @@ hipError_t launch(const RotaryParams& p, hipStream_t s) {
     BYOC_ROTARY(64)
   }
 #undef BYOC_ROTARY
+#undef BYOC_ROTARY_AS
   return hipGetLastError();
 }
 
