@@ -109,6 +109,17 @@ __device__ __forceinline__ int chunk_batch(const AttnParams& p, int q, Chunks* o
   *out = Chunks{__builtin_amdgcn_readlane(c.first, b), __builtin_amdgcn_readlane(c.count, b), uniform(c.size)};
   return b;
 }
+// The sequence with the n-th most keys (of at most 64; the lower number first among equals).
+__device__ __forceinline__ int nth_longest(const AttnParams& p, int n) {
+  const int lane = threadIdx.x & 63;
+  const int mine = lane < p.batch ? batch_len(p, lane) : -1;
+  int rank = 0;
+  for (int j = 0; j < p.batch; ++j) {
+    const int other = __builtin_amdgcn_readlane(mine, j);
+    rank += other > mine || (other == mine && j < lane);
+  }
+  return __builtin_ctzll(__ballot(lane < p.batch && rank == n));
+}
 // The workspace: for each sequence the first of its chunks and their number (written by that chunk's
 // workgroup, so that the join need not count them again; a sequence without keys has none), then the
 // sums, then the maxima and weights.
@@ -409,12 +420,22 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   // Head fastest: with a multiple of 8 heads each XCD (workgroup b runs on XCD b % 8) keeps to its own
   // heads' keys and values; the last rows first, which see the most keys under a causal mask.
   const int bh = blockIdx.x % nh;
-  const int tile = nt - 1 - blockIdx.x / nh;
-  const int chunk = bh / p.kv_heads, kh = bh - chunk * p.kv_heads;
+  int tile = nt - 1 - blockIdx.x / nh;
+  int chunk = bh / p.kv_heads, kh = bh - chunk * p.kv_heads;
   const bool joined = p.chunks > p.batch;
   Chunks ck;
-  const int b = uniform(chunk_batch(p, chunk, &ck));
-  if (b < 0) return;
+  int b;
+  if (p.lengths && !p.causal && !joined && p.batch <= 64) {
+    // sequences of different lengths: the longest first, all of its rows
+    const int per = p.kv_heads * nt, pos = blockIdx.x / per, rem = blockIdx.x - pos * per;
+    tile = rem / p.kv_heads;
+    kh = rem - tile * p.kv_heads;
+    b = chunk = uniform(nth_longest(p, pos));
+    ck = uniform_chunks(p, b);
+  } else {
+    b = uniform(chunk_batch(p, chunk, &ck));
+    if (b < 0) return;
+  }
   if (joined && tile == 0 && kh == 0) note_chunks(p, b, chunk, ck);
   const int len = uniform(batch_len(p, b));
   const int row0 = tile * 32 * NW + wave * 32, row = row0 + col;
