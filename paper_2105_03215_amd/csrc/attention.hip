@@ -171,6 +171,74 @@ __device__ __forceinline__ uint4 load_vt(const char* vt, int row0, int d, int la
   return make_uint4(vf[0].x, vf[0].y, vf[1].x, vf[1].y);
 }
 
+// Under a causal mask a tile holds keys that some of its rows do not see.  Their weights are
+// zero, but zero times an infinite or NaN value is NaN.  A wave whose results are not
+// all finite forms those rows again, key by key, with the seen keys alone (tiles first,
+// first + step, ... < end of `keys` keys): slow, and only then.
+template <typename T, int DB, int QS>
+__device__ __forceinline__ void redo_not_finite(const AttnParams& p, const char* kb, const char* vb, int64_t sk, int64_t sv,
+                                                int lim, int first, int end, int step, int keys, const uint4* qf,
+                                                float c2, f32x16* o, float& m, float& l) {
+  constexpr int PER = 16 / sizeof(T);  // values of a 16-byte chunk
+  const int h = (threadIdx.x & 63) >> 5;
+  float far = 0.0f;  // NaN when a result is not finite
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) far = __builtin_fmaf(o[d][i], 0.0f, far);
+  far = half_sum(far);
+  const bool bad = far != far;
+  if (!__any(bad)) return;
+  if (!bad) lim = 0;  // (the others keep what they have)
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = bad ? 0.0f : o[d][i];
+  m = bad ? -INFINITY : m;
+  l = bad ? 0.0f : l;
+  for (int t = first; t < end; t += step)
+    for (int j = t * keys; j < (t + 1) * keys && __any(j < lim); ++j) {
+      const bool seen = j < lim;
+      float s = 0.0f;
+#pragma unroll
+      for (int st = 0; st < QS; ++st) {
+        const int c = 2 * st + h;
+        if (seen && c * PER < p.D) {
+          float a[8], b[8];
+          const uint4 k = *(const uint4*)(kb + (int64_t)j * sk + c * 16);
+          if constexpr (PER == 8) {
+            unpack8(k, a);
+            unpack8(qf[st], b);
+          } else {
+            const f32x4 kf = __builtin_bit_cast(f32x4, k), qq = __builtin_bit_cast(f32x4, qf[st]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[e] = kf[e], b[e] = qq[e];
+          }
+#pragma unroll
+          for (int e = 0; e < PER; ++e) s = __builtin_fmaf(a[e], b[e], s);
+        }
+      }
+      s = half_sum(s) * c2;
+      if (!seen) continue;
+      const float mn = fmaxf(m, s), use = mn == -INFINITY ? 0.0f : mn;
+      const float keep = exp2_(m - use), w = exp2_(s - use);
+      m = mn;
+      l = l * keep + (h == 0 ? w : 0.0f);  // (the halves' sums are added later)
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int col = d * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
+          if (col >= p.D) continue;
+          const T x = *(const T*)(vb + (int64_t)j * sv + col * sizeof(T));
+          float v;
+          if constexpr (sizeof(T) == 2) v = bf16_to_f32(x);
+          else v = x;
+          o[d][i] = o[d][i] * keep + w * v;
+        }
+    }
+}
+
 // A workgroup takes 32 packed query rows of one (batch, key head) and a share of
 // its keys; its waves take tiles of 32 keys in turn, each through its own LDS
 // tiles, without a barrier until their results meet at the end.
@@ -327,6 +395,9 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
     buf = NBUF == 2 ? buf ^ 1 : 0;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+
+  if (p.causal && p.q_len > 1)
+    redo_not_finite<T, DB, QS>(p, kb, vb, sk, sv, lim, t0 + wave, t_end, NW, kKeys, qf, c2, o, m, l);
 
   // the waves' results: a common maximum, then the sums in wave order
   l = half_sum(l);
@@ -636,6 +707,8 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
     if (t + KS + kg < t_wave) step(t + KS + kg, odd, sb, sa);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (p.causal && p.q_len > 1)
+    redo_not_finite<bf16_t, DB, QS>(p, kb, vb, sk, sv, lim, t0 + kg, t_end, KS, kTileKeys, qf, c2, o, m, l);
   l = half_sum(l);
   if constexpr (KS > 1) {
     // the second key group hands its results over, lane by lane, in the place of the tiles

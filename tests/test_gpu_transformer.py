@@ -349,6 +349,29 @@ def test_attention_infinities_and_nan_in_seen_places(q_len):
     assert np.isnan(y[q_len:]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_len, k_len, d", [(8, 50, 64), (100, 100, 64), (100, 100, 128), (300, 300, 32), (70, 70, 256)])
+def test_attention_causal_hides_infinities_and_nan(q_len, k_len, d, dtype):
+    """A key that a row does not see cannot reach it, though its tile holds rows that see it."""
+    r = np.random.default_rng(7)
+    h, kv = 4, 2
+    q, k, v = _normal(r, q_len, h * d), _normal(r, k_len, kv * d), _normal(r, k_len, kv * d)
+    v[k_len - 3, 1] = np.nan
+    v[k_len - 5, d + 2] = np.inf
+    v[k_len - 4, 7] = -np.inf
+    k[k_len - 1, d:] = np.nan
+    attrs = {"batch": 1, "heads": h, "kv_heads": kv, "head_dim": d, "causal": True}
+    y = _run("attention", {"q": q, "k": k, "v": v}, ["q", "k", "v"], attrs, dtype)
+    with np.errstate(invalid="ignore"):
+        ref, absum, score = T.attention(attrs, q, k, v, None, magnitudes=True)
+    assert np.array_equal(np.isnan(y), np.isnan(ref)) and np.isnan(ref).any() and not np.isnan(ref).all()
+    inf = np.isinf(ref)
+    assert inf.any() and np.array_equal(y[inf], ref[inf])
+    fine = np.isfinite(ref)
+    bound = (2 * (d + 8) * E * score + (k_len + 64) * E + (U if dtype == "bf16" else 0)) * absum
+    _close(y[fine], ref[fine], bound[fine], dtype)
+
+
 def test_attention_separate_and_shared_inputs_agree():
     r = np.random.default_rng(6)
     b, lq, lk, h, d = 2, 40, 70, 2, 64
