@@ -1216,33 +1216,38 @@ void Planner::plan_qdense(int ni) {
   const auto& ws = g.values[n.weight].shape;
   const int M = (int)xs[0], K = (int)xs[1], N = (int)ws[0];
   const int Kq = (int)rup(K, 128), rows = (int)rup(N, kRowPad);
-  const bool fused = qdense_fuses_rows(M, Kq);
+  Launch L;
+  const bool fused = L.fused = qdense_fuses_rows(M, cp[n.out], Kq);
   Launch& Q = quant_of[n.data];
-  if (Q.x.kind == Ref::None) {
+  if (fused) {
+    L.x = loc[n.data];
+    L.qr.ldx = cp[n.data];
+    L.qr.M = L.qr.rows = M, L.qr.K = K, L.qr.Kq = Kq;
+    L.qr.f32 = !bf16;
+  } else if (Q.x.kind == Ref::None) {
     Q.op = Launch::QuantRows;
     Q.info.kind = BYOC_K_QDENSE;
     Q.info.node = ni;
     Q.x = loc[n.data];
     Q.qr_scales = rup((int64_t)M * Kq, 256);
-    if (!fused) Q.y = arena(Q.qr_scales + (int64_t)M * 4);
+    Q.y = arena(Q.qr_scales + (int64_t)M * 4);
     Q.qr.ldx = cp[n.data];
     Q.qr.M = Q.qr.rows = M, Q.qr.K = K, Q.qr.Kq = Kq;
     Q.qr.f32 = !bf16;
     Q.info.bytes = act_bytes(n.data) + (int64_t)M * K + M * 4;
     name(Q, "quant_rows");
-    if (!fused) e->launches.push_back(Q);
+    e->launches.push_back(Q);
   }
-  Launch L;
   L.op = Launch::QDense;
   L.info.kind = BYOC_K_QDENSE;
   L.info.node = ni;
   L.info.flops = 2 * n.macs;
   L.info.bytes = (int64_t)M * K + M * 4 + (int64_t)N * K + N * 4 + (n.bias >= 0 ? N * 4 : 0) +
                  act_bytes(n.out) * (n.residual >= 0 ? 2 : 1);
-  L.fused = fused;
-  L.x = fused ? Q.x : Q.y;
-  L.qr = Q.qr;
-  L.qr_scales = Q.qr_scales;
+  if (!fused) {
+    L.x = Q.y;
+    L.qr_scales = Q.qr_scales;
+  }
   L.y = loc[n.out];
   if (n.residual >= 0) L.res = loc[n.residual];
   const int wc = g.values[n.weight].index;

@@ -478,7 +478,7 @@ struct QDenseTile {
 };
 QDenseTile choose_qdense_tile(int64_t M, int64_t N, int64_t Kq);
 // Few enough rows for the product's workgroups to quantize them for themselves (q: the rows; p.x and p.xs unused).
-bool qdense_fuses_rows(int64_t M, int64_t Kq);
+bool qdense_fuses_rows(int64_t M, int64_t N, int64_t Kq);
 hipError_t launch_qdense_fused(const QDenseParams& p, const QRowsParams& q, hipStream_t s);
 hipError_t launch_qdense(const QDenseParams& p, QDenseTile t, hipStream_t s);
 

@@ -653,10 +653,15 @@ hipError_t launch_quant_rows(const QRowsParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-bool qdense_fuses_rows(int64_t M, int64_t Kq) { return M <= 8 && M * Kq <= kFusedCodes; }
+constexpr int kRowsN = 16 * 256;  // channels of the rows kernel: a workgroup of 16 for each CU
+
+// (1 x 4096 x 4096: 8.4 us, 8.7 with a launch for the rows; 8 x 1024 x 4096: 5.3 and 7.9; but 4 x 4096 x 4096,
+// as every workgroup quantizes all rows, 12.5 and 8.9, and 1 x 4096 x 12288, 768 workgroups, 18.5 and 12.5 on
+// 64x64 tiles)
+bool qdense_fuses_rows(int64_t M, int64_t N, int64_t Kq) { return M <= 8 && M * Kq <= kFusedCodes && N <= kRowsN; }
 
 hipError_t launch_qdense_fused(const QDenseParams& p, const QRowsParams& q, hipStream_t s) {
-  if (!qdense_fuses_rows(p.M, p.Kq)) return hipErrorInvalidValue;
+  if (!qdense_fuses_rows(p.M, p.N, p.Kq)) return hipErrorInvalidValue;
   return p.f32 ? launch_rows<true>(p, q, true, s) : launch_rows<false>(p, q, true, s);
 }
 
@@ -664,7 +669,7 @@ hipError_t launch_qdense_fused(const QDenseParams& p, const QRowsParams& q, hipS
 // 3072: 8.8 us against 9.4 on 32x32 tiles, 16 x 8192 x 1024: 15.0 against 16.4; but 16 x
 // 4096 x 12288, 768 workgroups: 23.5 against 15.2); else the tile of least modelled time.
 QDenseTile choose_qdense_tile(int64_t M, int64_t N, int64_t Kq) {
-  if (qdense_fuses_rows(M, Kq) || (M <= 32 && N <= 16 * 256)) return {kQDenseRows, (int)(M + 15) / 16 * 16, 16};
+  if (M <= 32 && N <= kRowsN) return {kQDenseRows, (int)(M + 15) / 16 * 16, 16};
   QDenseTile best{};
   double least = INFINITY;
 #define X(ID, BM, BN, WM, WN, NS, OCC, LONE, BUSY, ROUND)                                                \

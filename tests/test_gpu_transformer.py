@@ -74,6 +74,9 @@ QDENSE = [
     (1, 1, 1, "bf16", "_bias"),
     (1, 1, 1, "f32", "_bias"),
     (2, 1000, 24, "bf16", "_bias_add_relu"),
+    (2, 512, 4104, "bf16", "_bias_gelu"),
+    (8, 1000, 4096, "f32", "_bias"),
+    (32, 384, 4096, "bf16", "_add"),
     (3, 129, 257, "bf16", "_bias"),
     (4, 4096, 96, "bf16", "_bias"),
     (5, 100, 1003, "f32", "_bias_add"),
