@@ -417,6 +417,27 @@ struct Planner {
     return r;
   }
 
+  // Reads of value v by nodes and by outputs past the first, and whether qdense nodes alone read it as rows
+  // or residual.
+  int reads(int v) const {
+    int n = -1;
+    for (const IoDesc& o : g.outputs) n += o.value == v;
+    n = std::max(n, 0);
+    for (const Node& x : g.nodes) {
+      for (int a : {x.data, x.residual, x.other, x.key, x.value, x.index}) n += a == v;
+      if (x.op == OpKind::Concat) n += (int)std::count(x.cat.begin() + 1, x.cat.end(), v);
+    }
+    return n;
+  }
+  bool only_qdense_reads(int v) const {
+    int n = 0;
+    for (const Node& x : g.nodes)
+      if (x.op == OpKind::QDense) n += (x.data == v) + (x.residual == v);
+    for (const IoDesc& o : g.outputs)
+      if (o.value == v && g.values[v].source == Value::Input) return false;
+    return n == reads(v);
+  }
+
   Status plan();
   Status plan_i8();
   void plan_node(int ni);
@@ -1104,9 +1125,10 @@ Status Planner::plan() {
       loc[v] = io(Ref::Input, (int)i);
       continue;
     }
-    const bool direct = bf16 ? (s.size() == 2 && in.dtype == DType::BF16 && s[1] % 8 == 0)
-                             : (in.dtype == DType::F32);
+    const bool rows = bf16 && s.size() == 2 && in.dtype == DType::BF16;
+    const bool direct = bf16 ? rows && (s[1] % 8 == 0 || only_qdense_reads(v)) : (in.dtype == DType::F32);
     if (direct) {
+      if (bf16) cp[v] = (int)s[1];  // (qdense takes rows of any width)
       loc[v] = io(Ref::Input, (int)i);
       continue;
     }
@@ -1145,9 +1167,11 @@ Status Planner::plan() {
     for (size_t j = 0; j < g.outputs.size() && !placed; ++j) {
       const IoDesc& o = g.outputs[j];
       if (o.value != v || direct_out[j]) continue;
-      const bool ok = bf16 ? (s.size() == 2 && o.dtype == DType::BF16 && s[1] % 8 == 0)
+      const bool rows = bf16 && s.size() == 2 && o.dtype == DType::BF16;
+      const bool ok = bf16 ? rows && (s[1] % 8 == 0 || (n.op == OpKind::QDense && only_qdense_reads(v) && reads(v) == 0))
                            : (o.dtype == DType::F32);
       if (ok) {
+        if (bf16) cp[v] = (int)s[1];  // (qdense writes rows of any width)
         loc[v] = io(Ref::Output, (int)j);
         direct_out[j] = true;
         placed = true;
@@ -1266,7 +1290,8 @@ void Planner::plan_qdense(int ni) {
   QDenseParams& p = L.qn;
   p.M = M, p.N = cp[n.out], p.Kq = Kq;
   p.ldy = cp[n.out];
-  p.ldr = cp[n.out];
+  p.ldr = n.residual >= 0 ? cp[n.residual] : 0;
+  p.channels = N;
   p.act = (int)n.act;
   p.alpha = n.alpha;
   p.f32 = !bf16;

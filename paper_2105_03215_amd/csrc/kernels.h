@@ -466,7 +466,8 @@ struct QDenseParams {
   const void* res;    // [M][ldr], the type of y, or nullptr
   void* y;            // [M][ldy], bf16 or f32
   int64_t ldy, ldr;
-  int M, N, Kq;       // N: columns written
+  int M, N, Kq;       // N: columns written (of y: channels and their padding)
+  int channels;       // of the layer
   int act;
   float alpha;
   int f32;

@@ -20,7 +20,7 @@ using namespace dma;
 
 // 8 consecutive values of a row as they are stored, zero from column K on.  f32 rows
 // need not be 16-byte aligned (their stride is any number of columns); bf16 rows
-// are, but for constants of other widths (`vec` false).
+// are, but for constants and callers' rows of other widths (`vec` false).
 struct __attribute__((packed, aligned(4))) F32x4u {
   float v[4];
 };
@@ -236,7 +236,7 @@ __device__ __forceinline__ Chunk<F32> load_res(const QDenseParams& p, int64_t m,
       for (int e = 0; e < 8; ++e) r.v[e] = p.res && n + e < p.N ? rp[e] : 0.0f;
     }
   } else {
-    r.u = p.res ? *(const uint4*)((const bf16_t*)p.res + m * p.ldr + n) : make_uint4(0u, 0u, 0u, 0u);
+    r.load(p.res, m * p.ldr, n, p.res ? (p.ldr % 8 == 0 ? (int)p.ldr : p.channels) : 0, p.ldr % 8 == 0);
   }
   return r;
 }
@@ -260,7 +260,14 @@ __device__ __forceinline__ void finish8(const QDenseParams& p, const int* acc, f
         if (n + e < p.N) y[e] = v[e];
     }
   } else {
-    *(uint4*)((bf16_t*)p.y + m * p.ldy + n) = pack8(v);
+    bf16_t* y = (bf16_t*)p.y + m * p.ldy + n;
+    if (p.ldy % 8 == 0) {
+      *(uint4*)y = pack8(v);
+    } else {  // (rows of the caller's, of any width)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (n + e < p.N) y[e] = f32_to_bf16(v[e]);
+    }
   }
 }
 

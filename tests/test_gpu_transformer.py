@@ -155,6 +155,29 @@ def test_qdense_odd_rows(m):
         _close(y, ref, 8 * E * np.abs(ref) + 2.0 ** -126, "bf16")
 
 
+def test_qdense_odd_widths_between_layers():
+    """Rows of a width that is no multiple of 8, as input, residual, between layers and twice an output."""
+    from paper_2105_03215_amd import capi, runtime
+    g = workloads.GraphBuilder("t", 97)
+    x = g.input("x", [21, 77], "normal")
+    r = g.input("r", [21, 131], "normal")
+    h = g.qdense(x, 131, act="relu", residual=r)
+    y = g.qdense(h, 53, act="gelu")
+    z = g.add(h, r)
+    for v in (y, h, y, z):
+        g.output(v)
+    wl = g.finish()
+    with capi.Subgraph(wl.graph, wl.consts, device=0) as sg:
+        got = runtime.run_once(sg, wl.inputs, DEV)
+    vals = {"x": wl.inputs[0], "r": wl.inputs[1]}
+    by = {c["name"]: wl.consts[c["index"]] for c in wl.graph["constants"]}
+    for node, v in zip(wl.graph["nodes"], (got[1], got[0], got[3])):
+        ref = oracle.run_node(node, [vals.get(a, by.get(a)) for a in node["inputs"]], mode="exact")
+        _close(v, ref, 2.0 ** -18 * (np.abs(ref) + 20), "bf16")
+        vals[node["name"]] = v
+    assert np.array_equal(got[0], got[2])
+
+
 def test_qdense_rows_of_one_value_share_their_codes():
     """Two products of one value, and the graph that holds both, give what each gives alone."""
     from paper_2105_03215_amd import capi, runtime
