@@ -485,7 +485,18 @@ __global__ __launch_bounds__(kRowThreads) void qdense_rows_kernel(QDenseParams p
         a[u][j] = t < steps ? *(const uint4*)(wp + (int64_t)j * 16 * p.Kq + t * 64) : make_uint4(0u, 0u, 0u, 0u);
     }
   };
+  // this thread's 8 outputs, and what they need besides the sums: on its way from the start
+  static_assert(MT * 16 * NT * 2 <= kRowThreads, "an output group each");
+  const int om = tid / (NT * 2), og = tid % (NT * 2), on = n0 + og * 8;
+  const bool out = om < p.M && on < p.N && tid < MT * 16 * NT * 2;
+  float ws[8], bias[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  Chunk<F32> res;
   load_w(0);
+  if (out) {
+    load8f(p.ws + on, ws);
+    if (p.bias) load8f(p.bias + on, bias);
+    res = load_res<F32>(p, om, on);
+  }
   if constexpr (FUSED) {
     // waves per row: as many as there are for the rows rounded up to a power of two
     const int lg = p.M > 4 ? 3 : (p.M > 2 ? 2 : p.M - 1);
@@ -558,36 +569,23 @@ __global__ __launch_bounds__(kRowThreads) void qdense_rows_kernel(QDenseParams p
 #pragma unroll
     for (int j = 0; j < NT; ++j) red[wave][k * NT + j][lane] = acc[k][j];
   __syncthreads();
-  // row m, channels n0 + 16 j + 4 c .. + 3 sit in lane 16 c + m % 16 of tile (m / 16, j) of every wave;
-  // a thread takes 8 channels
+  // row m, channels n0 + 16 j + 4 c .. + 3 sit in lane 16 c + m % 16 of tile (m / 16, j) of every wave
+  if (!out) return;
   const ActClamp ac = act_clamp_of(p.act, p.alpha);
-  auto epilogue = [&](auto mode_tag) {
-    for (int at = tid; at < MT * 16 * NT * 2; at += kRowThreads) {
-      const int m = at / (NT * 2), g = at % (NT * 2);
-      const int n = n0 + g * 8;
-      if (m >= p.M || n >= p.N) continue;
-      int s[8];
+  int sum[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[e] = 0;
+  for (int e = 0; e < 8; ++e) sum[e] = 0;
 #pragma unroll
-      for (int w = 0; w < kRowWaves; ++w)
+  for (int w = 0; w < kRowWaves; ++w)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const i32x4 r = red[w][(m >> 4) * NT + (g >> 1)][((g & 1) * 2 + half) * 16 + (m & 15)];
+    for (int half = 0; half < 2; ++half) {
+      const i32x4 r = red[w][(om >> 4) * NT + (og >> 1)][((og & 1) * 2 + half) * 16 + (om & 15)];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[4 * half + e] += r[e];
-        }
-      float ws[8], bias[8];
-      load8f(p.ws + n, ws);
-      if (p.bias) {
-        load8f(p.bias + n, bias);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) bias[e] = 0.0f;
-      }
-      finish8<F32, decltype(mode_tag)::value>(p, s, FUSED ? scales[m] : p.xs[m], ws, bias,
-                                              load_res<F32>(p, m, n), m, n, ac);
+      for (int e = 0; e < 4; ++e) sum[4 * half + e] += r[e];
     }
+  const float xs = FUSED ? scales[om] : p.xs[om];
+  auto epilogue = [&](auto mode_tag) {
+    finish8<F32, decltype(mode_tag)::value>(p, sum, xs, ws, bias, res, om, on, ac);
   };
   if (act_mode(p.act) == 1)
     epilogue(std::integral_constant<int, 1>{});
