@@ -66,6 +66,10 @@ template <>
 struct Raw<bf16_t> {
   uint4 u;
   __device__ __forceinline__ void load(const bf16_t* p) { u = *(const uint4*)p; }
+  __device__ __forceinline__ void load(const bf16_t* p, const bf16_t* q) {  // 4 columns each
+    const uint2 a = *(const uint2*)p, b = *(const uint2*)q;
+    u = make_uint4(a.x, a.y, b.x, b.y);
+  }
   __device__ __forceinline__ void get(float* f) const { unpack8(u, f); }
   __device__ __forceinline__ Raw across(int d) const {
     Raw r;
@@ -78,6 +82,10 @@ template <>
 struct Raw<float> {
   float v[8];
   __device__ __forceinline__ void load(const float* p) { load8(p, v); }
+  __device__ __forceinline__ void load(const float* p, const float* q) {
+    const float4 a = *(const float4*)p, b = *(const float4*)q;
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+  }
   __device__ __forceinline__ void get(float* f) const {
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = v[e];
@@ -130,8 +138,10 @@ __device__ __forceinline__ void coefficients(const RotaryParams& p, int row0, in
 
 // LH lanes per head, 8 consecutive columns each (D <= 8 LH); RB rows per workgroup,
 // hb heads per workgroup; U heads of a lane on their way together.  In the half
-// layout a lane needs its partner's columns too: from the lane that has them where
-// the whole head turns and fills its lanes (ACROSS), else read again.
+// layout a lane needs its partners' columns too: from the lane that has them where
+// the whole head turns and fills its lanes (ACROSS), else read again, four at a time, as
+// half of the turning columns need not be whole chunks (8192 rows of 32 normed heads of 48,
+// 24 columns turning: 81 us column by column, 14 so).
 template <typename T, int LH, bool NORM, bool INTER, bool ACROSS, int U>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int RB, int hb) {
   extern __shared__ __align__(16) float2 cs[];
@@ -146,7 +156,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int RB
   const int e0 = c * 8;
   const bool live = e0 < p.D;
   const bool turn = live && e0 < p.rd;                 // (whole chunks turn or stay)
-  const int pe = e0 >= half ? e0 - half : e0 + half;  // half layout: the partner's first column
+  // half layout: the partners' first columns, of the first and of the last four
+  const int pe0 = e0 >= half ? e0 - half : e0 + half, pe1 = e0 + 4 >= half ? e0 + 4 - half : e0 + 4 + half;
   const T* const x0 = (const T*)p.x + (int64_t)row0 * p.ldx + (int64_t)h0 * p.D;
   T* const y0 = (T*)p.y + (int64_t)row0 * p.ldy + (int64_t)h0 * p.D;
   // item it: row it / nh, head it % nh of this workgroup; a lane's first and its next
@@ -162,7 +173,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int RB
       if (it + u * SLOTS < items) {
         const T* x = x0 + (int64_t)r * p.ldx + h * p.D;
         if (live) v[u].load(x + e0);
-        if (!INTER && !ACROSS && turn) o[u].load(x + pe);
+        if (!INTER && !ACROSS && turn) o[u].load(x + pe0, x + pe1);
       }
       r += dr, h += dh;
       if (h >= nh) h -= nh, ++r;
@@ -272,7 +283,7 @@ hipError_t launch(const RotaryParams& p, hipStream_t s) {
   const int RB = std::min(4, std::max(1, p.M / 1024));
   int lh = 1;
   while (lh * 8 < p.D) lh *= 2;
-  const bool fast = p.D % 8 == 0 && lh <= 64 && (p.interleaved ? p.rd : half) % 8 == 0 &&
+  const bool fast = p.D % 8 == 0 && lh <= 64 && p.rd % 8 == 0 &&
                     (sizeof(T) == 2 || (p.ldx % 4 == 0 && p.ldy % 4 == 0));
   const int slots = fast ? kThreads / lh : kThreads / 64;
   const int hb = p.M >= 1024 ? H : std::min(H, slots);

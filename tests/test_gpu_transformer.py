@@ -251,6 +251,19 @@ def test_rotary(m, heads, kv, d, rd, dtype, norm, layout, scaling, extra):
     _close(y, ref, 2.0 ** -20 * 1.5 * mag.reshape(m, -1) + (d / 8 + 8) * E * mag.reshape(m, -1), dtype)
 
 
+@pytest.mark.parametrize("m, heads, kv, d, rd, dtype, norm, layout, scaling, extra", [
+    (5, 3, 2, 48, 24, "bf16", True, "half", None, 0),
+    (1100, 2, 1, 80, 40, "bf16", False, "half", "linear", 5),
+    (9, 2, 2, 80, 40, "f32", True, "half", "yarn", 8),
+    (9, 3, 1, 8, 8, "bf16", True, "half", None, 0),
+    (7, 2, 0, 56, 8, "f32", False, "half", None, 4),
+    (7, 2, 1, 40, 20, "bf16", True, "half", None, 0),
+])
+def test_rotary_halves_of_no_whole_chunks(m, heads, kv, d, rd, dtype, norm, layout, scaling, extra):
+    """Pairs whose two columns lie in 16-byte chunks at different places."""
+    test_rotary(m, heads, kv, d, rd, dtype, norm, layout, scaling, extra)
+
+
 def test_rotary_padding_columns_are_zero():
     """Heads that do not fill a multiple of 8 columns feed a dense layer, which reads the padding."""
     from paper_2105_03215_amd import capi, runtime
