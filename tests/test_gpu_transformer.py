@@ -135,6 +135,19 @@ def test_qdense_f32_values_of_any_bits():
     _close(y, T.qdense(x, w), step * 1.001, "f32")
 
 
+@pytest.mark.parametrize("m, k, n, dtype, suffix", [
+    (9, 1003, 4099, "bf16", "_bias_add_gelu"),
+    (70, 515, 1001, "bf16", "_add"),
+    (300, 2051, 301, "bf16", "_bias_add_relu"),
+    (513, 130, 2305, "bf16", "_add"),
+    (301, 515, 1003, "f32", "_bias_add"),
+    (9, 7, 9, "bf16", "_add"),
+])
+def test_qdense_rows_at_any_address(m, k, n, dtype, suffix):
+    """Rows of odd widths: their values start at any multiple of their own size."""
+    test_qdense(m, k, n, dtype, suffix)
+
+
 @pytest.mark.parametrize("m", [1, 9, 70])
 def test_qdense_odd_rows(m):
     """Rows of zeros, of one value, with infinities and NaN, of the smallest and largest magnitudes."""
