@@ -63,9 +63,12 @@ __device__ __forceinline__ int batch_len(const AttnParams& p, int b) {
 
 // The key axis of few rows is split into p.chunks chunks, shared by the sequences in
 // proportion to their lengths, which only the device knows: chunks of `size` tiles each,
-// the first of sequence b number `first`, `count` of them.  With size = ceil(tiles of all /
-// (chunks - batch)) they never need more than p.chunks.  More than 64 sequences
-// (lanes) get the same number each.  chunks == batch: a sequence each.
+// the first of sequence b number `first`, `count` of them, with the least size that needs
+// no more than p.chunks.  That is at least ceil(tiles of all / chunks) and at most ceil(tiles
+// of all / (chunks - batch)), as rounding up costs a sequence less than one chunk: each lane
+// counts the chunks of one size between (16 x 1 over 16384 keys, 8 heads of 64: 146 us
+// with the upper bound, which left half of the CUs without work, 114 so).
+// More than 64 sequences (lanes) get the same number each.  chunks == batch: a sequence each.
 // (floats of the workspace's head, a multiple of 4 so that the sums can be written 16 bytes at a time)
 __host__ __device__ __forceinline__ int64_t head_floats(const AttnParams& p) { return (2 * (int64_t)p.batch + 3) / 4 * 4; }
 struct Chunks {
@@ -79,7 +82,19 @@ __device__ __forceinline__ Chunks lane_chunks(const AttnParams& p) {
   for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d, 64);
   Chunks c;
   const int spare = p.chunks - p.batch;
-  c.size = max(1, (total + spare - 1) / spare);
+  const int low = max(1, (total + p.chunks - 1) / p.chunks), high = max(1, (total + spare - 1) / spare);
+  const int size = low + lane * ((high - low + 62) / 63);
+  const float inv = 1.0f / (float)size;
+  int need = 0;
+  for (int b = 0; b < p.batch; ++b) {
+    const int n = __builtin_amdgcn_readlane(mine, b);
+    int q = (int)((float)n * inv);  // (at most p.chunks: not more than 1 away from the quotient)
+    const int r = n - q * size;
+    q += r > size ? 2 : r > 0 ? 1 : r > -size ? 0 : -1;  // rounded up
+    need += q;
+  }
+  const unsigned long long fits = __ballot(need <= p.chunks);
+  c.size = __builtin_amdgcn_readlane(size, __builtin_ctzll(fits));  // (lane 63's is `high` or more: it fits)
   c.count = (mine + c.size - 1) / c.size;
   c.first = c.count;
 #pragma unroll
@@ -775,48 +790,76 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
     }
 }
 
-// Joins the chunks of a packed row: a group of D / 4 lanes (of 64 / 32 / 16 lanes), 4 columns each.
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p, int lanes) {
+// Joins the chunks of a packed row: D / 4 lanes (of 64 / 32 / 16), 4 columns each, and `split` such groups a
+// row that take the chunks in turn, so that many chunks are on their way together where there are few rows
+// (one token over 32768 keys, 16 heads on one of 128, 16 rows of 85 chunks: 39 us by one group, 17 by eight).
+__global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p, int lanes, int split) {
+  __shared__ float4 part[256];
+  __shared__ float2 part_ml[256];
   const int R = p.q_len * p.group;
   // rows of one sequence per workgroup row (blockIdx.y), so that a wave has one set of chunks
   const int b = blockIdx.y;
   const int len = batch_len(p, b);
   const int2 ck = len > 0 ? ((const int2*)p.ws)[b] : make_int2(0, 0);  // first chunk, count
-  const int at = blockIdx.x * (256 / lanes) + threadIdx.x / lanes;  // (key head, packed row)
+  const int slot = threadIdx.x / lanes, g0 = slot % split;
+  const int at = blockIdx.x * (256 / lanes / split) + slot / split;  // (key head, packed row)
   const int c = threadIdx.x % lanes * 4;
-  if (at >= p.kv_heads * R || c >= p.D) return;
-  const int kh = at / R, row = at - kh * R;
-  const float* ml = part_scale(p, kh, row, ck.x);
-  const float* os = part_sums(p, kh, row, ck.x) + c;
+  const bool live = at < p.kv_heads * R && c < p.D;
+  const int kh = live ? at / R : 0, row = live ? at - kh * R : 0;
   // eight chunks at a time, their loads on the way together
   float top = -INFINITY, total = 0.0f;
   float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s0 = 0; s0 < ck.y; s0 += 8) {
-    float2 m[8];
-    float4 x[8];
+  if (live) {
+    const float* ml = part_scale(p, kh, row, ck.x);
+    const float* os = part_sums(p, kh, row, ck.x) + c;
+    for (int s0 = g0; s0 < ck.y; s0 += 8 * split) {
+      float2 m[8];
+      float4 x[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int s = min(s0 + k, ck.y - 1);
-      m[k] = *(const float2*)(ml + 2 * s);
-      x[k] = *(const float4*)(os + (int64_t)s * p.D);
+      for (int k = 0; k < 8; ++k) {
+        const int s = min(s0 + k * split, ck.y - 1);
+        m[k] = *(const float2*)(ml + 2 * s);
+        x[k] = *(const float4*)(os + (int64_t)s * p.D);
+      }
+      float most = top;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) most = fmaxf(most, m[k].x);
+      const float use = most == -INFINITY ? 0.0f : most;
+      const float keep = exp2_(top - use);
+      top = most;
+      total *= keep;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] *= keep;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (s0 + k * split >= ck.y) break;
+        const float f = exp2_(m[k].x - use);
+        total += m[k].y * f;
+        v[0] += x[k].x * f, v[1] += x[k].y * f, v[2] += x[k].z * f, v[3] += x[k].w * f;
+      }
     }
+  }
+  if (split > 1) {  // (the groups in order, so that a sum does not depend on their timing)
+    part[threadIdx.x] = make_float4(v[0], v[1], v[2], v[3]);
+    part_ml[threadIdx.x] = make_float2(top, total);
+    __syncthreads();
+    if (g0 > 0) return;
     float most = top;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) most = fmaxf(most, m[k].x);
+    for (int k = 1; k < split; ++k) most = fmaxf(most, part_ml[threadIdx.x + k * lanes].x);
     const float use = most == -INFINITY ? 0.0f : most;
     const float keep = exp2_(top - use);
-    top = most;
     total *= keep;
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] *= keep;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (s0 + k >= ck.y) break;
-      const float f = exp2_(m[k].x - use);
-      total += m[k].y * f;
-      v[0] += x[k].x * f, v[1] += x[k].y * f, v[2] += x[k].z * f, v[3] += x[k].w * f;
+    for (int k = 1; k < split; ++k) {
+      const float2 m = part_ml[threadIdx.x + k * lanes];
+      const float4 x = part[threadIdx.x + k * lanes];
+      const float f = exp2_(m.x - use);
+      total += m.y * f;
+      v[0] += x.x * f, v[1] += x.y * f, v[2] += x.z * f, v[3] += x.w * f;
     }
   }
+  if (!live) return;
   const bool any = seen_keys(p, len, row) > 0;
   const int i = row / p.group, g = row - i * p.group;
   const int64_t out = (b * (int64_t)p.q_len + i) * p.ldy + (kh * p.group + g) * p.D + c;
@@ -850,14 +893,15 @@ void choose_attention(AttnParams& p) {
   p.tile_keys = tiled ? kTileKeys : kKeys;
   const int64_t blocks = (int64_t)p.batch * p.kv_heads * row_blocks(p);
   // Tiles: a split fills the two workgroups that a CU has room for where there is less than one.
-  int64_t most = blocks >= 256 ? 1 : std::min<int64_t>(512 / blocks, ceil_div(p.k_len, 512));
+  int64_t slots = blocks >= 256 ? 0 : 512, per = ceil_div(p.k_len, 512);
   if (!tiled) {
     // Rows: one workgroup has a CU to itself; three rounds of its waves in each at least, which take as
     // long as the join
-    const int round = kKeys * row_waves(p);
-    most = std::min<int64_t>(256 / std::min<int64_t>(blocks, 256), ceil_div(p.k_len, round) / 3);
+    slots = 256;
+    per = ceil_div(p.k_len, kKeys * row_waves(p)) / 3;
   }
-  p.chunks = p.batch * (int)std::max<int64_t>(1, std::min<int64_t>(most, 256));
+  const int64_t chunks = std::min<int64_t>(slots / std::max<int64_t>(1, blocks / p.batch), p.batch * per);
+  p.chunks = chunks < 2 * (int64_t)p.batch ? p.batch : (int)(p.batch > 64 ? chunks / p.batch * p.batch : chunks);
 }
 
 const char* attention_name(const AttnParams& p) {
@@ -896,8 +940,11 @@ hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
 
 hipError_t launch_attention_join(const AttnParams& p, hipStream_t s) {
   const int lanes = p.D <= 64 ? 16 : p.D <= 128 ? 32 : 64;
-  const dim3 grid(ceil_div((int64_t)p.kv_heads * p.q_len * p.group, 256 / lanes), p.batch);
-  attention_join_kernel<<<grid, 256, 0, s>>>(p, lanes);
+  const int64_t rows = (int64_t)p.kv_heads * p.q_len * p.group;
+  int split = 1;
+  while (split < 256 / lanes && split * 8 < p.chunks && rows * p.batch * split * lanes < 256 * 256) split *= 2;
+  const dim3 grid(ceil_div(rows, 256 / lanes / split), p.batch);
+  attention_join_kernel<<<grid, 256, 0, s>>>(p, lanes, split);
   return hipGetLastError();
 }
 

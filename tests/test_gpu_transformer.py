@@ -435,6 +435,28 @@ def test_attention_separate_and_shared_inputs_agree():
     assert np.array_equal(a, c)
 
 
+# Key axes split over workgroups: sequences of one length and of different ones, empty ones among them,
+# more sequences than a wave has lanes, chunks that some rows see nothing of, joins of few and of many chunks.
+ATTENTION_SPLIT = [
+    (16, 1, 3000, 4, 4, 64, "bf16", False, None),
+    (1, 1, 9000, 16, 1, 128, "bf16", False, None),
+    (1, 1, 9001, 2, 1, 256, "bf16", False, [8999]),
+    (5, 7, 4100, 2, 1, 40, "f32", True, [4100, 0, 3, 1500, 2222]),
+    (12, 1, 2000, 2, 2, 128, "bf16", False, [2000, 1, 0, 999, 1024, 1025, 31, 33, 0, 1999, 500, 1700]),
+    (64, 1, 800, 1, 1, 64, "bf16", False, [(37 * i) % 801 for i in range(64)]),
+    (70, 1, 500, 1, 1, 32, "bf16", False, [(61 * i) % 501 for i in range(70)]),
+    (3, 50, 3000, 2, 2, 64, "bf16", True, None),
+    (2, 45, 2600, 1, 1, 128, "bf16", True, [2600, 40]),
+]
+
+
+@pytest.mark.parametrize("batch, q_len, k_len, heads, kv, d, dtype, causal, lengths", ATTENTION_SPLIT)
+def test_attention_split_keys(batch, q_len, k_len, heads, kv, d, dtype, causal, lengths):
+    announce("attention split b %d q %d k %d heads %d/%d d %d %s" % (batch, q_len, k_len, heads, kv, d, dtype))
+    y, ref, bound = _attention(batch, q_len, k_len, heads, kv, d, dtype, causal, lengths, seed=8, spoil=lengths is not None)
+    _close(y, ref, bound, dtype)
+
+
 # ---- buffers, streams, graphs -------------------------------------------------------
 
 def test_misaligned_buffers_are_refused():
