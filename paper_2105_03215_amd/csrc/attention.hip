@@ -326,6 +326,11 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   constexpr std::integral_constant<bool, false> keys{};
   constexpr std::integral_constant<bool, true> values{};
 
+  // LDS offsets of this lane's operands in a tile: its key row at chunk h, whose other chunks are an XOR away; and
+  // (fp32) column col of value rows 4 h and on, where v_key(r + 4 h) = v_key(r) ^ h
+  const uint32_t ka = col * RB + ((h ^ k_key<CPR>(col)) << 4);
+  const uint32_t va = 4 * h * RB + (((col >> 2) ^ h) << 4) + (col & 3) * 4;
+
   f32x16 o[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) o[d] = f32x16{};
@@ -342,7 +347,7 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
     f32x16 s{};
 #pragma unroll
     for (int st = 0; st < QS; ++st) {
-      const uint4 a = *(const uint4*)(kt + col * RB + (((2 * st + h) ^ k_key<CPR>(col)) * 16));
+      const uint4 a = *(const uint4*)(kt + (ka ^ (st % 8 << 5)) + st / 8 * 256);
       if constexpr (BF) {
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a), as_bf16x8(qf[st]), s, 0, 0, 0);
       } else {
@@ -386,11 +391,10 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
     } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int r = 8 * (i >> 2) + 4 * h + (i & 3);
+        const int r = 8 * (i >> 2) + (i & 3);  // (and 4 h)
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
-          const int c = d * 8 + (col >> 2);
-          const float vf = *(const float*)(vt + r * RB + ((c ^ v_key<CPR>(r)) * 16) + (col & 3) * 4);
+          const float vf = *(const float*)(vt + (va ^ ((v_key<CPR>(r) & 7) << 4)) + r * RB + ((d ^ (v_key<CPR>(r) >> 3)) * 128));
           o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[i], o[d], 0, 0, 0);
         }
       }
@@ -477,6 +481,34 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   }
 }
 
+// What a workgroup of `rows` packed rows works on.
+struct Place {
+  int b, kh, chunk, tile;  // b < 0: nothing
+  Chunks ck;
+};
+__device__ __forceinline__ Place place(const AttnParams& p, int rows) {
+  const int nh = p.chunks * p.kv_heads;
+  const int nt = (p.q_len * p.group + rows - 1) / rows;
+  Place w;
+  if (p.lengths && !p.causal && p.chunks == p.batch && p.batch <= 64) {
+    // sequences of different lengths: the longest first, all of its rows
+    const int per = p.kv_heads * nt, pos = blockIdx.x / per, rem = blockIdx.x - pos * per;
+    w.tile = rem / p.kv_heads;
+    w.kh = rem - w.tile * p.kv_heads;
+    w.b = w.chunk = uniform(nth_longest(p, pos));
+    w.ck = uniform_chunks(p, w.b);
+    return w;
+  }
+  // Head fastest: with a multiple of 8 heads each XCD (workgroup b runs on XCD b % 8) keeps to its own
+  // heads' keys and values; the last rows first, which see the most keys under a causal mask.
+  const int bh = blockIdx.x % nh;
+  w.tile = nt - 1 - blockIdx.x / nh;
+  w.chunk = bh / p.kv_heads;
+  w.kh = bh - w.chunk * p.kv_heads;
+  w.b = uniform(chunk_batch(p, w.chunk, &w.ck));
+  return w;
+}
+
 // Many rows, bf16: four waves of 32 packed rows each share tiles of 64 keys and
 // values, double-buffered in LDS; a tile's loads run while the one before is
 // multiplied, with one barrier a tile.  Two such workgroups fit a CU (D <= 128), so
@@ -501,27 +533,11 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int wave = uniform((tid >> 6) % NW), kg = uniform((tid >> 6) / NW);  // place among the rows; key group
   const int R = p.q_len * p.group;
-  const int nh = p.chunks * p.kv_heads;
-  const int nt = (R + 32 * NW - 1) / (32 * NW);
-  // Head fastest: with a multiple of 8 heads each XCD (workgroup b runs on XCD b % 8) keeps to its own
-  // heads' keys and values; the last rows first, which see the most keys under a causal mask.
-  const int bh = blockIdx.x % nh;
-  int tile = nt - 1 - blockIdx.x / nh;
-  int chunk = bh / p.kv_heads, kh = bh - chunk * p.kv_heads;
   const bool joined = p.chunks > p.batch;
-  Chunks ck;
-  int b;
-  if (p.lengths && !p.causal && !joined && p.batch <= 64) {
-    // sequences of different lengths: the longest first, all of its rows
-    const int per = p.kv_heads * nt, pos = blockIdx.x / per, rem = blockIdx.x - pos * per;
-    tile = rem / p.kv_heads;
-    kh = rem - tile * p.kv_heads;
-    b = chunk = uniform(nth_longest(p, pos));
-    ck = uniform_chunks(p, b);
-  } else {
-    b = uniform(chunk_batch(p, chunk, &ck));
-    if (b < 0) return;
-  }
+  const Place pl = place(p, 32 * NW);
+  const int b = pl.b, kh = pl.kh, chunk = pl.chunk, tile = pl.tile;
+  const Chunks ck = pl.ck;
+  if (b < 0) return;
   if (joined && tile == 0 && kh == 0) note_chunks(p, b, chunk, ck);
   const int len = uniform(batch_len(p, b));
   const int row0 = tile * 32 * NW + wave * 32, row = row0 + col;
@@ -790,6 +806,141 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
     }
 }
 
+// Many rows, fp32: four waves of 32 packed rows each share tiles of 32 keys and values, double-buffered in
+// LDS, a tile's loads running while the one before is multiplied; bound by the fp32 matrix cores (4096 cycles a
+// tile of 64 columns, beside which the softmax is short).  The key axes are not split: choose_attention
+// comes here where there are rows enough.
+template <int DP>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_kernel(AttnParams p) {
+  constexpr int NW = 4;
+  constexpr int RB = DP * 4, CPR = RB / 16;
+  constexpr int TILE = kKeys * RB;
+  constexpr int NI = TILE / (NW * 1024);  // loads of a tile per lane
+  constexpr int DB = DP / 32, QS = CPR / 2;
+  __shared__ __align__(1024) char lds[4 * TILE];  // keys, values, keys, values
+  static_assert(sizeof(lds) <= kLdsLimit, "LDS");
+
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
+  const int wave = uniform(tid >> 6);
+  const int R = p.q_len * p.group;
+  const Place pl = place(p, 32 * NW);
+  const int b = pl.b, kh = pl.kh, tile = pl.tile;
+  const int len = uniform(batch_len(p, b));
+  const int row0 = tile * 32 * NW + wave * 32, row = row0 + col;
+  const int lim = seen_keys(p, len, row);
+  const int lim_hi = uniform(row0 < R ? seen_keys(p, len, min(row0 + 32, R) - 1) : 0);  // (rows see more keys further down)
+  const int kend = uniform(seen_keys(p, len, min((tile + 1) * 32 * NW, R) - 1));
+  const int t_end = (kend + kKeys - 1) / kKeys;
+  const int t_wave = min(t_end, (lim_hi + kKeys - 1) / kKeys);  // tiles that this wave's rows see
+
+  uint4 qf[QS];
+  const int i = row / p.group, g = row - i * p.group;
+  {
+    const char* qp = (const char*)p.q + ((b * (int64_t)p.q_len + i) * p.ldq + (kh * p.group + g) * p.D) * 4;
+#pragma unroll
+    for (int st = 0; st < QS; ++st) {
+      const int c = 2 * st + h;
+      qf[st] = row < R && c * 4 < p.D ? *(const uint4*)(qp + c * 16) : make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+  const int64_t sk = p.ldk * 4, sv = p.ldv * 4;
+  const char* kb = (const char*)p.k + (int64_t)b * p.k_len * sk + kh * p.D * 4;
+  const char* vb = (const char*)p.v + (int64_t)b * p.k_len * sv + kh * p.D * 4;
+  const uint32_t lds0 = uniform(lds_addr(lds)) + wave * 1024;
+  // a tile of keys and values; rows past the length (and tiles past the end) read as zeros, whatever stands there
+  auto fill = [&](int par, int t) {
+    const int64_t k0 = (int64_t)t * kKeys;
+    const int n = t < t_end ? min(kKeys, len - t * kKeys) : 0;
+    const i32x4 rk = buffer_rsrc(kb + k0 * sk, n > 0 ? (n - 1) * (int)sk + p.D * 4 : 0);
+    const i32x4 rv = buffer_rsrc(vb + k0 * sv, n > 0 ? (n - 1) * (int)sv + p.D * 4 : 0);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int at = (j * NW + wave) * 64 + lane, r = at / CPR, x = at % CPR;
+      const int ck = x ^ k_key<CPR>(r), cv = x ^ v_key<CPR>(r);
+      lds_fill16(rk, lds0 + par * 2 * TILE + j * NW * 1024, ck * 4 < p.D ? (uint32_t)(r * (int)sk + ck * 16) : kOOB);
+      lds_fill16(rv, lds0 + (par * 2 + 1) * TILE + j * NW * 1024, cv * 4 < p.D ? (uint32_t)(r * (int)sv + cv * 16) : kOOB);
+    }
+  };
+
+  // LDS offsets of this lane's operands in a tile: its key row at chunk h, whose other chunks are an XOR away; and
+  // column col of value rows 4 h and on (v_key(r + 4 h) = v_key(r) ^ h)
+  static_assert(CPR >= 16, "swizzle keys of 4 bits");
+  const uint32_t ka = col * RB + ((h ^ k_key<CPR>(col)) << 4);
+  const uint32_t va = 4 * h * RB + (((col >> 2) ^ h) << 4) + (col & 3) * 4;
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d) o[d] = f32x16{};
+  float m = -INFINITY, l = 0.0f;
+  const float c2 = p.scale * 1.44269504088896340736f;
+  auto compute = [&](int par, int t) {
+    const char* kt = lds + par * 2 * TILE;
+    const char* vt = kt + TILE;
+    f32x16 s{};
+#pragma unroll
+    for (int st = 0; st < QS; ++st) {
+      const f32x4 a = *(const f32x4*)(kt + (ka ^ (st % 8 << 5)) + st / 8 * 256);
+      const f32x4 q = __builtin_bit_cast(f32x4, qf[st]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[e], s, 0, 0, 0);
+    }
+    const int k0 = t * kKeys + 4 * h;
+    float top = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = k0 + 8 * (e >> 2) + (e & 3) < lim ? s[e] * c2 : -INFINITY;
+      top = fmaxf(top, s[e]);
+    }
+    const float mn = fmaxf(m, half_max(top));
+    const float use = mn == -INFINITY ? 0.0f : mn;  // (no key seen yet: every weight is zero)
+    const float keep = exp2_(m - use);
+    m = mn;
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = exp2_(s[e] - use);
+      sum += s[e];
+    }
+    l = l * keep + sum;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] *= keep;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int r = 8 * (e >> 2) + (e & 3);  // (and 4 h)
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        const float vf = *(const float*)(vt + (va ^ ((v_key<CPR>(r) & 7) << 4)) + r * RB + ((d ^ (v_key<CPR>(r) >> 3)) * 128));
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, s[e], o[d], 0, 0, 0);
+      }
+    }
+  };
+
+  fill(0, 0);
+  for (int t = 0, par = 0; t < t_end; ++t, par ^= 1) {
+    // tile t has landed for every wave, and every wave is done with the one before, whose place t + 1 takes
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    fill(par ^ 1, t + 1);
+    if (t < t_wave) compute(par, t);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (p.causal && p.q_len > 1)
+    redo_not_finite<float, DB, QS>(p, kb, vb, sk, sv, lim, 0, t_end, 1, kKeys, qf, c2, o, m, l);
+  l = half_sum(l);
+  if (row >= R) return;
+  // (a row without keys is zero; one whose seen scores are all -inf divides zero by zero, as the softmax does)
+  float* const y = (float*)p.y + (b * (int64_t)p.q_len + i) * p.ldy + (kh * p.group + g) * p.D;
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int c = d * 32 + 8 * e + 4 * h;
+      float v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = lim > 0 ? o[d][4 * e + j] / l : 0.0f;
+      if (c < p.D) *(float4*)(y + c) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+}
+
 // Joins the chunks of a packed row: D / 4 lanes (of 64 / 32 / 16), 4 columns each, and `split` such groups a
 // row that take the chunks in turn, so that many chunks are on their way together where there are few rows
 // (one token over 32768 keys, 16 heads on one of 128, 16 rows of 85 chunks: 39 us by one group, 17 by eight).
@@ -881,19 +1032,25 @@ int row_blocks(const AttnParams& p) {
 
 }  // namespace
 
-// The kernel and the split.  The shared tiles take more than 32 packed rows (with fewer three
-// of their four waves would idle; fp32 products are bound by the matrix cores either way).
+// The kernel and the split.  bf16: the shared tiles take more than 32 packed rows (with fewer three of
+// their four waves would idle).  fp32 products are bound by the matrix cores either way: the shared
+// tiles where their workgroups of 128 rows fill the chip, or where the keys are too few for the
+// waves of the rows kernel (us, tiles and rows kernel: 11 x 1242 over 25 keys, 16 heads on one of 96,
+// 71, 292; 16 x 300 over 200, 12 of 128, 106, 134; 8 x 512 over 100, 8 of 32, 15.4, 19.7; but 8 x 512 over
+// 512, 12 of 64, 84, 77; 4 x 512 over 256, 8 of 128, 45, 36).
 void choose_attention(AttnParams& p) {
-  const bool tiled = !p.f32 && p.q_len * (int64_t)p.group > 32;
+  const int64_t rows = p.q_len * (int64_t)p.group;
+  const int64_t quads = (int64_t)p.batch * p.kv_heads * ceil_div(rows, 128);
+  const bool tiled = rows > 32 && (!p.f32 || quads >= (p.D <= 64 ? 512 : 256) || (p.k_len <= 4 * kKeys && quads >= 128));
   // Up to 64 columns a head, two waves along the rows and two along the keys where 128-row workgroups would
   // not fill the chip twice: causal 1 x 2048, 16 heads of 64: 30.5 us as 256 workgroups of 128 rows, 21.4 as
   // 512 of 64; 128 columns need the LDS of a CU for that and lose (1 x 1024, 32 over 8 of 128: 25.1, 29.1).
-  const bool halves = tiled && p.D <= 64 && (int64_t)p.batch * p.kv_heads * ceil_div((int64_t)p.q_len * p.group, 128) <= 320;
+  const bool halves = tiled && !p.f32 && p.D <= 64 && quads <= 320;
   p.tile_rows = tiled ? (halves ? 64 : 128) : kCols;
-  p.tile_keys = tiled ? kTileKeys : kKeys;
+  p.tile_keys = tiled && !p.f32 ? kTileKeys : kKeys;
   const int64_t blocks = (int64_t)p.batch * p.kv_heads * row_blocks(p);
   // Tiles: a split fills the two workgroups that a CU has room for where there is less than one.
-  int64_t slots = blocks >= 256 ? 0 : 512, per = ceil_div(p.k_len, 512);
+  int64_t slots = blocks >= 256 ? 0 : p.D > 128 ? 256 : 512, per = ceil_div(p.k_len, 512);
   if (!tiled) {
     // Rows: one workgroup has a CU to itself; three rounds of its waves in each at least, which take as
     // long as the join
@@ -905,7 +1062,8 @@ void choose_attention(AttnParams& p) {
 }
 
 const char* attention_name(const AttnParams& p) {
-  return p.f32 ? "attention_rows_f32" : p.tile_rows > kCols ? "attention_tiles" : "attention_rows";
+  if (p.tile_rows > kCols) return p.f32 ? "attention_tiles_f32" : "attention_tiles";
+  return p.f32 ? "attention_rows_f32" : "attention_rows";
 }
 
 int64_t attn_workspace(const AttnParams& p) {
@@ -917,7 +1075,11 @@ hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
   if (p.D < 8 || p.D > 256 || p.D % 8 != 0 || p.chunks < p.batch) return hipErrorInvalidValue;
   const int grid = p.chunks * p.kv_heads * row_blocks(p);
   if (p.tile_rows > kCols) {
-    if (p.tile_rows == 64) {
+    if (p.f32) {
+      if (p.D <= 64) attention_tiles_f32_kernel<64><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 128) attention_tiles_f32_kernel<128><<<grid, 256, 0, s>>>(p);
+      else attention_tiles_f32_kernel<256><<<grid, 256, 0, s>>>(p);
+    } else if (p.tile_rows == 64) {
       attention_tiles_kernel<64, 2><<<grid, 256, 0, s>>>(p);
     } else {
       if (p.D <= 64) attention_tiles_kernel<64, 1><<<grid, 256, 0, s>>>(p);

@@ -457,6 +457,22 @@ def test_attention_split_keys(batch, q_len, k_len, heads, kv, d, dtype, causal, 
     _close(y, ref, bound, dtype)
 
 
+@pytest.mark.parametrize("batch, q_len, k_len, heads, kv, d, causal, lengths", [
+    (130, 33, 1, 1, 1, 8, False, None),
+    (64, 40, 100, 2, 2, 64, True, [(29 * i) % 101 for i in range(64)]),  # (rows that see no key, tiles that end inside)
+    (16, 100, 128, 8, 8, 40, True, None),
+    (64, 130, 33, 1, 1, 64, False, [(5 * i) % 34 for i in range(64)]),
+    (32, 40, 140, 8, 8, 128, False, [140 - 4 * i for i in range(32)]),
+    (256, 36, 45, 1, 1, 256, True, None),
+    (8, 65, 330, 32, 32, 72, True, [330, 0, 1, 64, 65, 66, 200, 329]),
+    (43, 200, 35, 6, 1, 200, False, None),
+])
+def test_attention_f32_many_rows(batch, q_len, k_len, heads, kv, d, causal, lengths):
+    announce("attention f32 b %d q %d k %d heads %d/%d d %d" % (batch, q_len, k_len, heads, kv, d))
+    y, ref, bound = _attention(batch, q_len, k_len, heads, kv, d, "f32", causal, lengths, seed=9, spoil=lengths is not None)
+    _close(y, ref, bound, "f32")
+
+
 # ---- buffers, streams, graphs -------------------------------------------------------
 
 def test_misaligned_buffers_are_refused():
