@@ -257,7 +257,9 @@ __device__ __forceinline__ void redo_not_finite(const AttnParams& p, const char*
 // A workgroup takes 32 packed query rows of one (batch, key head) and a share of
 // its keys; its waves take tiles of 32 keys in turn, each through its own LDS
 // tiles, without a barrier until their results meet at the end.
-template <typename T, int DP, int NW>
+//
+// DP columns of a head in LDS (a power of two), DC of them multiplied.
+template <typename T, int DP, int DC, int NW>
 __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int ES = sizeof(T);
@@ -266,11 +268,11 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   constexpr int TILE = kKeys * RB;    // bytes of a tile
   constexpr int NBUF = BF ? 2 : 1;
   constexpr int NI = TILE / 1024;     // loads of a tile per lane
-  constexpr int DB = DP / 32;         // 32-column blocks of the output
+  constexpr int DB = DC / 32;         // 32-column blocks of the output
   __shared__ __align__(16) char lds[NW * NBUF * 2 * TILE];
   __shared__ float ml[NW][2][kCols];
   static_assert(sizeof(lds) + sizeof(ml) <= kLdsLimit, "LDS");
-  static_assert(NW * NBUF * 2 * TILE >= NW * DP * kPitch * 4, "the waves' results take the tiles' place");
+  static_assert(NW * NBUF * 2 * TILE >= NW * DC * kPitch * 4, "the waves' results take the tiles' place");
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int wave = uniform(tid >> 6);
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   const int ncb = (R + kCols - 1) / kCols;
   const int kh = blockIdx.x % p.kv_heads;
   const int rest = blockIdx.x / p.kv_heads;
-  const int cb = rest % ncb, chunk = rest / ncb;
+  const int cb = ncb - 1 - rest % ncb, chunk = rest / ncb;  // (the last rows, which see the most keys, first)
   const bool joined = p.chunks > p.batch;
   Chunks ck;
   const int b = uniform(chunk_batch(p, chunk, &ck));
@@ -292,7 +294,7 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   const int t_end = min(t0 + ck.size, (kend + kKeys - 1) / kKeys);
 
   // this lane's part of its query row: 16-byte chunks 2 st + h
-  constexpr int QS = CPR / 2;
+  constexpr int QS = DC * ES / 32;
   uint4 qf[QS];
   {
     const int i = row / p.group, g = row - i * p.group;
@@ -434,7 +436,7 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) os[(wave * DP + d * 32 + 8 * (i >> 2) + 4 * h + (i & 3)) * kPitch + col] = o[d][i] * f;
+    for (int i = 0; i < 16; ++i) os[(wave * DC + d * 32 + 8 * (i >> 2) + 4 * h + (i & 3)) * kPitch + col] = o[d][i] * f;
   float total = 0.0f;
 #pragma unroll
   for (int w = 0; w < NW; ++w) total += ml[w][1][col] * exp2_(ml[w][0][col] - use);
@@ -452,15 +454,15 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   if (!joined) __syncthreads();
   // thread = 4 columns of a packed row, rows in turn
   const int rows = min(kCols, R - cb * kCols);
-  for (int at = tid; at < rows * (DP / 4); at += 64 * NW) {
-    const int c = at / (DP / 4), e = at % (DP / 4) * 4;
+  for (int at = tid; at < rows * (DC / 4); at += 64 * NW) {
+    const int c = at / (DC / 4), e = at % (DC / 4) * 4;
     if (e >= p.D) continue;
     float v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       v[j] = os[(e + j) * kPitch + c];
 #pragma unroll
-      for (int w = 1; w < NW; ++w) v[j] += os[(w * DP + e + j) * kPitch + c];
+      for (int w = 1; w < NW; ++w) v[j] += os[(w * DC + e + j) * kPitch + c];
     }
     const int r = cb * kCols + c;
     if (joined) {
@@ -520,13 +522,17 @@ __device__ __forceinline__ Place place(const AttnParams& p, int rows) {
 constexpr int kTileKeys = 64;
 constexpr float kSlack = 8.0f;
 
-template <int DP, int KS>
+//
+// DP columns of a head in LDS (a power of two), DC of them multiplied (causal 2 x 2048, 20 heads over 4 of 80:
+// 48.7 us with all 128, 43.2 with 96).
+template <int DP, int DC, int KS>
 __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_kernel(AttnParams p) {
   constexpr int NW = 4 / KS;  // waves along the rows
   constexpr int RB = DP * 2, CPR = RB / 16;
   constexpr int TILE = kTileKeys * RB;
   constexpr int NI = TILE / (NW * 1024);  // loads of a tile per lane
-  constexpr int DB = DP / 32, QS = CPR / 2, KB = kTileKeys / 32;
+  constexpr int DB = DC / 32, QS = DC / 16, KB = kTileKeys / 32;
+  static_assert(DC % 32 == 0 && DC <= DP, "columns multiplied");
   __shared__ __align__(1024) char lds[KS * 4 * TILE];
   static_assert(sizeof(lds) <= kLdsLimit, "LDS");
 
@@ -685,23 +691,21 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
     float sums[2] = {0.0f, 0.0f};
     uint4 pf[2 * KB];
     VFrag vf[2];
-    constexpr int SL = 16 * KB / QS;  // weights of a slice
     static_for<0, QS>([&](auto st) {
       constexpr int i = decltype(st)::value;
+      constexpr int from = 16 * KB * i / QS, to = 16 * KB * (i + 1) / QS;  // weights of a slice
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (i + 2 < QS) kf[(i + 2) % 3] = read_k(other, std::integral_constant<int, i + 2>{});
       if constexpr (i == QS - 1) vf[0] = read_v(par_tag, c0);
       mul_k(kf[i % 3], st, next);
 #pragma unroll
-      for (int e = i * SL; e < (i + 1) * SL; ++e) {
+      for (int e = from; e < to; ++e) {
         const float w = exp2_(__builtin_fmaf(s[e >> 4][e & 15], c2, -use));
         s[e >> 4][e & 15] = w;
         sums[e & 1] += w;
       }
-      if constexpr ((i + 1) * SL % 8 == 0) {
 #pragma unroll
-        for (int ks = i * SL / 8; ks < (i + 1) * SL / 8; ++ks) pf[ks] = pack_weights(s[ks >> 1], ks & 1);
-      }
+      for (int ks = from / 8; ks < to / 8; ++ks) pf[ks] = pack_weights(s[ks >> 1], ks & 1);
     });
     l += sums[0] + sums[1];
     static_for<0, 2 * KB>([&](auto ks) {
@@ -810,13 +814,13 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
 // LDS, a tile's loads running while the one before is multiplied; bound by the fp32 matrix cores (4096 cycles a
 // tile of 64 columns, beside which the softmax is short).  The key axes are not split: choose_attention
 // comes here where there are rows enough.
-template <int DP>
+template <int DP, int DC>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_kernel(AttnParams p) {
   constexpr int NW = 4;
   constexpr int RB = DP * 4, CPR = RB / 16;
   constexpr int TILE = kKeys * RB;
   constexpr int NI = TILE / (NW * 1024);  // loads of a tile per lane
-  constexpr int DB = DP / 32, QS = CPR / 2;
+  constexpr int DB = DC / 32, QS = DC / 8;
   __shared__ __align__(1024) char lds[4 * TILE];  // keys, values, keys, values
   static_assert(sizeof(lds) <= kLdsLimit, "LDS");
 
@@ -1035,8 +1039,8 @@ int row_blocks(const AttnParams& p) {
 // The kernel and the split.  bf16: the shared tiles take more than 32 packed rows (with fewer three of
 // their four waves would idle).  fp32 products are bound by the matrix cores either way: the shared
 // tiles where their workgroups of 128 rows fill the chip, or where the keys are too few for the
-// waves of the rows kernel (us, tiles and rows kernel: 11 x 1242 over 25 keys, 16 heads on one of 96,
-// 71, 292; 16 x 300 over 200, 12 of 128, 106, 134; 8 x 512 over 100, 8 of 32, 15.4, 19.7; but 8 x 512 over
+// waves of the rows kernel (us, tiles and rows kernel: 16 x 600 over 60 keys, 16 heads on one of 128,
+// 72, 218; 16 x 300 over 200, 12 of 128, 106, 134; 16 x 100 over 100, 12 of 64, 16, 20; but 8 x 512 over
 // 512, 12 of 64, 84, 77; 4 x 512 over 256, 8 of 128, 45, 36).
 void choose_attention(AttnParams& p) {
   const int64_t rows = p.q_len * (int64_t)p.group;
@@ -1076,26 +1080,36 @@ hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
   const int grid = p.chunks * p.kv_heads * row_blocks(p);
   if (p.tile_rows > kCols) {
     if (p.f32) {
-      if (p.D <= 64) attention_tiles_f32_kernel<64><<<grid, 256, 0, s>>>(p);
-      else if (p.D <= 128) attention_tiles_f32_kernel<128><<<grid, 256, 0, s>>>(p);
-      else attention_tiles_f32_kernel<256><<<grid, 256, 0, s>>>(p);
+      if (p.D <= 32) attention_tiles_f32_kernel<64, 32><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 64) attention_tiles_f32_kernel<64, 64><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 96) attention_tiles_f32_kernel<128, 96><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 128) attention_tiles_f32_kernel<128, 128><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 192) attention_tiles_f32_kernel<256, 192><<<grid, 256, 0, s>>>(p);
+      else attention_tiles_f32_kernel<256, 256><<<grid, 256, 0, s>>>(p);
     } else if (p.tile_rows == 64) {
-      attention_tiles_kernel<64, 2><<<grid, 256, 0, s>>>(p);
+      if (p.D <= 32) attention_tiles_kernel<64, 32, 2><<<grid, 256, 0, s>>>(p);
+      else attention_tiles_kernel<64, 64, 2><<<grid, 256, 0, s>>>(p);
     } else {
-      if (p.D <= 64) attention_tiles_kernel<64, 1><<<grid, 256, 0, s>>>(p);
-      else if (p.D <= 128) attention_tiles_kernel<128, 1><<<grid, 256, 0, s>>>(p);
-      else attention_tiles_kernel<256, 1><<<grid, 256, 0, s>>>(p);
+      if (p.D <= 32) attention_tiles_kernel<64, 32, 1><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 64) attention_tiles_kernel<64, 64, 1><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 96) attention_tiles_kernel<128, 96, 1><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 128) attention_tiles_kernel<128, 128, 1><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 192) attention_tiles_kernel<256, 192, 1><<<grid, 256, 0, s>>>(p);
+      else attention_tiles_kernel<256, 256, 1><<<grid, 256, 0, s>>>(p);
     }
     return hipGetLastError();
   }
   if (p.f32) {
-    if (p.D <= 64) attention_rows_kernel<float, 64, 4><<<grid, 256, 0, s>>>(p);
-    else if (p.D <= 128) attention_rows_kernel<float, 128, 4><<<grid, 256, 0, s>>>(p);
-    else attention_rows_kernel<float, 256, 2><<<grid, 128, 0, s>>>(p);
+    if (p.D <= 32) attention_rows_kernel<float, 64, 32, 4><<<grid, 256, 0, s>>>(p);
+    else if (p.D <= 64) attention_rows_kernel<float, 64, 64, 4><<<grid, 256, 0, s>>>(p);
+    else if (p.D <= 96) attention_rows_kernel<float, 128, 96, 4><<<grid, 256, 0, s>>>(p);
+    else if (p.D <= 128) attention_rows_kernel<float, 128, 128, 4><<<grid, 256, 0, s>>>(p);
+    else if (p.D <= 192) attention_rows_kernel<float, 256, 192, 2><<<grid, 128, 0, s>>>(p);
+    else attention_rows_kernel<float, 256, 256, 2><<<grid, 128, 0, s>>>(p);
   } else {
-    if (p.D <= 64) attention_rows_kernel<bf16_t, 64, 8><<<grid, 512, 0, s>>>(p);
-    else if (p.D <= 128) attention_rows_kernel<bf16_t, 128, 4><<<grid, 256, 0, s>>>(p);
-    else attention_rows_kernel<bf16_t, 256, 2><<<grid, 128, 0, s>>>(p);
+    if (p.D <= 64) attention_rows_kernel<bf16_t, 64, 64, 8><<<grid, 512, 0, s>>>(p);
+    else if (p.D <= 128) attention_rows_kernel<bf16_t, 128, 128, 4><<<grid, 256, 0, s>>>(p);
+    else attention_rows_kernel<bf16_t, 256, 256, 2><<<grid, 128, 0, s>>>(p);
   }
   return hipGetLastError();
 }

@@ -473,6 +473,15 @@ def test_attention_f32_many_rows(batch, q_len, k_len, heads, kv, d, causal, leng
     _close(y, ref, bound, "f32")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [8, 32, 40, 72, 88, 96, 104, 136, 192, 200])
+def test_attention_head_sizes(d, dtype):
+    """Heads that end inside the columns that are multiplied, for few rows and for many, masked and not."""
+    for q_len, causal in ((1, False), (45, True), (150, False)):
+        y, ref, bound = _attention(2, q_len, 170, 2, 1, d, dtype, causal, [170, 133], seed=d, spoil=True)
+        _close(y, ref, bound, dtype)
+
+
 # ---- buffers, streams, graphs -------------------------------------------------------
 
 def test_misaligned_buffers_are_refused():
