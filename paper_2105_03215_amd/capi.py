@@ -143,14 +143,6 @@ def validate(graph, consts):
     _check(lib.byoc_subgraph_validate(js, len(js), cs.c, cs.n))
 
 
-def _ptr(t):
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return t
-    return t.data_ptr()
-
-
 _ELEM_DTYPE = {"bf16": "torch.bfloat16", "f32": "torch.float32", "i32": "torch.int32"}
 
 
@@ -197,7 +189,7 @@ class Subgraph:
         # host time, more than a small subgraph's kernel
         self._counts = tuple([int(np.prod(d["shape"])) if d["shape"] else 1 for d in ds] for ds in self._descs)
         self._ptrs = (ctypes.c_void_p * max(self.n_in, 1), ctypes.c_void_p * max(self.n_out, 1))
-        self._torch = None  # (dtypes by desc, device, current raw stream), on the first run
+        self._torch = None  # (dtypes by desc, device number, current raw stream), on the first run
 
     def io_desc(self, is_output, idx):
         d = TensorDesc()
@@ -230,25 +222,26 @@ class Subgraph:
         if len(inputs) != self.n_in or len(outputs) != self.n_out:
             raise ByocError(1, "expected %d inputs and %d outputs, got %d and %d"
                             % (self.n_in, self.n_out, len(inputs), len(outputs)))
-        io = self._torch
-        for side, ts in enumerate((inputs, outputs)):
-            for i, t in enumerate(ts):
-                if t is None or isinstance(t, int):
-                    continue
-                if io is None:
-                    io = self._torch_io()
-                if not (t.dtype is io[0][side][i] and t.numel() == self._counts[side][i] and t.device == io[1]
-                        and t.is_contiguous()):
-                    _check_tensor(t, self._descs[side][i], self.device, "%s %d" % (("input", "output")[side], i))
-        ins = self._ptrs[0](*[_ptr(t) for t in inputs])
-        outs = self._ptrs[1](*[_ptr(t) for t in outputs])
+        ins, outs = self._pointers(0, inputs), self._pointers(1, outputs)
         if stream is None:
-            s = (io or self._torch_io())[2](self.device)
+            s = (self._torch or self._torch_io())[2](self.device)
         elif isinstance(stream, int):
             s = stream
         else:
             s = stream.cuda_stream
-        return ins, outs, ctypes.c_void_p(s)
+        return ins, outs, s
+
+    def _pointers(self, side, ts):
+        ptrs = []
+        for i, t in enumerate(ts):
+            if t is not None and not isinstance(t, int):
+                dtypes, index, _ = self._torch or self._torch_io()
+                if not (t.dtype is dtypes[side][i] and t.numel() == self._counts[side][i] and t.get_device() == index
+                        and t.is_contiguous()):
+                    _check_tensor(t, self._descs[side][i], self.device, "%s %d" % (("input", "output")[side], i))
+                t = t.data_ptr()
+            ptrs.append(t)
+        return self._ptrs[side](*ptrs)
 
     def _torch_io(self):
         import torch
@@ -258,7 +251,7 @@ class Subgraph:
             def raw(device):
                 return torch.cuda.current_stream(device).cuda_stream
         self._torch = (tuple([kinds[d["dtype"]] for d in ds] for ds in self._descs),
-                       torch.device("cuda", int(self.device)), raw)
+                       int(self.device), raw)
         return self._torch
 
     def run(self, inputs, outputs, stream=None):
