@@ -17,6 +17,7 @@
 // O^T = V^T P^T: register group i of a lane half h holds keys 8 (i / 4) + 4 h + i % 4,
 // and V^T is read in the same order (the order of a sum over keys is free).
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "lds_dma.h"
@@ -1040,6 +1041,25 @@ int row_blocks(const AttnParams& p) {
 
 }  // namespace
 
+// Chunks of each sequence for the tiles kernel on `blocks` workgroups a chunk: the number of least modelled time (us), of
+// the tiles of 64 keys that a workgroup takes one after another, slower where two share a CU, and of the results' way
+// through memory to the join.  Measured, whole and in the chunks of this rule: 1 x 1024 over 1024, 12 heads of 64, 11.4 as
+// both (18.8 in two chunks); 1 x 1024 over 4096, 8 of 128, 68 and 38; 4 x 40 over 8192, 8 of 64, 54 and 20.
+int split_tiles(const AttnParams& p, int64_t blocks) {
+  const double tile = p.D <= 64 ? 0.4 : p.D <= 96 ? 0.93 : p.D <= 128 ? 1.03 : p.D <= 192 ? 2.1 : 2.65;
+  const double shared = p.D <= 64 ? 1.0 : 0.4;  // (the vector ALU, which bounds 64 columns, is full with one)
+  const double tiles = ceil_div(p.k_len, kTileKeys);
+  const double part = 8e-6 / 4.1 * p.D * p.batch * p.kv_heads * p.q_len * p.group;  // a chunk's sums, written and read
+  int best = 1;
+  double least = INFINITY;
+  const int64_t most = std::min<int64_t>((p.D > 128 ? 256 : 512) / blocks, ceil_div(p.k_len, 4 * kTileKeys));
+  for (int n = 1; n <= most; ++n) {
+    const double t = tiles / n * tile * (1.0 + shared * std::max(0.0, blocks * n / 256.0 - 1.0)) + (n > 1 ? 6.0 + part * n : 0.0);
+    if (t < least) least = t, best = n;
+  }
+  return best;
+}
+
 // The kernel and the split.  bf16: the shared tiles take more than 32 packed rows (with fewer three of
 // their four waves would idle).  fp32 products are bound by the matrix cores either way: the shared
 // tiles where their workgroups of 128 rows fill the chip, or where the keys are too few for the
@@ -1057,15 +1077,15 @@ void choose_attention(AttnParams& p) {
   p.tile_rows = tiled ? (halves ? 64 : 128) : kCols;
   p.tile_keys = tiled && !p.f32 ? kTileKeys : kKeys;
   const int64_t blocks = (int64_t)p.batch * p.kv_heads * row_blocks(p);
-  // Tiles: a split fills the two workgroups that a CU has room for where there is less than one.
-  int64_t slots = blocks >= 256 ? 0 : p.D > 128 ? 256 : 512, per = ceil_div(p.k_len, 512);
+  int64_t chunks = p.batch;
   if (!tiled) {
     // Rows: one workgroup has a CU to itself; three rounds of its waves in each at least, which take as
     // long as the join
-    slots = 256;
-    per = ceil_div(p.k_len, kKeys * row_waves(p)) / 3;
+    chunks = std::min<int64_t>(256 / std::max<int64_t>(1, blocks / p.batch),
+                               p.batch * (ceil_div(p.k_len, kKeys * row_waves(p)) / 3));
+  } else if (blocks < 256) {
+    chunks = p.batch * split_tiles(p, blocks);
   }
-  const int64_t chunks = std::min<int64_t>(slots / std::max<int64_t>(1, blocks / p.batch), p.batch * per);
   p.chunks = chunks < 2 * (int64_t)p.batch ? p.batch : (int)(p.batch > 64 ? chunks / p.batch * p.batch : chunks);
 }
 
