@@ -445,6 +445,9 @@ ATTENTION_SPLIT = [
     (12, 1, 2000, 2, 2, 128, "bf16", False, [2000, 1, 0, 999, 1024, 1025, 31, 33, 0, 1999, 500, 1700]),
     (64, 1, 800, 1, 1, 64, "bf16", False, [(37 * i) % 801 for i in range(64)]),
     (70, 1, 500, 1, 1, 32, "bf16", False, [(61 * i) % 501 for i in range(70)]),
+    (70, 1, 1700, 1, 1, 64, "bf16", False, [(211 * i) % 1701 for i in range(70)]),
+    (67, 33, 4100, 1, 1, 32, "bf16", False, [(611 * i) % 4101 for i in range(67)]),
+    (33, 34, 4100, 1, 1, 64, "bf16", False, [(711 * i) % 4101 for i in range(33)]),
     (3, 50, 3000, 2, 2, 64, "bf16", True, None),
     (2, 45, 2600, 1, 1, 128, "bf16", True, [2600, 40]),
 ]
