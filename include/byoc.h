@@ -25,7 +25,8 @@
  *
  * Serialized format (schema "byoc-subgraph", version 1), a JSON object:
  *   "inputs":    [{"name", "shape", "dtype": "f32"|"bf16", "layout": "NCHW"|"ROWMAJOR"}]
- *                or {"name", "shape": [n], "dtype": "i32"}: positions or lengths
+ *                or {"name", "shape": [n], "dtype": "i32"}: positions or lengths,
+ *                in bf16 and f32 graphs
  *   "constants": [{"name", "index", "shape", "dtype"}]   index into the
  *                constant array passed to create; conv weights OIHW, dense
  *                weights [out, in], biases [out]

@@ -729,6 +729,8 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
     const Value& v = g.values[in.value];
     if (g.compute != DType::I8 && v.has_q)
       return uerr("input " + v.name + ": quant parameters only in int8 graphs");
+    if (g.compute == DType::I8 && v.dtype == DType::I32)  // (no int8 composite reads one)
+      return uerr("input " + v.name + ": i32 inputs only in bf16 and f32 graphs");
   }
 
   // ---- outputs -------------------------------------------------------------
