@@ -59,6 +59,11 @@ __device__ __forceinline__ void angles(const RotaryParams& p, int row0, int rows
   __syncthreads();
 }
 
+// Heads with values above 2^59 or so, whose squares leave float32, are normed at 2^-70 of their size (an
+// infinity or a NaN stays one); these are the only ones that cost more than a comparison.
+constexpr float kTooLarge = 0x1p-70f;
+__device__ __forceinline__ float inv_rms(float sum, int D, float eps) { return 1.0f / sqrtf(sum / (float)D + eps); }
+
 // 8 columns as they are stored.
 template <typename T>
 struct Raw;
@@ -195,13 +200,25 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p, int RB
     for (int u = 0; u < U; ++u) {
       float inv = 1.0f;
       if constexpr (NORM) {
-        float sum = 0.0f;
+        auto squares = [&] {
+          float sum = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(f[u][e], f[u][e], sum);
-        sum = live ? sum : 0.0f;
+          for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(f[u][e], f[u][e], sum);
+          sum = live ? sum : 0.0f;
 #pragma unroll
-        for (int d = LH / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-        inv = 1.0f / sqrtf(sum / (float)p.D + p.eps);
+          for (int d = LH / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+          return sum;
+        };
+        const float sum = squares();
+        inv = inv_rms(sum, p.D, p.eps);
+        if (!(sum < INFINITY)) {  // (the same in all lanes of a head)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            f[u][e] *= kTooLarge;
+            if constexpr (!INTER) q[u][e] *= kTooLarge;
+          }
+          inv = inv_rms(squares(), p.D, p.eps * (kTooLarge * kTooLarge));
+        }
       }
       if (it + u * SLOTS >= items || !live) continue;
       T* const out = y0 + (int64_t)fr[u] * p.ldy + fh[u] * p.D + e0;
@@ -241,26 +258,34 @@ __global__ __launch_bounds__(kThreads) void rotary_any_kernel(RotaryParams p, in
     const int r = it / nh, h = h0 + it - r * nh;
     const T* x = (const T*)p.x + (int64_t)(row0 + r) * p.ldx + (int64_t)h * p.D;
     T* y = (T*)p.y + (int64_t)(row0 + r) * p.ldy + (int64_t)h * p.D;
-    float inv = 1.0f;
+    float inv = 1.0f, size = 1.0f;
     if (p.wq) {
-      float sum = 0.0f;
-      for (int e = lane; e < p.D; e += 64) {
-        const float v = load1(x + e);
-        sum = __builtin_fmaf(v, v, sum);
-      }
+      auto squares = [&] {
+        float sum = 0.0f;
+        for (int e = lane; e < p.D; e += 64) {
+          const float v = load1(x + e) * size;
+          sum = __builtin_fmaf(v, v, sum);
+        }
 #pragma unroll
-      for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-      inv = 1.0f / sqrtf(sum / (float)p.D + p.eps);
+        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+        return sum;
+      };
+      const float sum = squares();
+      inv = inv_rms(sum, p.D, p.eps);
+      if (!(sum < INFINITY)) {
+        size = kTooLarge;
+        inv = inv_rms(squares(), p.D, p.eps * (kTooLarge * kTooLarge));
+      }
     }
     const float* w = h >= p.heads ? p.wk : p.wq;
     for (int e = lane; e < p.D; e += 64) {
-      float v = load1(x + e);
+      float v = load1(x + e) * size;
       if (p.wq) v *= inv * w[e];
       if (e < p.rd) {
         const bool second = p.interleaved ? e & 1 : e >= half;
         const int pair = p.interleaved ? e >> 1 : (second ? e - half : e);
         const int pe = p.interleaved ? e ^ 1 : (second ? e - half : e + half);
-        float o = load1(x + pe);
+        float o = load1(x + pe) * size;
         if (p.wq) o *= inv * w[pe];
         const float2 t = cs[r * half + pair];
         v = v * t.x + (second ? o : -o) * t.y;

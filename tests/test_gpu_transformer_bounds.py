@@ -1,0 +1,51 @@
+"""The transformer-layer composites at the edges of their ranges: magnitudes near the ends of float32, infinities
+and NaN without a loss of speed, every product tile, and what a plan shares, pads and overlaps.
+
+Rounding bounds as in test_gpu_transformer (u = 2^-8, e = 2^-24), and: an angle in turns is off by 2^-24 where a
+position is near 2^31 (53 bits of turns per position times 31 of position) and by 2^-26 from its rounding to float32.
+"""
+
+import decimal
+
+import numpy as np
+import pytest
+
+import oracle
+from oracle import transformer as T
+from paper_2105_03215_amd import workloads
+from paper_2105_03215_amd.workloads import to_bf16_values
+from parity_util import announce, bf16_ulp
+from test_gpu_transformer import DEV, E, U, _close, _engine, _layer, _normal, _run
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- rotary --------------------------------------------------------------------
+
+@pytest.mark.parametrize("heads, kv, d, rd, layout, dtype", [
+    (2, 1, 128, 128, "half", "bf16"),
+    (2, 1, 128, 128, "half", "f32"),
+    (1, 0, 64, 64, "interleaved", "bf16"),
+    (3, 1, 80, 40, "half", "bf16"),
+    (2, 2, 6, 4, "half", "bf16"),
+    (1, 1, 512, 510, "interleaved", "f32"),
+])
+def test_norm_of_large_heads(heads, kv, d, rd, layout, dtype):
+    """Heads whose squares leave float32 have a norm all the same; one that holds an infinity has none, and its other
+    columns are zero, as a number over infinity is."""
+    announce("norm of large heads %d+%d d %d rd %d %s %s" % (heads, kv, d, rd, layout, dtype))
+    r = np.random.default_rng(d + rd)
+    powers = [0, 40, 58, 60, 62, 64, 66, 90, 124]
+    x = _normal(r, len(powers) + 2, (heads + kv) * d)
+    x[:len(powers)] = to_bf16_values((x[:len(powers)] * np.exp2(np.array(powers))[:, None]).astype(np.float32))
+    x[-2, 1] = 2.0 ** 126       # one value above the others of its head
+    x[-1, 0] = np.inf
+    pos = np.arange(len(x)).astype(np.int32)
+    attrs = {"heads": heads, "kv_heads": kv, "head_dim": d, "rotary_dim": rd, "layout": layout}
+    ws = [(n, (1 + r.normal(size=d) * 0.2).astype(np.float32)) for n in ("wq", "wk")[:2 if kv else 1]]
+    y = _run("qk_norm_rotary", {"x": x, "p": pos}, ["x"] + [n for n, _ in ws] + ["p"], attrs, dtype, ws)
+    with np.errstate(invalid="ignore"):
+        ref = T.rotary(attrs, x, pos, [w for _, w in ws])
+    # a normed value is sqrt(D) at most, and a pair is two (weights below 2)
+    _close(y, ref, np.full_like(ref, (2.0 ** -20 * 1.5 + (d / 8 + 8) * E) * 4 * d ** 0.5), dtype)
+    assert (np.abs(ref[:len(powers)]).max(axis=1) > 0.5).all()
