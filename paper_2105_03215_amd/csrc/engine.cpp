@@ -8,6 +8,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <limits>
 
 namespace byoc {
 namespace {
@@ -1317,7 +1318,7 @@ void Planner::plan_rotary(int ni) {
   p.heads = n.heads, p.kv_heads = n.kv_heads, p.D = n.head_dim, p.rd = n.rotary_dim;
   p.interleaved = n.interleaved;
   p.mag = (float)n.mag;
-  p.eps = (float)n.eps;
+  p.eps = std::max((float)n.eps, std::numeric_limits<float>::min());  // (positive in float32 too: a head of zeros is zero)
   p.f32 = !bf16;
   std::vector<uint8_t> turns(n.theta.size() * sizeof(double));
   for (size_t i = 0; i < n.theta.size(); ++i) {

@@ -49,3 +49,15 @@ def test_norm_of_large_heads(heads, kv, d, rd, layout, dtype):
     # a normed value is sqrt(D) at most, and a pair is two (weights below 2)
     _close(y, ref, np.full_like(ref, (2.0 ** -20 * 1.5 + (d / 8 + 8) * E) * 4 * d ** 0.5), dtype)
     assert (np.abs(ref[:len(powers)]).max(axis=1) > 0.5).all()
+
+
+@pytest.mark.parametrize("d, dtype", [(64, "bf16"), (10, "bf16"), (64, "f32")])
+def test_norm_of_zeros_with_the_smallest_eps(d, dtype):
+    """A head of zeros is zero for every positive eps, also one below float32."""
+    x = _normal(np.random.default_rng(2), 5, 2 * d)
+    x[1], x[3, d:] = 0, 0
+    w = np.ones(d, np.float32)
+    attrs = {"heads": 2, "head_dim": d, "eps": 1e-60}
+    y = _run("qk_norm_rotary", {"x": x, "p": np.arange(5, dtype=np.int32)}, ["x", "w", "p"], attrs, dtype, [("w", w)])
+    ref = T.rotary(attrs, x, np.arange(5), [w])
+    _close(y, ref, np.full_like(ref, (2.0 ** -20 * 1.5 + (d / 8 + 8) * E) * 4 * d ** 0.5), dtype)
