@@ -239,14 +239,16 @@ __device__ __forceinline__ Chunk<F32> load_res(const QDenseParams& p, int64_t m,
   return r;
 }
 
-// Eight columns of one output row: y = act(acc * scale + bias + res).
+// Eight columns of one output row: y = act(acc * scale + bias + res).  The sum meets the
+// channel's scale first: the product of the two scales alone may leave float32 where the result
+// does not (rows of 2^-64 under weights of 2^-64: the product of the scales has 7 bits left).
 template <bool F32, int MODE>
 __device__ __forceinline__ void finish8(const QDenseParams& p, const int* acc, float xs, const float* ws,
                                         const float* bias, const Chunk<F32>& res, int64_t m, int n, ActClamp ac) {
   float r[8], v[8];
   res.get(r);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = act_nan<F32, MODE>(__builtin_fmaf((float)acc[e], xs * ws[e], bias[e]) + r[e], ac);
+  for (int e = 0; e < 8; ++e) v[e] = act_nan<F32, MODE>(__builtin_fmaf((float)acc[e] * ws[e], xs, bias[e]) + r[e], ac);
   if constexpr (F32) {
     float* y = (float*)p.y + m * p.ldy + n;
     if (n + 8 <= p.N) {

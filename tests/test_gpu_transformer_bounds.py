@@ -61,3 +61,25 @@ def test_norm_of_zeros_with_the_smallest_eps(d, dtype):
     y = _run("qk_norm_rotary", {"x": x, "p": np.arange(5, dtype=np.int32)}, ["x", "w", "p"], attrs, dtype, [("w", w)])
     ref = T.rotary(attrs, x, np.arange(5), [w])
     _close(y, ref, np.full_like(ref, (2.0 ** -20 * 1.5 + (d / 8 + 8) * E) * 4 * d ** 0.5), dtype)
+
+
+# ---- qdense ----------------------------------------------------------------------
+
+@pytest.mark.parametrize("m", [1, 9, 70])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_qdense_scales_whose_product_leaves_float32(m, dtype):
+    """Sums times scales that are numbers, though the product of the two scales is below the normal range or above all
+    of it."""
+    r = np.random.default_rng(21)
+    k, n = 8192, 40
+    x, w = np.abs(_normal(r, m, k, std=2.0 ** -66)), np.abs(_normal(r, n, k, std=2.0 ** -66))
+    y = _run("qdense", {"x": x}, ["x", "w"], {}, dtype, [("w", w)])
+    ref = T.qdense(x, w)
+    assert np.abs(ref).min() > 2.0 ** -122  # (a_m / 127) (b_n / 127) is about 2^-142
+    _close(y, ref, 8 * E * np.abs(ref), dtype)
+    # a sum of zero between rows whose scales multiply to more than float32 holds
+    x, w = np.full((m, 2), 2.0 ** 110, np.float32), np.full((n, 2), 2.0 ** 40, np.float32)
+    x[:, 1] *= -1
+    b = r.normal(size=n).astype(np.float32)
+    y = _run("qdense_bias", {"x": x}, ["x", "w", "b"], {}, dtype, [("w", w), ("b", b)])
+    _close(y, np.broadcast_to(b, (m, n)).astype(np.float64), np.full((m, n), 4 * E), dtype)
