@@ -1297,8 +1297,10 @@ void Planner::plan_qdense(int ni) {
   p.alpha = n.alpha;
   p.f32 = !bf16;
   L.qt = choose_qdense_tile(p.M, p.N, Kq);
+  // BYOC_QDENSE_TILE=<id>: that tile wherever a tile is chosen (tests run every one with it)
+  if (const char* ev = std::getenv("BYOC_QDENSE_TILE"); ev && L.qt.id != kQDenseRows) (void)qdense_tile_of(std::atoi(ev), &L.qt);
   if (L.qt.id == kQDenseRows) std::snprintf(L.info.name, sizeof(L.info.name), "qdense_rows_m%d%s", M, fused ? "_fused" : "");
-  else std::snprintf(L.info.name, sizeof(L.info.name), "qdense_%dx%d", L.qt.bm, L.qt.bn);
+  else std::snprintf(L.info.name, sizeof(L.info.name), "qdense_%dx%d_s%d", L.qt.bm, L.qt.bn, L.qt.stages);
   e->launches.push_back(L);
 }
 

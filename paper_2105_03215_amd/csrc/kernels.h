@@ -475,9 +475,10 @@ struct QDenseParams {
 };
 constexpr int kQDenseRows = -1;  // QDenseTile::id of the kernel of few rows
 struct QDenseTile {
-  int id, bm, bn;
+  int id, bm, bn, stages;
 };
 QDenseTile choose_qdense_tile(int64_t M, int64_t N, int64_t Kq);
+bool qdense_tile_of(int id, QDenseTile* t);  // false: no such tile
 // Few enough rows for the product's workgroups to quantize them for themselves (q: the rows; p.x and p.xs unused).
 bool qdense_fuses_rows(int64_t M, int64_t N, int64_t Kq);
 hipError_t launch_qdense_fused(const QDenseParams& p, const QRowsParams& q, hipStream_t s);

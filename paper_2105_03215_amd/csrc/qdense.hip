@@ -676,14 +676,22 @@ hipError_t launch_qdense_fused(const QDenseParams& p, const QRowsParams& q, hipS
 // 3072: 8.8 us against 9.4 on 32x32 tiles, 16 x 8192 x 1024: 15.0 against 16.4; but 16 x
 // 4096 x 12288, 768 workgroups: 23.5 against 15.2); else the tile of least modelled time.
 QDenseTile choose_qdense_tile(int64_t M, int64_t N, int64_t Kq) {
-  if (M <= 32 && N <= kRowsN) return {kQDenseRows, (int)(M + 15) / 16 * 16, 16};
+  if (M <= 32 && N <= kRowsN) return {kQDenseRows, (int)(M + 15) / 16 * 16, 16, 0};
   QDenseTile best{};
   double least = INFINITY;
 #define X(ID, BM, BN, WM, WN, NS, OCC, LONE, BUSY, ROUND)                                                \
-  if (const double c = tile_cost(BM, BN, OCC, LONE, BUSY, ROUND, M, N, Kq); c < least) least = c, best = {ID, BM, BN};
+  if (const double c = tile_cost(BM, BN, OCC, LONE, BUSY, ROUND, M, N, Kq); c < least) least = c, best = {ID, BM, BN, NS};
   BYOC_QDENSE_TILES(X)
 #undef X
   return best;
+}
+
+bool qdense_tile_of(int id, QDenseTile* t) {
+#define X(ID, BM, BN, WM, WN, NS, OCC, LONE, BUSY, ROUND) \
+  if (id == ID) return *t = {ID, BM, BN, NS}, true;
+  BYOC_QDENSE_TILES(X)
+#undef X
+  return false;
 }
 
 hipError_t launch_qdense(const QDenseParams& p, QDenseTile t, hipStream_t s) {

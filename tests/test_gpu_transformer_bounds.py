@@ -83,3 +83,60 @@ def test_qdense_scales_whose_product_leaves_float32(m, dtype):
     b = r.normal(size=n).astype(np.float32)
     y = _run("qdense_bias", {"x": x}, ["x", "w", "b"], {}, dtype, [("w", w), ("b", b)])
     _close(y, np.broadcast_to(b, (m, n)).astype(np.float64), np.full((m, n), 4 * E), dtype)
+
+
+TILES = ["256x256_s2", "256x128_s3", "128x128_s3", "128x128_s2", "128x64_s3", "64x64_s4", "32x32_s8"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tile", range(len(TILES)))
+@pytest.mark.parametrize("m, k, n, suffix", [
+    (70, 100, 300, "_bias_add"),          # one stage of 128 codes, in any ring; a part of a tile either way
+    (300, 390, 525, "_bias_add_gelu"),    # rows and channels past the largest tile
+    (517, 1283, 264, "_add_leaky"),       # 11 stages
+    (1100, 257, 1030, "_bias_relu"),      # more tiles than XCDs, in bands of rows
+])
+def test_qdense_every_tile(m, k, n, suffix, tile, dtype, monkeypatch):
+    announce("qdense%s %dx%dx%d %s on %s" % (suffix, m, k, n, dtype, TILES[tile]))
+    r = np.random.default_rng(m + k + n)
+    x, w = _normal(r, m, k), _normal(r, n, k, std=0.05)
+    b, res = r.normal(size=n).astype(np.float32), _normal(r, m, n)
+    ins, args, consts = {"x": x}, ["x", "w"], [("w", w)]
+    if "_bias" in suffix:
+        consts.append(("b", b))
+        args.append("b")
+    if "_add" in suffix:
+        ins["r"] = res
+        args.append("r")
+    attrs = {"alpha": 0.2} if "leaky" in suffix else {}
+    monkeypatch.setenv("BYOC_QDENSE_TILE", str(tile))
+    _, sg = _engine("qdense" + suffix, ins, args, attrs, dtype, consts)
+    with sg:
+        assert [l["name"] for l in sg.launches()] == ["quant_rows", "qdense_" + TILES[tile]]
+    y = _run("qdense" + suffix, ins, args, attrs, dtype, consts)
+    ref = oracle.run_node({"composite": "qdense" + suffix, "attrs": attrs, "out_dtype": dtype},
+                          [x, w] + ([b] if "_bias" in suffix else []) + ([res] if "_add" in suffix else []), mode="exact")
+    terms = np.abs(T.qdense(x, w)) + (np.abs(b) if "_bias" in suffix else 0) + (np.abs(res) if "_add" in suffix else 0)
+    _close(y, ref, (2.0 ** -18 if "gelu" in suffix else 8 * E) * terms + 1e-37, dtype)
+
+
+@pytest.mark.parametrize("m, k, n, name", [
+    (901, 100, 8201, "256x256_s2"),
+    (513, 2051, 8200, "256x128_s3"),
+    (200, 1000, 8200, "128x128_s3"),
+    (1029, 100, 4100, "128x128_s2"),
+    (200, 129, 8200, "128x64_s3"),
+    (33, 129, 8200, "64x64_s4"),
+    (70, 300, 130, "32x32_s8"),
+])
+def test_qdense_tiles_that_the_sizes_choose(m, k, n, name):
+    """The tile of least modelled time, whole and at its remainders."""
+    announce("qdense %dx%dx%d on %s" % (m, k, n, name))
+    r = np.random.default_rng(m + k + n)
+    x, w, res = _normal(r, m, k), _normal(r, n, k, std=0.05), _normal(r, m, n)
+    _, sg = _engine("qdense_add", {"x": x, "r": res}, ["x", "w", "r"], {}, "bf16", [("w", w)])
+    with sg:
+        assert [l["name"] for l in sg.launches()] == ["quant_rows", "qdense_" + name]
+    y = _run("qdense_add", {"x": x, "r": res}, ["x", "w", "r"], {}, "bf16", [("w", w)])
+    ref = T.qdense(x, w)
+    _close(y, ref + res, 8 * E * (np.abs(ref) + np.abs(res)) + 1e-37, "bf16")
