@@ -63,6 +63,33 @@ def test_norm_of_zeros_with_the_smallest_eps(d, dtype):
     _close(y, ref, np.full_like(ref, (2.0 ** -20 * 1.5 + (d / 8 + 8) * E) * 4 * d ** 0.5), dtype)
 
 
+def test_rotary_padding_columns_written_over_nan():
+    """The padding columns of a rotation inside a plan are zeros, whatever the memory held: the intermediates stand in
+    the static scratch, where an engine of NaN values ran before."""
+    import torch
+    from paper_2105_03215_amd import capi, runtime
+    p = workloads.GraphBuilder("poison", 96)
+    p.output(p.qdense(p.qdense(p.input("x", [8, 64], "normal"), 512), 64))  # (qdense keeps a NaN; one launch each)
+    pw = p.finish()
+    g = workloads.GraphBuilder("t", 98)
+    x = g.input("x", [9, 40], "normal")
+    g.output(g.dense(g.rotary(x, g.index_input("p", np.arange(9)), 3, 0, 6), 16))
+    wl = g.finish()
+    with capi.Subgraph(pw.graph, pw.consts, device=0) as poison, capi.Subgraph(wl.graph, wl.consts, device=0) as sg:
+        # 18 columns padded to 24 of 9 rows stand where the poison's 8 x 512 values stood
+        assert sg.stats()["arena_bytes"] >= 9 * 24 * 2 and poison.stats()["arena_bytes"] >= 8 * 512 * 2
+        pin, pout = runtime.inputs_for(poison, pw.inputs, DEV), runtime.outputs_for(poison, DEV)
+        pin[0].fill_(float("nan"))
+        ins, outs = runtime.inputs_for(sg, wl.inputs, DEV), runtime.outputs_for(sg, DEV)
+        poison.run_static(pin, pout)
+        sg.run_static(ins, outs)
+        torch.cuda.synchronize()
+        assert torch.isnan(pout[0]).all()
+        got = runtime.to_host_f64(outs[0])
+    ref = oracle.run_graph(wl.graph, wl.consts, wl.inputs)[0]
+    assert np.isfinite(got).all() and np.abs(got - ref).max() <= 1e-2 * (1 + np.abs(ref).max())
+
+
 # ---- qdense ----------------------------------------------------------------------
 
 @pytest.mark.parametrize("m", [1, 9, 70])
