@@ -167,3 +167,24 @@ def test_qdense_tiles_that_the_sizes_choose(m, k, n, name):
     y = _run("qdense_add", {"x": x, "r": res}, ["x", "w", "r"], {}, "bf16", [("w", w)])
     ref = T.qdense(x, w)
     _close(y, ref + res, 8 * E * (np.abs(ref) + np.abs(res)) + 1e-37, "bf16")
+
+
+def test_qdense_rows_are_quantized_once_for_all_their_products():
+    """One quantization of a value that two products read, and the bits that each product has alone."""
+    from paper_2105_03215_amd import capi, runtime
+    g = workloads.GraphBuilder("t", 99)
+    x = g.input("x", [40, 96], "normal")
+    g.output(g.qdense(x, 64, act="relu"))
+    g.output(g.qdense(x, 200))
+    wl = g.finish()
+    with capi.Subgraph(wl.graph, wl.consts, device=0) as sg:
+        assert [l["name"] for l in sg.launches()].count("quant_rows") == 1
+        both = runtime.run_once(sg, wl.inputs, DEV)
+    for node, y in zip(wl.graph["nodes"], both):
+        names = set(node["inputs"])
+        consts = [c for c in wl.graph["constants"] if c["name"] in names]
+        alone = dict(wl.graph, nodes=[node], outputs=[{"name": node["name"], "dtype": "bf16"}],
+                     constants=[dict(c, index=i) for i, c in enumerate(consts)])
+        with capi.Subgraph(alone, [wl.consts[c["index"]] for c in consts], device=0) as sg:
+            assert [l["name"] for l in sg.launches()].count("quant_rows") == 1
+            assert np.array_equal(runtime.run_once(sg, wl.inputs, DEV)[0], y)
