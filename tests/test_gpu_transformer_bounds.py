@@ -169,6 +169,19 @@ def test_qdense_tiles_that_the_sizes_choose(m, k, n, name):
     _close(y, ref + res, 8 * E * (np.abs(ref) + np.abs(res)) + 1e-37, "bf16")
 
 
+def test_qdense_gelu_of_bf16_far_below_zero():
+    """A GELU in bf16 down to -9 is off by its rounding, half a step of bf16 there, and 2^-16 for the short form."""
+    n = 4096
+    b = np.linspace(-9, 9, n).astype(np.float32)
+    for m in (1, 20, 40):  # rows of zeros: the bias alone
+        x = np.zeros((m, 64), np.float32)
+        y = _run("qdense_bias_gelu", {"x": x}, ["x", "w", "b"], {}, "bf16", [("w", np.ones((n, 64), np.float32)), ("b", b)])
+        ref = np.broadcast_to(oracle.run_node({"composite": "dense_bias_gelu", "out_dtype": "f32"},
+                                              [np.zeros((1, 1)), np.zeros((n, 1)), b], mode="exact"), (m, n))
+        # (the steps of a value that the short form may have moved past a power of two)
+        assert (np.abs(y - ref) <= 0.5 * bf16_ulp(ref * (1 + 2.0 ** -16)) + 2.0 ** -16 * np.abs(ref)).all()
+
+
 def test_qdense_rows_are_quantized_once_for_all_their_products():
     """One quantization of a value that two products read, and the bits that each product has alone."""
     from paper_2105_03215_amd import capi, runtime
