@@ -201,3 +201,35 @@ def test_qdense_rows_are_quantized_once_for_all_their_products():
         with capi.Subgraph(alone, [wl.consts[c["index"]] for c in consts], device=0) as sg:
             assert [l["name"] for l in sg.launches()].count("quant_rows") == 1
             assert np.array_equal(runtime.run_once(sg, wl.inputs, DEV)[0], y)
+
+
+# ---- plans -----------------------------------------------------------------------
+
+def test_decoder_layer_two_streams(monkeypatch):
+    """Launches that do not depend on the one before them on the engine's second stream: the bits of one stream, also
+    replayed from a graph."""
+    import torch
+    from paper_2105_03215_amd import capi, runtime
+    wl = _layer(batch=2, tokens=40, encoder_tokens=300)
+    monkeypatch.delenv("BYOC_STREAMS", raising=False)
+    one = capi.Subgraph(wl.graph, wl.consts, device=0)
+    monkeypatch.setenv("BYOC_STREAMS", "2")
+    two = capi.Subgraph(wl.graph, wl.consts, device=0)
+    monkeypatch.delenv("BYOC_STREAMS")
+    s = torch.cuda.Stream(device=DEV)
+    with one, two:
+        ins, ref = runtime.inputs_for(one, wl.inputs, DEV), runtime.outputs_for(one, DEV)
+        torch.cuda.synchronize()
+        one.run(ins, ref, s)
+        s.synchronize()
+        for replay in (False, True, True, True):
+            two.set_options(graph_replay=replay)
+            out = runtime.outputs_for(two, DEV)
+            out[0].fill_(float("nan"))
+            torch.cuda.synchronize()
+            for _ in range(2):
+                two.run(ins, out, s)
+            s.synchronize()
+            assert torch.equal(ref[0].view(torch.int16), out[0].view(torch.int16))
+            torch.mm(torch.ones(64, 64, device=DEV), torch.ones(64, 64, device=DEV))
+            torch.cuda.synchronize()
