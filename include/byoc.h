@@ -66,8 +66,8 @@
  *       {"type": "linear"|"ntk"|"yarn", "factor" >= 1, and for yarn
  *       "original_length", "beta_fast" (32), "beta_slow" (1),
  *       "attention_factor" (0.1 ln(factor) + 1)} for contexts longer than
- *       trained on.  Pair i turns by position * base^(-2i / rotary_dim), exactly for
- *       every 32-bit position.
+ *       trained on.  Pair i turns by position * base^(-2i / rotary_dim), formed in
+ *       float64: off by 2^-26 of a turn, and by 2^-24 at positions near 2^31.
  *   qk_norm_rotary    data, query weight [D][, key weight [D] if kv_heads > 0],
  *                     positions: the same after x / sqrt(mean(x^2) + eps) * weight
  *                     over each head; also attrs eps (default 1e-6)

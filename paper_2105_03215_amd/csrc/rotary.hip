@@ -5,8 +5,9 @@
 //   (a, b) of pair i -> (a cos - b sin, b cos + a sin) * mag,  angle = position * theta_i
 //
 // The angle is reduced in turns in float64 (position x turns per position, less its
-// integer part), exact enough for every 32-bit position, before the float32 sine
-// and cosine; in float32 a position of 10^5 would lose 2^-8 of a radian.
+// integer part) before the float32 sine and cosine: off by 2^-26 of a turn as it is rounded to
+// float32, and by another 2^-24 at positions near 2^31, where 53 bits of turns per position end;
+// in float32 a position of 10^5 would lose 2^-8 of a radian.
 //
 // HBM bound: every row is read and written once.  What a row's columns are multiplied
 // with is formed once by its workgroup, into LDS, for all of its heads.  8192 rows of 40

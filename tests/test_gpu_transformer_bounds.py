@@ -63,6 +63,26 @@ def test_norm_of_zeros_with_the_smallest_eps(d, dtype):
     _close(y, ref, np.full_like(ref, (2.0 ** -20 * 1.5 + (d / 8 + 8) * E) * 4 * d ** 0.5), dtype)
 
 
+def test_rotary_angles_of_the_farthest_positions():
+    """Sines and cosines at both ends of 32 bits, against 60 digits."""
+    d = 64
+    pos = np.array([2 ** 31 - 1, -2 ** 31, 2 ** 30 + 7, -(2 ** 29) - 1, 123456789], np.int32)
+    x = np.zeros((len(pos), d), np.float32)
+    x[:, :d // 2] = 1.0  # (a, b) = (1, 0) of every pair: its cosine and sine come out
+    y = _run("rotary", {"x": x, "p": pos}, ["x", "p"], {"heads": 1, "head_dim": d}, "f32")
+    with decimal.localcontext() as c:
+        c.prec = 60
+        two_pi = 2 * decimal.Decimal("3.14159265358979323846264338327950288419716939937510582097494459")
+        ref = np.zeros_like(y)
+        for i in range(d // 2):
+            theta = decimal.Decimal(10000) ** (decimal.Decimal(-2 * i) / d)
+            for m, p in enumerate(pos):
+                turns = int(p) * theta / two_pi
+                angle = float((turns - turns.to_integral_value()) * two_pi)
+                ref[m, i], ref[m, i + d // 2] = np.cos(angle), np.sin(angle)
+    _close(y, ref, np.full_like(ref, 2.0 ** -20), "f32")
+
+
 def test_rotary_padding_columns_written_over_nan():
     """The padding columns of a rotation inside a plan are zeros, whatever the memory held: the intermediates stand in
     the static scratch, where an engine of NaN values ran before."""
