@@ -223,6 +223,32 @@ def test_qdense_rows_are_quantized_once_for_all_their_products():
             assert np.array_equal(runtime.run_once(sg, wl.inputs, DEV)[0], y)
 
 
+# ---- attention -------------------------------------------------------------------
+
+@pytest.mark.parametrize("k_len, d, group", [(64, 64, 1), (200, 128, 4), (70, 256, 2), (600, 64, 8)])
+def test_attention_weights_of_few_rows_are_not_rounded_to_bf16(k_len, d, group):
+    """Values that cancel leave the error of the weights alone: where few rows share the keys 2^-16 of each, two
+    roundings to bf16 one after the other."""
+    announce("attention weights k %d d %d group %d" % (k_len, d, group))
+    r = np.random.default_rng(k_len + d)
+    # (scores near each other, so that their own rounding stays below that of the weights)
+    q, k = np.repeat(_normal(r, 1, d, std=0.02), group, axis=0).reshape(1, -1), _normal(r, k_len, d)
+    v = r.normal(size=(k_len, d))
+    s = k.astype(np.float64) @ q[0, :d].astype(np.float64) / d ** 0.5
+    p = np.exp(s - s.max())
+    p /= p.sum()
+    big = np.argmax(p)
+    v[big] = 0
+    v[big] = -(p @ v) / p[big]
+    v = to_bf16_values(v.astype(np.float32))
+    attrs = {"batch": 1, "heads": group, "kv_heads": 1, "head_dim": d}
+    y = _run("attention", {"q": q, "k": k, "v": v}, ["q", "k", "v"], attrs, "bf16")
+    ref, absum, score = T.attention(attrs, q, k, v, None, magnitudes=True)
+    bound = (2 * (d + 8) * E * score + (k_len + 64) * E + 2.0 ** -16) * absum + U * np.abs(ref)
+    far = np.abs(y - ref) - bound
+    assert far.max() <= 0, "worst by %.3g of %.3g" % (far.max(), absum.max())
+
+
 # ---- plans -----------------------------------------------------------------------
 
 def test_decoder_layer_two_streams(monkeypatch):
