@@ -17,6 +17,7 @@
 // O^T = V^T P^T: register group i of a lane half h holds keys 8 (i / 4) + 4 h + i % 4,
 // and V^T is read in the same order (the order of a sum over keys is free).
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <type_traits>
 
@@ -208,72 +209,86 @@ __device__ __forceinline__ uint4 load_vt(const char* vt, int row0, int d, int la
   return make_uint4(vf[0].x, vf[0].y, vf[1].x, vf[1].y);
 }
 
-// Under a causal mask a tile holds keys that some of its rows do not see.  Their weights are
-// zero, but zero times an infinite or NaN value is NaN.  A wave whose results are not
-// all finite forms those rows again, key by key, with the seen keys alone (tiles first,
-// first + step, ... < end of `keys` keys): slow, and only then.
+// Under a causal mask a wave's last tiles (two at most, as its rows' limits are less than 32 apart) hold keys that
+// some of its rows do not see.  Their weights are zero, but zero times an infinite or NaN value is NaN: at the first
+// of these tiles that holds one the wave stops, and add_keys adds the keys from there on one by one.  (1 x 4096, 32
+// heads of 128: 156 us, up to 299 with a NaN; 1 x 1024, 8 heads of 64: 12 and 88; 2 x 2048, 8 heads of 256, where the
+// check of 32 KB a tile counts most: 80.7 without it, 83.3.)
+template <bool BF, int BYTES>
+__device__ __forceinline__ bool holds_not_finite(const char* tile) {
+  typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+  const uint4* at = (const uint4*)tile + (threadIdx.x & 63);
+  uint32_t top = 0;
+#pragma unroll 8
+  for (int i = 0; i < BYTES / 1024; ++i) {
+    const uint4 x = at[i * 64];
+    for (uint32_t w : {x.x, x.y, x.z, x.w}) {
+      if constexpr (BF)
+        top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top),
+                                                                     __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu)));
+      else
+        top = max(top, w & 0x7FFFFFFFu);
+    }
+  }
+  return __any(BF ? max(top & 0xFFFFu, top >> 16) >= 0x7F80u : top >= 0x7F800000u);
+}
+
+// 4 columns of a row as floats.
+__device__ __forceinline__ void load4(const bf16_t* p, float* v) {
+  const uint2 u = *(const uint2*)p;
+  v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xFFFF0000u);
+  v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void load4(const float* p, float* v) {
+  const float4 u = *(const float4*)p;
+  v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
+}
+
+// Adds keys j0 .. j1 - 1 to each row that sees them.
 template <typename T, int DB, int QS>
-__device__ __forceinline__ void redo_not_finite(const AttnParams& p, const char* kb, const char* vb, int64_t sk, int64_t sv,
-                                                int lim, int first, int end, int step, int keys, const uint4* qf,
-                                                float c2, f32x16* o, float& m, float& l) {
+__device__ __forceinline__ void add_keys(const AttnParams& p, const char* kb, const char* vb, int64_t sk, int64_t sv, int lim,
+                                         int j0, int j1, const uint4* qf, float c2, f32x16* o, float& m, float& l) {
   constexpr int PER = 16 / sizeof(T);  // values of a 16-byte chunk
   const int h = (threadIdx.x & 63) >> 5;
-  float far = 0.0f;  // NaN when a result is not finite
+#pragma unroll 1
+  for (int j = j0; j < j1 && __any(j < lim); ++j) {
+    const bool seen = j < lim;
+    const T* const kr = (const T*)(kb + (int64_t)j * sk) + h * PER;
+    const T* const vr = (const T*)(vb + (int64_t)j * sv) + 4 * h;
+    float s = 0.0f;
 #pragma unroll
-  for (int d = 0; d < DB; ++d)
+    for (int st = 0; st < QS; ++st) {
+      if (!seen || (2 * st + h) * PER >= p.D) continue;
+      float a[8], b[8];
+      const uint4 k = *(const uint4*)(kr + 2 * st * PER);
+      if constexpr (PER == 8) {
+        unpack8(k, a);
+        unpack8(qf[st], b);
+      } else {
+        const f32x4 kf = __builtin_bit_cast(f32x4, k), qq = __builtin_bit_cast(f32x4, qf[st]);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) far = __builtin_fmaf(o[d][i], 0.0f, far);
-  far = half_sum(far);
-  const bool bad = far != far;
-  if (!__any(bad)) return;
-  if (!bad) lim = 0;  // (the others keep what they have)
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[d][i] = bad ? 0.0f : o[d][i];
-  m = bad ? -INFINITY : m;
-  l = bad ? 0.0f : l;
-  for (int t = first; t < end; t += step)
-    for (int j = t * keys; j < (t + 1) * keys && __any(j < lim); ++j) {
-      const bool seen = j < lim;
-      float s = 0.0f;
-#pragma unroll
-      for (int st = 0; st < QS; ++st) {
-        const int c = 2 * st + h;
-        if (seen && c * PER < p.D) {
-          float a[8], b[8];
-          const uint4 k = *(const uint4*)(kb + (int64_t)j * sk + c * 16);
-          if constexpr (PER == 8) {
-            unpack8(k, a);
-            unpack8(qf[st], b);
-          } else {
-            const f32x4 kf = __builtin_bit_cast(f32x4, k), qq = __builtin_bit_cast(f32x4, qf[st]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) a[e] = kf[e], b[e] = qq[e];
-          }
-#pragma unroll
-          for (int e = 0; e < PER; ++e) s = __builtin_fmaf(a[e], b[e], s);
-        }
+        for (int e = 0; e < 4; ++e) a[e] = kf[e], b[e] = qq[e];
       }
-      s = half_sum(s) * c2;
-      if (!seen) continue;
-      const float mn = fmaxf(m, s), use = mn == -INFINITY ? 0.0f : mn;
-      const float keep = exp2_(m - use), w = exp2_(s - use);
-      m = mn;
-      l = l * keep + (h == 0 ? w : 0.0f);  // (the halves' sums are added later)
 #pragma unroll
-      for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int col = d * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
-          if (col >= p.D) continue;
-          const T x = *(const T*)(vb + (int64_t)j * sv + col * sizeof(T));
-          float v;
-          if constexpr (sizeof(T) == 2) v = bf16_to_f32(x);
-          else v = x;
-          o[d][i] = o[d][i] * keep + w * v;
-        }
+      for (int e = 0; e < PER; ++e) s = __builtin_fmaf(a[e], b[e], s);
     }
+    s = half_sum(s) * c2;
+    if (!seen) continue;
+    const float mn = fmaxf(m, s), use = mn == -INFINITY ? 0.0f : mn;
+    const float keep = exp2_(m - use), w = exp2_(s - use);
+    m = mn;
+    l = l * keep + (h == 0 ? w : 0.0f);  // (the halves' sums are added later)
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        if (d * 32 + 8 * g + 4 * h >= p.D) continue;
+        float v[4];
+        load4(vr + d * 32 + 8 * g, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[d][4 * g + e] = o[d][4 * g + e] * keep + w * v[e];
+      }
+  }
 }
 
 // A workgroup takes 32 packed query rows of one (batch, key head) and a share of
@@ -313,7 +328,8 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   const int len = uniform(batch_len(p, b));
   const int row = cb * kCols + col;
   const int lim = seen_keys(p, len, row);
-  const int kend = uniform(seen_keys(p, len, min(cb * kCols + kCols, R) - 1));  // (rows see more keys further down)
+  const int lim_lo = uniform(seen_keys(p, len, cb * kCols));  // (rows see more keys further down)
+  const int kend = uniform(seen_keys(p, len, min(cb * kCols + kCols, R) - 1));
   const int t0 = (chunk - ck.first) * ck.size;
   const int t_end = min(t0 + ck.size, (kend + kKeys - 1) / kKeys);
 
@@ -362,6 +378,7 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   for (int d = 0; d < DB; ++d) o[d] = f32x16{};
   float m = -INFINITY, l = 0.0f;
   const float c2 = p.scale * 1.44269504088896340736f;
+  const int masked = p.causal && p.q_len > 1 ? lim_lo / kKeys : INT_MAX;  // the first tile that some rows see a part of
 
   // Loads of 2 NBUF half tiles are in flight: a half is filled again as soon as it has been read.
   auto landed = [] { asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * NBUF - 1) * NI) : "memory"); };
@@ -437,8 +454,12 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
     fill(n, t0 + wave + n * NW, keys);
     fill(n, t0 + wave + n * NW, values);
   }
-  int buf = 0;
-  for (int t = t0 + wave; t < t_end; t += NW) {
+  int buf = 0, t = t0 + wave;
+  for (; t < t_end; t += NW) {
+    if (t >= masked) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * NBUF - 2) * NI) : "memory");  // the tile's keys and values
+      if (holds_not_finite<BF, TILE>(mine + (buf * 2 + 1) * TILE)) break;
+    }
     compute(buf, t);
     read();
     fill(buf, t + NBUF * NW, values);
@@ -446,8 +467,7 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
-  if (p.causal && p.q_len > 1)
-    redo_not_finite<T, DB, QS>(p, kb, vb, sk, sv, lim, t0 + wave, t_end, NW, kKeys, qf, c2, o, m, l);
+  for (; t < t_end; t += NW) add_keys<T, DB, QS>(p, kb, vb, sk, sv, lim, t * kKeys, (t + 1) * kKeys, qf, c2, o, m, l);
 
   // the waves' results: a common maximum, then the sums in wave order
   l = half_sum(l);
@@ -633,6 +653,8 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   float m = -INFINITY, l = 0.0f;
   const float c2 = p.scale * 1.44269504088896340736f;
   const int t_wave = min(t_end, (lim_hi + kTileKeys - 1) / kTileKeys);  // tiles that this wave's rows see
+  const int masked = p.causal && p.q_len > 1 ? lim_lo / kTileKeys : INT_MAX;  // the first that some rows see a part of
+  int stop = t_wave;                                                          // the tiles from there on are left to add_keys
 
   // LDS offsets of this lane's operands in a tile: its key row at chunk h, whose other chunks are an XOR
   // away (chunk 2 st + h at st << 5); and its part of V^T for 32-column block d, key group j
@@ -748,6 +770,9 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
     __builtin_amdgcn_sched_barrier(0);
   };
 
+  auto check = [&](int t, auto par_tag) {
+    if (t >= masked && t < stop && holds_not_finite<true, TILE>(vt + decltype(par_tag)::value * TILE)) stop = t;
+  };
   // Before step t: its values and the keys of t + 1 have landed for every wave, and every wave is done with
   // the tiles before, whose places keys t + 2 (that of t) and values t + 1 take.
   auto turn = [&](auto same, auto other) {
@@ -767,14 +792,16 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   static_for<0, QS>([&](auto st) { mul_k(read_k(even, st), st, sa); });
   for (int t = t0; t < t_end; t += 2 * KS) {
     turn(even, odd);
-    if (t + kg < t_wave) step(t + kg, even, sa, sb);
+    check(t + kg, even);
+    if (t + kg < stop) step(t + kg, even, sa, sb);
     if (t + KS >= t_end) break;
     turn(odd, even);
-    if (t + KS + kg < t_wave) step(t + KS + kg, odd, sb, sa);
+    check(t + KS + kg, odd);
+    if (t + KS + kg < stop) step(t + KS + kg, odd, sb, sa);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  if (p.causal && p.q_len > 1)
-    redo_not_finite<bf16_t, DB, QS>(p, kb, vb, sk, sv, lim, t0 + kg, t_end, KS, kTileKeys, qf, c2, o, m, l);
+  for (; stop < t_wave; stop += KS)
+    add_keys<bf16_t, DB, QS>(p, kb, vb, sk, sv, lim, stop * kTileKeys, (stop + 1) * kTileKeys, qf, c2, o, m, l);
   l = half_sum(l);
   if constexpr (KS > 1) {
     // the second key group hands its results over, lane by lane, in the place of the tiles
@@ -863,7 +890,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
   const int len = uniform(batch_len(p, b));
   const int row0 = tile * 32 * NW + wave * 32, row = row0 + col;
   const int lim = seen_keys(p, len, row);
-  const int lim_hi = uniform(row0 < R ? seen_keys(p, len, min(row0 + 32, R) - 1) : 0);  // (rows see more keys further down)
+  const int lim_lo = uniform(seen_keys(p, len, min(row0, R - 1)));  // (rows see more keys further down)
+  const int lim_hi = uniform(row0 < R ? seen_keys(p, len, min(row0 + 32, R) - 1) : 0);
   const int kend = uniform(seen_keys(p, len, min((tile + 1) * 32 * NW, R) - 1));
   const int t_end = (kend + kKeys - 1) / kKeys;
   const int t_wave = min(t_end, (lim_hi + kKeys - 1) / kKeys);  // tiles that this wave's rows see
@@ -908,6 +936,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
   for (int d = 0; d < DB; ++d) o[d] = f32x16{};
   float m = -INFINITY, l = 0.0f;
   const float c2 = p.scale * 1.44269504088896340736f;
+  const int masked = p.causal && p.q_len > 1 ? lim_lo / kKeys : INT_MAX;  // the first tile that some rows see a part of
+  int stop = t_wave;                                                      // the tiles from there on are left to add_keys
   auto compute = [&](int par, int t) {
     const char* kt = lds + par * 2 * TILE;
     const char* vt = kt + TILE;
@@ -955,11 +985,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
     // tile t has landed for every wave, and every wave is done with the one before, whose place t + 1 takes
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     fill(par ^ 1, t + 1);
-    if (t < t_wave) compute(par, t);
+    if (t >= masked && t < stop && holds_not_finite<false, TILE>(lds + (par * 2 + 1) * TILE)) stop = t;
+    if (t < stop) compute(par, t);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  if (p.causal && p.q_len > 1)
-    redo_not_finite<float, DB, QS>(p, kb, vb, sk, sv, lim, 0, t_end, 1, kKeys, qf, c2, o, m, l);
+  for (; stop < t_wave; ++stop)
+    add_keys<float, DB, QS>(p, kb, vb, sk, sv, lim, stop * kKeys, (stop + 1) * kKeys, qf, c2, o, m, l);
   l = half_sum(l);
   if (row >= R) return;
   // (a row without keys is zero; one whose seen scores are all -inf divides zero by zero, as the softmax does)

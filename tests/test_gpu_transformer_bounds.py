@@ -249,6 +249,52 @@ def test_attention_weights_of_few_rows_are_not_rounded_to_bf16(k_len, d, group):
     assert far.max() <= 0, "worst by %.3g of %.3g" % (far.max(), absum.max())
 
 
+def _time(sg, ins, outs, n=5):
+    import torch
+    best = float("inf")
+    for _ in range(n):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        sg.run(ins, outs)
+        b.record()
+        b.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return best
+
+
+@pytest.mark.parametrize("q_len, heads, d, dtype", [(1024, 8, 64, "bf16"), (1024, 4, 128, "bf16"), (1024, 32, 64, "f32"),
+                                                    (8, 1, 64, "bf16"), (8, 1, 128, "f32")])
+def test_attention_nan_costs_no_time(q_len, heads, d, dtype):
+    """An infinite or NaN value that the rows see, or that a causal mask hides from a few of them, leaves a prompt at
+    its speed (ten times at most: the rows that share its tile are formed key by key, over that tile alone)."""
+    import torch
+    announce("attention of NaN q %d heads %d d %d %s" % (q_len, heads, d, dtype))
+    n = 1024
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    kind = torch.bfloat16 if dtype == "bf16" else torch.float32
+    q, k, v = (torch.randn(m, heads * d, generator=g, device=DEV).to(kind) for m in (q_len, n, n))
+    host = {"q": np.zeros(q.shape, np.float32), "k": np.zeros(k.shape, np.float32), "v": np.zeros(v.shape, np.float32)}
+    _, sg = _engine("attention", host, ["q", "k", "v"], {"batch": 1, "heads": heads, "head_dim": d, "causal": True}, dtype)
+    with sg:
+        out, clean_out = torch.empty_like(q), torch.empty_like(q)
+        _time(sg, [q, k, v], [out])
+        clean = _time(sg, [q, k, v], [clean_out])
+        for at, value in ((0, float("nan")), (n - q_len, float("inf")), (n - 4, float("nan")), (n - 2, float("-inf"))):
+            bad = v.clone()
+            bad[at, 1] = value
+            t = _time(sg, [q, k, bad], [out])
+            assert t <= 10 * clean, "value %g at key %d: %.3f ms, %.3f without" % (value, at, t, clean)
+            # the rows before it, and the other columns, are what they were
+            seen = torch.arange(q_len, device=DEV) + n - q_len >= at
+            assert not torch.isfinite(out[seen, 1]).any()
+            keep = torch.ones_like(out, dtype=torch.bool)
+            keep[seen, 1] = False
+            assert torch.isfinite(out[keep]).all()
+            # (their weights may be rounded on one way and not on the other)
+            assert ((out[keep] - clean_out[keep]).float().abs() <= 2.0 ** -6 * (1 + clean_out[keep].float().abs())).all()
+
+
 # ---- plans -----------------------------------------------------------------------
 
 def test_decoder_layer_two_streams(monkeypatch):
