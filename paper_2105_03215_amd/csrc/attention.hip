@@ -294,7 +294,7 @@ __device__ __forceinline__ void add_keys(const AttnParams& p, const char* kb, co
 // A workgroup takes 32 packed query rows of one (batch, key head) and a share of
 // its keys; its waves take tiles of 32 keys in turn, each through its own LDS
 // tiles, without a barrier until their results meet at the end.  Single tokens are
-// bound by the keys' and values' bytes: 4 x 1 over up to 32768 keys, 32 heads over 8 of 128 (388 MB): 77 us,
+// bound by the keys' and values' bytes: 4 x 1 over up to 32768 keys, 32 heads over 8 of 128 (388 MB): 78 us,
 // 5.0 TB/s.
 //
 // DP columns of a head in LDS (a power of two), DC of them multiplied.
@@ -563,9 +563,10 @@ __device__ __forceinline__ Place place(const AttnParams& p, int rows) {
 // Many rows, bf16: four waves of 32 packed rows each share tiles of 64 keys and
 // values, double-buffered in LDS; a tile's loads run while the one before is
 // multiplied, with one barrier a tile.  Two such workgroups fit a CU (D <= 128), so
-// that one's softmax runs beside the other's products.  Bound by the matrix cores at 128 columns (causal
-// 2 x 4096, 32 heads over 8 of 128: 272 us, 1010 TFLOP/s), by the exponentials on the vector ALU at 64 (causal 2 x
-// 4096, 12 of 64: 74 us).
+// that one's softmax runs beside the other's products.  Bound by both at 128 columns (causal 2 x 4096, 32 heads over 8
+// of 128: 264 to 276 us, 1000 to 1040 TFLOP/s, the matrix cores busy for 58% of the cycles and the vector ALU for 56%), by the vector
+// ALU at 64 (causal 2 x 4096, 12 of 64: 72 to 74 us, 39% and 65%); of sequences of different lengths by the longest one's chain
+// of tiles (8 x 449 over 53 to 1027, 12 of 64: 19 us, 17 tiles in a row; 18% and 37%).
 //
 // The running maximum moves only when a tile's exceeds it by more than 2^8 (kSlack):
 // the weights then stay under 2^8, far from overflow, and the 16 x D / 32 products
@@ -1104,7 +1105,7 @@ int row_blocks(const AttnParams& p) {
 // both (18.8 in two chunks); 1 x 1024 over 4096, 8 of 128, 68 and 38; 4 x 40 over 8192, 8 of 64, 54 and 20.
 int split_tiles(const AttnParams& p, int64_t blocks) {
   const double tile = p.D <= 64 ? 0.4 : p.D <= 96 ? 0.93 : p.D <= 128 ? 1.03 : p.D <= 192 ? 2.1 : 2.65;
-  const double shared = p.D <= 64 ? 1.0 : 0.4;  // (the vector ALU, which bounds 64 columns, is full with one)
+  const double shared = p.D <= 64 ? 1.0 : 0.4;  // (at 64 columns, which the vector ALU bounds, a second workgroup gains nothing)
   const double tiles = ceil_div(p.k_len, kTileKeys);
   const double part = 8e-6 / 4.1 * p.D * p.batch * p.kv_heads * p.q_len * p.group;  // a chunk's sums, written and read
   int best = 1;

@@ -274,8 +274,8 @@ __device__ __forceinline__ void finish8(const QDenseParams& p, const int* acc, f
 
 // BM rows x BN channels per workgroup of WM x WN waves; both operands streamed
 // HBM -> LDS in stages of 128 codes through a ring of NS, the MFMA operands of a
-// step of 64 codes read while the previous step multiplies.  Bound by that feed (below, at the
-// tiles): 8192 x 4096 x 8192 256 us, 2.1 POP/s.
+// step of 64 codes read while the previous step multiplies.  Bound by the wait at the end of a stage (below,
+// at the tiles): 8192 x 4096 x 8192 256 us, 2.1 POP/s.
 template <int BM, int BN, int WM, int WN, int NS, bool F32>
 __global__ __launch_bounds__(64 * WM * WN) void qdense_kernel(QDenseParams p) {
   constexpr int kNT = 64 * WM * WN;
@@ -627,11 +627,12 @@ hipError_t launch_one(QDenseParams p, hipStream_t s) {
 // a stage of 128 codes while at most one workgroup runs per CU or all slots (occ per
 // CU) are busy, and a round's prologue and epilogue.  Fitted to 15 shapes from 24 x 4096 x
 // 12288 to 8192 x 4096 x 8192, on which the choice is never more than 8% behind the
-// fastest tile (18 others: 18% at 700 x 128 x 700, 16% at 284 x 5549 x 10785, else up to 10%).  What bounds the large tiles is the feed: a 256x256 stage moves 64 KB from
-// L2 to LDS and 192 KB from LDS to registers in 1.8 us, for 0.9 us of matrix
-// operations; with 4 waves of 128 x 128 the LDS reads fall by a third, but one wave per SIMD hides
-// nothing (8192 x 4096 x 8192: 347 us against 256), and half-depth stages in a ring of
-// five fetch half cache lines (285).
+// fastest tile (18 others: 18% at 700 x 128 x 700, 16% at 284 x 5549 x 10785, else up to 10%).  A 256x256 stage, 64 KB from
+// L2 to LDS and 192 KB from LDS to registers, takes 1.8 us for 0.9 us of matrix operations: in
+// 8192 x 4096 x 8192 the matrix cores are busy for 56% of the cycles, the LDS for 21%, and a third of the
+// waves' time is waiting at the end of a stage, for its loads and its barrier, with a ring of two.  With 4 waves of 128 x
+// 128 the LDS reads fall by a third, but one wave per SIMD hides nothing (347 us against 256), and
+// half-depth stages in a ring of five fetch half cache lines (285).
 //   id BM BN WM WN NS  occ  lone  busy  round
 #define BYOC_QDENSE_TILES(X)                 \
   X(0, 256, 256, 2, 4, 2, 1, 1.33, 1.8, 9.0) \
