@@ -25,8 +25,8 @@
  *
  * Serialized format (schema "byoc-subgraph", version 1), a JSON object:
  *   "inputs":    [{"name", "shape", "dtype": "f32"|"bf16", "layout": "NCHW"|"ROWMAJOR"}]
- *                or {"name", "shape": [n], "dtype": "i32"}: positions or lengths,
- *                in bf16 and f32 graphs
+ *                or {"name", "shape": [n], "dtype": "i32"}: positions, lengths,
+ *                tokens and the like, in bf16 and f32 graphs
  *   "constants": [{"name", "index", "shape", "dtype"}]   index into the
  *                constant array passed to create; conv weights OIHW, dense
  *                weights [out, in], biases [out]
@@ -85,6 +85,47 @@
  *   attention_lengths also lengths [B] (i32): sequence b has min(max(n, 0), Lk)
  *                     keys; what its further rows hold does not matter.
  *                     A query that sees no key gives zeros.
+ * Composites of a step that verifies drafted tokens, on the same tensors and graphs:
+ *   mxdense[_bias][_add][_relu|_relu6|_gelu|_leaky]  data [M,K], weight [N,K]
+ *                     dense on microscaled 4-bit floating point: each row of
+ *                     data and of the weight in blocks of 32 columns, a block's values
+ *                     s c with s = 2^(floor(log2 max|v|) - 2), at least 2^-127, and c the nearest
+ *                     of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (ties to the even code); the
+ *                     products of these summed in float32, then bias, residual and
+ *                     activation.  A row that holds an infinity or a NaN gives NaN.
+ *                     K <= 131072.
+ *   attention_tree    queries [B T, *], keys and values of a cache [B Lk, *] each, drafted
+ *                     keys and values [B T, *] each, lengths [B] (i32), parents [B T] (i32)
+ *                     -> [B T, heads D]: attention of T <= 256 drafted tokens of each
+ *                     sequence.  Query i of sequence b sees the first min(max(lengths[b], 0), Lk)
+ *                     keys of its cache and, of the drafted keys, those of the tokens on its path:
+ *                     i itself, its parent, that one's parent and so on.  Parents are numbered
+ *                     within the sequence; one that is not of a token before its own
+ *                     (-1: a child of the last token of the cache) ends the path.  Drafted keys
+ *                     and values are read where a projection left them, so that a cache
+ *                     holds accepted tokens only.
+ *       attrs batch B, heads, kv_heads, head_dim, scale, q_col, k_col, v_col as attention's,
+ *       draft_k_col, draft_v_col (likewise).  f32 rows have a multiple of 4 columns.
+ *   logits[_penalties[_drafts]][_bias][_mask]        logits [B R, V] -> [B R, V]: the rules in
+ *                     the name, at least one, on the R rows of each of B sequences, in this
+ *                     order, in float32 with one rounding at the end.  Further inputs, in the
+ *                     order of the name:
+ *     penalties       history [B T] (i32), prompt lengths [B] (i32), lengths [B] (i32),
+ *                     strengths [B, 3] (f32: repetition, presence, frequency).  The history
+ *                     is the first min(max(length, 0), T) tokens, the first prompt-length of which
+ *                     are the prompt, the rest are generated.  A token anywhere in it has its
+ *                     logit divided by repetition if above zero, else multiplied; then
+ *                     a token that was generated n > 0 times loses frequency n + presence.
+ *     drafts          tokens [B R] (i32), parents [B R] (i32): row i is that of drafted token
+ *                     i, R <= 256, and the tokens on its path, its own included, count as
+ *                     generated
+ *     bias            tokens [B E] (i32), values [B, E] (f32): added; of several
+ *                     entries for a token the last counts
+ *     mask            words [B R ceil(V / 32)] (i32): token t of a row may be chosen where bit
+ *                     t % 32 of the row's word t / 32 is set, else its logit is -inf
+ *                     Tokens outside [0, V) are passed over, so that -1 marks an unused place.
+ *       attrs batch B.
+ *     The f32 inputs are read in place, aligned to 4 bytes, and are not rounded in bf16 graphs.
  * Buffers that these composites read or write directly are aligned to 16 bytes.
  * A leaky ReLU (suffix _leaky) takes its slope from attrs alpha in [0, 1)
  * (default 0.1).
@@ -179,7 +220,9 @@ typedef enum {
   BYOC_K_CONV_I8 = 8,   /* implicit-GEMM conv / dense on int8 MFMA      */
   BYOC_K_QDENSE = 9,    /* qdense: its rows' quantization and product   */
   BYOC_K_ROTARY = 10,
-  BYOC_K_ATTENTION = 11
+  BYOC_K_ATTENTION = 11,
+  BYOC_K_MXDENSE = 12,  /* mxdense: its rows' quantization and product  */
+  BYOC_K_LOGITS = 13
 } byoc_kernel_kind;
 
 /* One entry of the launch sequence a run enqueues.  Independent convolutions
@@ -261,7 +304,7 @@ byoc_status byoc_subgraph_num_io(const byoc_subgraph* g, int32_t* n_in, int32_t*
 byoc_status byoc_subgraph_io_desc(const byoc_subgraph* g, int32_t is_output, int32_t idx,
                                   byoc_tensor_desc* desc);
 
-/* Multiply-accumulates of the conv, dense and qdense composites (the cost measure
+/* Multiply-accumulates of the conv, dense, qdense and mxdense composites (the cost measure
  * of the paper's TensorRT fallback rule, Sec. 4.1), bytes of packed
  * constants and bytes of the intermediate arena.  Any pointer may be NULL. */
 byoc_status byoc_subgraph_stats(const byoc_subgraph* g, int64_t* macs, int64_t* weight_bytes,

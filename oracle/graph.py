@@ -26,6 +26,11 @@ the order data, weight, bias, residual.  Transformer-layer composites (module
 given, also in a bf16 graph), ``rotary`` (data, positions), ``qk_norm_rotary`` (data,
 query weight[, key weight], positions), ``attention`` (queries, keys, values) and
 ``attention_lengths`` (also lengths); positions and lengths are i32 inputs.
+Composites of drafted tokens (module ``drafts``): ``mxdense`` with dense's suffixes
+(weights quantized as given), ``attention_tree`` (queries, keys and values of the cache,
+drafted keys and values, lengths, parents) and ``logits[_penalties[_drafts]][_bias][_mask]``
+(logits, then history, prompt lengths, lengths, strengths; drafted tokens, parents;
+bias tokens, bias values; mask words), whose strengths and bias values stay float32.
 
 Precision semantics.  A node whose ``out_dtype`` is "bf16" belongs to a bf16
 graph: its activations are bf16 values, its weights are rounded to bf16 (ties
@@ -44,7 +49,7 @@ import json
 
 import numpy as np
 
-from . import ops, transformer
+from . import drafts, ops, transformer
 from .bf16 import round_bf16
 
 _ACTS = ("relu6", "relu", "gelu", "leaky")
@@ -60,11 +65,14 @@ def load_graph(js):
 def parse_composite(name):
     """Split a pattern name into (op, has_bias, has_add, activation)."""
     if name in ("max_pool2d", "global_avg_pool2d", "avg_pool2d", "concatenate",
-                "rotary", "qk_norm_rotary", "attention", "attention_lengths"):
+                "rotary", "qk_norm_rotary", "attention", "attention_lengths", "attention_tree"):
         return name, False, False, None
     parts = name.split("_")
     op = parts[0]
-    if op not in ("conv2d", "dense", "qdense", "add"):
+    if op == "logits":
+        drafts.rules_of(name)
+        return op, False, False, None
+    if op not in ("conv2d", "dense", "qdense", "mxdense", "add"):
         raise ValueError("unknown composite %r" % name)
     rest = parts[1:]
     act = None
@@ -107,12 +115,14 @@ def run_node(node, args, mode="bf16io"):
     dtype = node.get("out_dtype", "f32")
     op, has_bias, has_add, act = parse_composite(name)
     args = [np.asarray(a, dtype=np.float64) for a in args]
-    if op in ("conv2d", "dense", "qdense"):
+    if op in ("conv2d", "dense", "qdense", "mxdense"):
         x, w = args[0], args[1]
-        if dtype == "bf16" and op != "qdense":
+        if dtype == "bf16" and op in ("conv2d", "dense"):
             w = round_bf16(w)
         if op == "qdense":
             y = transformer.qdense(x, w)
+        elif op == "mxdense":
+            y = drafts.mxdense(x, w)
         elif op == "conv2d":
             y = ops.conv2d(x, w, tuple(attrs.get("strides", (1, 1))),
                            tuple(attrs.get("padding", (0, 0, 0, 0))),
@@ -141,6 +151,10 @@ def run_node(node, args, mode="bf16io"):
         y = transformer.rotary(attrs, args[0], args[-1], args[1:-1] if op == "qk_norm_rotary" else None)
     elif op in ("attention", "attention_lengths"):
         y = transformer.attention(attrs, *args)
+    elif op == "attention_tree":
+        y = drafts.attention_tree(attrs, *args)
+    elif op == "logits":
+        y = drafts.logits(name, attrs, *args)
     elif op == "concatenate":
         y = ops.concatenate(args, axis=1)
     else:
@@ -171,6 +185,7 @@ def run_graph(graph, consts, inputs, mode="bf16io", keep=False):
     """
     g = load_graph(graph)
     vals = {}
+    params = {n for node in g["nodes"] for n in drafts.float_params(node)}
     if len(inputs) != len(g["inputs"]):
         raise ValueError("expected %d inputs" % len(g["inputs"]))
     for desc, arr in zip(g["inputs"], inputs):
@@ -178,6 +193,8 @@ def run_graph(graph, consts, inputs, mode="bf16io", keep=False):
         if list(a.shape) != list(desc["shape"]):
             raise ValueError("input %s: shape %s != %s" % (desc["name"], a.shape, desc["shape"]))
         consumer = _graph_dtype_of_consumers(g, desc["name"])
+        if desc["name"] in params:  # (strengths and biases of logits are read as they come)
+            consumer = None
         if desc.get("dtype") != "i32" and (desc.get("dtype") == "bf16" or consumer == "bf16"):
             a = round_bf16(a)
         vals[desc["name"]] = a

@@ -17,7 +17,7 @@ BYOC_OK = 0
 F32, BF16, I32 = 0, 1, 3
 NCHW, NHWC, ROWMAJOR = 0, 1, 2
 KIND_NAMES = ["conv_mfma", "conv_f32", "depthwise", "maxpool", "avgpool", "add", "transform",
-              "reduce", "conv_i8", "qdense", "rotary", "attention"]
+              "reduce", "conv_i8", "qdense", "rotary", "attention", "mxdense", "logits"]
 STATUS_NAMES = ["OK", "INVALID_ARG", "PARSE", "UNSUPPORTED", "SHAPE", "DEVICE", "OOM", "INTERNAL"]
 
 # Every entry point declared in include/byoc.h.

@@ -16,12 +16,16 @@
 // halves of the wave, and its result is, in place, the right operand of
 // O^T = V^T P^T: register group i of a lane half h holds keys 8 (i / 4) + 4 h + i % 4,
 // and V^T is read in the same order (the order of a sum over keys is free).
+//
+// A tree of drafted tokens (TREE): the key axis is the cache's tiles, which every row sees,
+// and then the drafted keys' tiles, where each row has a bit for a key (tree_paths.h).
 #include <algorithm>
 #include <climits>
 #include <cmath>
 #include <type_traits>
 
 #include "lds_dma.h"
+#include "tree_paths.h"
 
 namespace byoc {
 namespace {
@@ -63,6 +67,24 @@ __device__ __forceinline__ int batch_len(const AttnParams& p, int b) {
   return p.lengths ? min(max(p.lengths[b], 0), p.k_len) : p.k_len;
 }
 
+// Tiles of the key axis of a sequence: of its keys and, after them, of a tree's drafted keys.
+__device__ __forceinline__ int key_tiles(int keys, int per) { return (keys + per - 1) / per; }
+template <bool TREE>
+__device__ __forceinline__ int batch_tiles(const AttnParams& p, int b) {
+  return key_tiles(batch_len(p, b), p.tile_keys) + (TREE ? key_tiles(p.q_len, p.tile_keys) : 0);
+}
+
+// A tree's rows: its paths in LDS, which the workgroup forms where it has drafted keys, and this lane's query.
+constexpr int kTreeWords = tree_lds_bytes(kMaxTree) / 4;
+struct TreeRow {
+  TreePaths paths;
+  int query;  // -1: none, a row past the last
+  // bit k: drafted key 32 w + k is on the row's path
+  __device__ __forceinline__ uint32_t word(int w) const { return query >= 0 && w < paths.words ? paths.word(query, w) : 0u; }
+};
+// The bits of a tile of 32 of the first n keys.
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? ~0u : n > 0 ? (1u << n) - 1u : 0u; }
+
 // The key axis of few rows is split into p.chunks chunks, shared by the sequences in
 // proportion to their lengths, which only the device knows: chunks of `size` tiles each,
 // the first of sequence b number `first`, `count` of them, with the least size that needs
@@ -76,9 +98,10 @@ __host__ __device__ __forceinline__ int64_t head_floats(const AttnParams& p) { r
 struct Chunks {
   int first, count, size;
 };
+template <bool TREE>
 __device__ __forceinline__ Chunks lane_chunks(const AttnParams& p) {
   const int lane = threadIdx.x & 63;
-  const int mine = lane < p.batch ? (batch_len(p, lane) + p.tile_keys - 1) / p.tile_keys : 0;
+  const int mine = lane < p.batch ? batch_tiles<TREE>(p, lane) : 0;
   int total = mine;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d, 64);
@@ -107,19 +130,21 @@ __device__ __forceinline__ Chunks lane_chunks(const AttnParams& p) {
   c.first -= c.count;
   return c;
 }
+template <bool TREE>
 __device__ __forceinline__ Chunks uniform_chunks(const AttnParams& p, int b) {
   const int per = p.chunks / p.batch;
-  const int tiles = (p.k_len + p.tile_keys - 1) / p.tile_keys;
+  const int tiles = key_tiles(p.k_len, p.tile_keys) + (TREE ? key_tiles(p.q_len, p.tile_keys) : 0);
   return Chunks{b * per, per, (tiles + per - 1) / per};
 }
 // The sequence of chunk q, -1 if no sequence needs it.
+template <bool TREE>
 __device__ __forceinline__ int chunk_batch(const AttnParams& p, int q, Chunks* out) {
   if (p.batch > 64 || p.chunks == p.batch) {
     const int b = q / (p.chunks / p.batch);
-    *out = uniform_chunks(p, b);
+    *out = uniform_chunks<TREE>(p, b);
     return b;
   }
-  const Chunks c = lane_chunks(p);
+  const Chunks c = lane_chunks<TREE>(p);
   const unsigned long long at = __ballot(q >= c.first && q < c.first + c.count);
   if (at == 0) return -1;
   const int b = __builtin_ctzll(at);
@@ -244,15 +269,16 @@ __device__ __forceinline__ void load4(const float* p, float* v) {
   v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
 }
 
-// Adds keys j0 .. j1 - 1 to each row that sees them.
-template <typename T, int DB, int QS>
+// Adds keys j0 .. j1 - 1 to each row that sees them: the keys below its limit (of a tree: those on its path).
+template <typename T, int DB, int QS, bool TREE = false>
 __device__ __forceinline__ void add_keys(const AttnParams& p, const char* kb, const char* vb, int64_t sk, int64_t sv, int lim,
-                                         int j0, int j1, const uint4* qf, float c2, f32x16* o, float& m, float& l) {
+                                         int j0, int j1, const uint4* qf, float c2, f32x16* o, float& m, float& l,
+                                         const TreeRow* tree = nullptr) {
   constexpr int PER = 16 / sizeof(T);  // values of a 16-byte chunk
   const int h = (threadIdx.x & 63) >> 5;
 #pragma unroll 1
   for (int j = j0; j < j1 && __any(j < lim); ++j) {
-    const bool seen = j < lim;
+    const bool seen = TREE ? j < lim && (tree->word(j >> 5) >> (j & 31) & 1u) : j < lim;
     const T* const kr = (const T*)(kb + (int64_t)j * sk) + h * PER;
     const T* const vr = (const T*)(vb + (int64_t)j * sv) + 4 * h;
     float s = 0.0f;
@@ -298,7 +324,7 @@ __device__ __forceinline__ void add_keys(const AttnParams& p, const char* kb, co
 // 5.0 TB/s.
 //
 // DP columns of a head in LDS (a power of two), DC of them multiplied.
-template <typename T, int DP, int DC, int NW>
+template <typename T, int DP, int DC, int NW, bool TREE>
 __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int ES = sizeof(T);
@@ -310,7 +336,8 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   constexpr int DB = DC / 32;         // 32-column blocks of the output
   __shared__ __align__(16) char lds[NW * NBUF * 2 * TILE];
   __shared__ float ml[NW][2][kCols];
-  static_assert(sizeof(lds) + sizeof(ml) <= kLdsLimit, "LDS");
+  __shared__ uint32_t tree_lds[TREE ? kTreeWords : 1];
+  static_assert(sizeof(lds) + sizeof(ml) + sizeof(tree_lds) <= kLdsLimit, "LDS");
   static_assert(NW * NBUF * 2 * TILE >= NW * DC * kPitch * 4, "the waves' results take the tiles' place");
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
@@ -322,7 +349,7 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   const int cb = ncb - 1 - rest % ncb, chunk = rest / ncb;  // (the last rows, which see the most keys, first)
   const bool joined = p.chunks > p.batch;
   Chunks ck;
-  const int b = uniform(chunk_batch(p, chunk, &ck));
+  const int b = uniform(chunk_batch<TREE>(p, chunk, &ck));
   if (b < 0) return;
   if (joined && cb == 0 && kh == 0) note_chunks(p, b, chunk, ck);
   const int len = uniform(batch_len(p, b));
@@ -331,7 +358,10 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   const int lim_lo = uniform(seen_keys(p, len, cb * kCols));  // (rows see more keys further down)
   const int kend = uniform(seen_keys(p, len, min(cb * kCols + kCols, R) - 1));
   const int t0 = (chunk - ck.first) * ck.size;
-  const int t_end = min(t0 + ck.size, (kend + kKeys - 1) / kKeys);
+  // (a tree: drafted keys from tile t_tree on, a row's own the last it sees)
+  const int t_tree = key_tiles(len, kKeys);
+  const int t_end = min(t0 + ck.size, TREE ? t_tree + key_tiles((min(cb * kCols + kCols, R) - 1) / p.group + 1, kKeys)
+                                           : key_tiles(kend, kKeys));
 
   // this lane's part of its query row: 16-byte chunks 2 st + h
   constexpr int QS = DC * ES / 32;
@@ -349,14 +379,19 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   const int64_t sk = p.ldk * ES, sv = p.ldv * ES;
   const char* kb = (const char*)p.k + (int64_t)b * p.k_len * sk + kh * p.D * ES;
   const char* vb = (const char*)p.v + (int64_t)b * p.k_len * sv + kh * p.D * ES;
+  const int64_t sk2 = p.ldk2 * ES, sv2 = p.ldv2 * ES;
+  const char* kb2 = TREE ? (const char*)p.k2 + (int64_t)b * p.q_len * sk2 + kh * p.D * ES : nullptr;
+  const char* vb2 = TREE ? (const char*)p.v2 + (int64_t)b * p.q_len * sv2 + kh * p.D * ES : nullptr;
   char* mine = lds + wave * (NBUF * 2 * TILE);
   // keys or values of a tile; rows past the length (and tiles past the end) read as zeros, whatever stands there
   auto fill = [&](int buf, int t, auto values_tag) {
     constexpr bool VALUES = decltype(values_tag)::value;
-    const int k0 = t * kKeys;
-    const int n = t < t_end ? min(kKeys, len - k0) : 0;
-    const int64_t stride = VALUES ? sv : sk;
-    const i32x4 r4 = buffer_rsrc((VALUES ? vb : kb) + (int64_t)k0 * stride, n > 0 ? (n - 1) * (int)stride + p.D * ES : 0);
+    const bool drafted = TREE && t >= t_tree;
+    const int k0 = (drafted ? t - t_tree : t) * kKeys;
+    const int n = t < t_end ? min(kKeys, (drafted ? p.q_len : len) - k0) : 0;
+    const int64_t stride = drafted ? (VALUES ? sv2 : sk2) : VALUES ? sv : sk;
+    const char* const base = drafted ? (VALUES ? vb2 : kb2) : VALUES ? vb : kb;
+    const i32x4 r4 = buffer_rsrc(base + (int64_t)k0 * stride, n > 0 ? (n - 1) * (int)stride + p.D * ES : 0);
     const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(mine + (buf * 2 + VALUES) * TILE));
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -378,7 +413,9 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   for (int d = 0; d < DB; ++d) o[d] = f32x16{};
   float m = -INFINITY, l = 0.0f;
   const float c2 = p.scale * 1.44269504088896340736f;
-  const int masked = p.causal && p.q_len > 1 ? lim_lo / kKeys : INT_MAX;  // the first tile that some rows see a part of
+  // the first tile that some rows see a part of
+  const int masked = TREE ? t_tree : p.causal && p.q_len > 1 ? lim_lo / kKeys : INT_MAX;
+  TreeRow tree{};
 
   // Loads of 2 NBUF half tiles are in flight: a half is filled again as soon as it has been read.
   auto landed = [] { asm volatile("s_waitcnt vmcnt(%0)" ::"n"((2 * NBUF - 1) * NI) : "memory"); };
@@ -402,10 +439,12 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
     read();
     fill(buf, t + NBUF * NW, keys);
     const int k0 = t * kKeys + 4 * h;
+    const uint32_t bits = TREE ? (t < t_tree ? first_bits(lim - t * kKeys) : tree.word(t - t_tree)) >> (4 * h) : 0u;
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      s[i] = k0 + 8 * (i >> 2) + (i & 3) < lim ? s[i] * c2 : -INFINITY;
+      const int at = 8 * (i >> 2) + (i & 3);
+      s[i] = (TREE ? (bits >> at & 1u) != 0u : k0 + at < lim) ? s[i] * c2 : -INFINITY;
       top = fmaxf(top, s[i]);
     }
     const float mn = fmaxf(m, half_max(top));
@@ -454,6 +493,10 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
     fill(n, t0 + wave + n * NW, keys);
     fill(n, t0 + wave + n * NW, values);
   }
+  if constexpr (TREE) {
+    if (t_end > t_tree) tree.paths = form_paths<64 * NW>(p.parents + (int64_t)b * p.q_len, p.q_len, tree_lds);
+    tree.query = row < R ? row / p.group : -1;
+  }
   int buf = 0, t = t0 + wave;
   for (; t < t_end; t += NW) {
     if (t >= masked) {
@@ -467,7 +510,13 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
-  for (; t < t_end; t += NW) add_keys<T, DB, QS>(p, kb, vb, sk, sv, lim, t * kKeys, (t + 1) * kKeys, qf, c2, o, m, l);
+  for (; t < t_end; t += NW) {
+    if constexpr (TREE)
+      add_keys<T, DB, QS, true>(p, kb2, vb2, sk2, sv2, p.q_len, (t - t_tree) * kKeys, (t - t_tree + 1) * kKeys, qf, c2, o, m, l,
+                                &tree);
+    else
+      add_keys<T, DB, QS>(p, kb, vb, sk, sv, lim, t * kKeys, (t + 1) * kKeys, qf, c2, o, m, l);
+  }
 
   // the waves' results: a common maximum, then the sums in wave order
   l = half_sum(l);
@@ -519,7 +568,7 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
       continue;
     }
     const float sum = ml[0][1][c];
-    const bool any = seen_keys(p, len, r) > 0;
+    const bool any = TREE || seen_keys(p, len, r) > 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = any ? v[j] / sum : 0.0f;
     const int i = r / p.group, g = r - i * p.group;
@@ -537,6 +586,7 @@ struct Place {
   int b, kh, chunk, tile;  // b < 0: nothing
   Chunks ck;
 };
+template <bool TREE>
 __device__ __forceinline__ Place place(const AttnParams& p, int rows) {
   const int nh = p.chunks * p.kv_heads;
   const int nt = (p.q_len * p.group + rows - 1) / rows;
@@ -547,7 +597,7 @@ __device__ __forceinline__ Place place(const AttnParams& p, int rows) {
     w.tile = rem / p.kv_heads;
     w.kh = rem - w.tile * p.kv_heads;
     w.b = w.chunk = uniform(nth_longest(p, pos));
-    w.ck = uniform_chunks(p, w.b);
+    w.ck = uniform_chunks<TREE>(p, w.b);
     return w;
   }
   // Head fastest: with a multiple of 8 heads each XCD (workgroup b runs on XCD b % 8) keeps to its own
@@ -556,7 +606,7 @@ __device__ __forceinline__ Place place(const AttnParams& p, int rows) {
   w.tile = nt - 1 - blockIdx.x / nh;
   w.chunk = bh / p.kv_heads;
   w.kh = bh - w.chunk * p.kv_heads;
-  w.b = uniform(chunk_batch(p, w.chunk, &w.ck));
+  w.b = uniform(chunk_batch<TREE>(p, w.chunk, &w.ck));
   return w;
 }
 
@@ -577,7 +627,7 @@ constexpr float kSlack = 8.0f;
 //
 // DP columns of a head in LDS (a power of two), DC of them multiplied (causal 2 x 2048, 20 heads over 4 of 80:
 // 48.7 us with all 128, 43.2 with 96).
-template <int DP, int DC, int KS>
+template <int DP, int DC, int KS, bool TREE>
 __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_kernel(AttnParams p) {
   constexpr int NW = 4 / KS;  // waves along the rows
   constexpr int RB = DP * 2, CPR = RB / 16;
@@ -586,13 +636,14 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   constexpr int DB = DC / 32, QS = DC / 16, KB = kTileKeys / 32;
   static_assert(DC % 32 == 0 && DC <= DP, "columns multiplied");
   __shared__ __align__(1024) char lds[KS * 4 * TILE];
-  static_assert(sizeof(lds) <= kLdsLimit, "LDS");
+  __shared__ uint32_t tree_lds[TREE ? kTreeWords : 1];
+  static_assert(sizeof(lds) + sizeof(tree_lds) <= kLdsLimit / (DP * KS <= 128 ? 2 : 1), "LDS");
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int wave = uniform((tid >> 6) % NW), kg = uniform((tid >> 6) / NW);  // place among the rows; key group
   const int R = p.q_len * p.group;
   const bool joined = p.chunks > p.batch;
-  const Place pl = place(p, 32 * NW);
+  const Place pl = place<TREE>(p, 32 * NW);
   const int b = pl.b, kh = pl.kh, chunk = pl.chunk, tile = pl.tile;
   const Chunks ck = pl.ck;
   if (b < 0) return;
@@ -604,7 +655,10 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   const int lim_hi = uniform(row0 < R ? seen_keys(p, len, min(row0 + 32, R) - 1) : 0);
   const int kend = uniform(seen_keys(p, len, min((tile + 1) * 32 * NW, R) - 1));
   const int t0 = (chunk - ck.first) * ck.size;
-  const int t_end = min(t0 + ck.size, (kend + kTileKeys - 1) / kTileKeys);
+  // (a tree: drafted keys from tile t_tree on, a row's own the last it sees)
+  const int t_tree = key_tiles(len, kTileKeys);
+  auto last_drafted = [&](int rows) { return t_tree + key_tiles((min(rows, R) - 1) / p.group + 1, kTileKeys); };
+  const int t_end = min(t0 + ck.size, TREE ? last_drafted((tile + 1) * 32 * NW) : key_tiles(kend, kTileKeys));
 
   uint4 qf[QS];
   const int i = row / p.group, g = row - i * p.group;
@@ -620,6 +674,9 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   const int64_t sk = p.ldk * 2, sv = p.ldv * 2;
   const char* kb = (const char*)p.k + (int64_t)b * p.k_len * sk + kh * p.D * 2;
   const char* vb = (const char*)p.v + (int64_t)b * p.k_len * sv + kh * p.D * 2;
+  const int64_t sk2 = p.ldk2 * 2, sv2 = p.ldv2 * 2;
+  const char* kb2 = TREE ? (const char*)p.k2 + (int64_t)b * p.q_len * sk2 + kh * p.D * 2 : nullptr;
+  const char* vb2 = TREE ? (const char*)p.v2 + (int64_t)b * p.q_len * sv2 + kh * p.D * 2 : nullptr;
   uint32_t ko[NI], vo[NI];
 #pragma unroll
   for (int n = 0; n < NI; ++n) {
@@ -645,16 +702,41 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   const char *kp = kb + (int64_t)first * kTileKeys * sk, *vp = vb + (int64_t)first * kTileKeys * sv;
   const int rest = t_end > first ? min(len, t_end * kTileKeys) - first * kTileKeys : 0;  // keys from there on
   int k_left = rest, v_left = rest;
-  auto fill_k = [&](auto par_tag) { fill(kp, sk, k_left, ko, lds0 + decltype(par_tag)::value * TILE); };
-  auto fill_v = [&](auto par_tag) { fill(vp, sv, v_left, vo, lds0 + (2 + decltype(par_tag)::value) * TILE); };
+  // (a tree's drafted tiles, of rows any distance apart: their offsets are formed where they are used)
+  int k_at = first, v_at = first;  // the tiles that come next
+  auto fill_drafted = [&](const char* base, int64_t stride, int t, auto values_tag, uint32_t at) {
+    constexpr bool VALUES = decltype(values_tag)::value;
+    const int j0 = (t - t_tree) * kTileKeys, valid = t < t_end ? min(kTileKeys, p.q_len - j0) : 0;
+    const i32x4 r4 = buffer_rsrc(base + j0 * stride, valid > 0 ? (valid - 1) * (int)stride + p.D * 2 : 0);
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      const int x = (n * NW + wave) * 64 + lane, r = x / CPR;
+      const int c = x % CPR ^ (VALUES ? v_key<CPR>(r) : k_key<CPR>(r));
+      lds_fill16(r4, at + n * NW * 1024, c * 8 < p.D ? (uint32_t)(r * (int)stride + c * 16) : kOOB);
+    }
+  };
+  auto fill_k = [&](auto par_tag) {
+    const uint32_t at = lds0 + decltype(par_tag)::value * TILE;
+    if (TREE && k_at >= t_tree) fill_drafted(kb2, sk2, k_at, std::false_type{}, at);
+    else fill(kp, sk, k_left, ko, at);
+    k_at += KS;
+  };
+  auto fill_v = [&](auto par_tag) {
+    const uint32_t at = lds0 + (2 + decltype(par_tag)::value) * TILE;
+    if (TREE && v_at >= t_tree) fill_drafted(vb2, sv2, v_at, std::true_type{}, at);
+    else fill(vp, sv, v_left, vo, at);
+    v_at += KS;
+  };
 
   f32x16 o[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d) o[d] = f32x16{};
   float m = -INFINITY, l = 0.0f;
   const float c2 = p.scale * 1.44269504088896340736f;
-  const int t_wave = min(t_end, (lim_hi + kTileKeys - 1) / kTileKeys);  // tiles that this wave's rows see
-  const int masked = p.causal && p.q_len > 1 ? lim_lo / kTileKeys : INT_MAX;  // the first that some rows see a part of
+  // tiles that this wave's rows see, and the first that some rows see a part of
+  const int t_wave = min(t_end, TREE ? (row0 < R ? last_drafted(row0 + 32) : 0) : key_tiles(lim_hi, kTileKeys));
+  const int masked = TREE ? t_tree : p.causal && p.q_len > 1 ? lim_lo / kTileKeys : INT_MAX;
+  TreeRow tree{};
   int stop = t_wave;                                                          // the tiles from there on are left to add_keys
 
   // LDS offsets of this lane's operands in a tile: its key row at chunk h, whose other chunks are an XOR
@@ -718,7 +800,15 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
     kf[0] = read_k(other, c0);
     kf[1] = read_k(other, c1);
     const int k0 = t * kTileKeys;
-    if (k0 + kTileKeys > lim_lo) {
+    if (TREE && t >= t_tree) {
+#pragma unroll
+      for (int n = 0; n < KB; ++n) {
+        const uint32_t bits = tree.word((t - t_tree) * KB + n) >> (4 * h);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!(bits >> (8 * (e >> 2) + (e & 3)) & 1u)) s[n][e] = -INFINITY;
+      }
+    } else if (k0 + kTileKeys > lim_lo) {
 #pragma unroll
       for (int n = 0; n < KB; ++n)
 #pragma unroll
@@ -785,6 +875,10 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   constexpr std::integral_constant<int, 1> odd{};
   f32x16 sa[KB], sb[KB];
   fill_k(even);
+  if constexpr (TREE) {
+    if (t_end > t_tree) tree.paths = form_paths<256>(p.parents + (int64_t)b * p.q_len, p.q_len, tree_lds);
+    tree.query = row < R ? i : -1;
+  }
   asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
   fill_k(odd);
   fill_v(even);
@@ -801,8 +895,13 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
     if (t + KS + kg < stop) step(t + KS + kg, odd, sb, sa);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  for (; stop < t_wave; stop += KS)
-    add_keys<bf16_t, DB, QS>(p, kb, vb, sk, sv, lim, stop * kTileKeys, (stop + 1) * kTileKeys, qf, c2, o, m, l);
+  for (; stop < t_wave; stop += KS) {
+    if constexpr (TREE)
+      add_keys<bf16_t, DB, QS, true>(p, kb2, vb2, sk2, sv2, p.q_len, (stop - t_tree) * kTileKeys,
+                                     (stop - t_tree + 1) * kTileKeys, qf, c2, o, m, l, &tree);
+    else
+      add_keys<bf16_t, DB, QS>(p, kb, vb, sk, sv, lim, stop * kTileKeys, (stop + 1) * kTileKeys, qf, c2, o, m, l);
+  }
   l = half_sum(l);
   if constexpr (KS > 1) {
     // the second key group hands its results over, lane by lane, in the place of the tiles
@@ -860,7 +959,7 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int at = 4 * (e + k) + 2 * j;
-          w[k][j] = lim > 0 ? pack2_bf16(o[d][at] * inv, o[d][at + 1] * inv) : 0u;
+          w[k][j] = TREE || lim > 0 ? pack2_bf16(o[d][at] * inv, o[d][at + 1] * inv) : 0u;
         }
       const u32x2 lo = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
       const u32x2 hi = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
@@ -873,7 +972,7 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
 // LDS, a tile's loads running while the one before is multiplied; bound by the fp32 matrix cores (4096 cycles a
 // tile of 64 columns, beside which the softmax is short).  The key axes are not split: choose_attention
 // comes here where there are rows enough (16 x 300 over 200, 12 of 128: 105 us, 56 TFLOP/s).
-template <int DP, int DC>
+template <int DP, int DC, bool TREE>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_kernel(AttnParams p) {
   constexpr int NW = 4;
   constexpr int RB = DP * 4, CPR = RB / 16;
@@ -881,12 +980,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
   constexpr int NI = TILE / (NW * 1024);  // loads of a tile per lane
   constexpr int DB = DC / 32, QS = DC / 8;
   __shared__ __align__(1024) char lds[4 * TILE];  // keys, values, keys, values
-  static_assert(sizeof(lds) <= kLdsLimit, "LDS");
+  __shared__ uint32_t tree_lds[TREE ? kTreeWords : 1];
+  static_assert(sizeof(lds) + sizeof(tree_lds) <= kLdsLimit / (DP <= 128 ? 2 : 1), "LDS");
 
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, h = lane >> 5;
   const int wave = uniform(tid >> 6);
   const int R = p.q_len * p.group;
-  const Place pl = place(p, 32 * NW);
+  const Place pl = place<TREE>(p, 32 * NW);
   const int b = pl.b, kh = pl.kh, tile = pl.tile;
   const int len = uniform(batch_len(p, b));
   const int row0 = tile * 32 * NW + wave * 32, row = row0 + col;
@@ -894,8 +994,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
   const int lim_lo = uniform(seen_keys(p, len, min(row0, R - 1)));  // (rows see more keys further down)
   const int lim_hi = uniform(row0 < R ? seen_keys(p, len, min(row0 + 32, R) - 1) : 0);
   const int kend = uniform(seen_keys(p, len, min((tile + 1) * 32 * NW, R) - 1));
-  const int t_end = (kend + kKeys - 1) / kKeys;
-  const int t_wave = min(t_end, (lim_hi + kKeys - 1) / kKeys);  // tiles that this wave's rows see
+  // (a tree: drafted keys from tile t_tree on, a row's own the last it sees)
+  const int t_tree = key_tiles(len, kKeys);
+  auto last_drafted = [&](int rows) { return t_tree + key_tiles((min(rows, R) - 1) / p.group + 1, kKeys); };
+  const int t_end = TREE ? last_drafted((tile + 1) * 32 * NW) : key_tiles(kend, kKeys);
+  // tiles that this wave's rows see
+  const int t_wave = min(t_end, TREE ? (row0 < R ? last_drafted(row0 + 32) : 0) : key_tiles(lim_hi, kKeys));
 
   uint4 qf[QS];
   const int i = row / p.group, g = row - i * p.group;
@@ -910,19 +1014,24 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
   const int64_t sk = p.ldk * 4, sv = p.ldv * 4;
   const char* kb = (const char*)p.k + (int64_t)b * p.k_len * sk + kh * p.D * 4;
   const char* vb = (const char*)p.v + (int64_t)b * p.k_len * sv + kh * p.D * 4;
+  const int64_t sk2 = p.ldk2 * 4, sv2 = p.ldv2 * 4;
+  const char* kb2 = TREE ? (const char*)p.k2 + (int64_t)b * p.q_len * sk2 + kh * p.D * 4 : nullptr;
+  const char* vb2 = TREE ? (const char*)p.v2 + (int64_t)b * p.q_len * sv2 + kh * p.D * 4 : nullptr;
   const uint32_t lds0 = uniform(lds_addr(lds)) + wave * 1024;
   // a tile of keys and values; rows past the length (and tiles past the end) read as zeros, whatever stands there
   auto fill = [&](int par, int t) {
-    const int64_t k0 = (int64_t)t * kKeys;
-    const int n = t < t_end ? min(kKeys, len - t * kKeys) : 0;
-    const i32x4 rk = buffer_rsrc(kb + k0 * sk, n > 0 ? (n - 1) * (int)sk + p.D * 4 : 0);
-    const i32x4 rv = buffer_rsrc(vb + k0 * sv, n > 0 ? (n - 1) * (int)sv + p.D * 4 : 0);
+    const bool drafted = TREE && t >= t_tree;
+    const int k0 = (drafted ? t - t_tree : t) * kKeys;
+    const int n = t < t_end ? min(kKeys, (drafted ? p.q_len : len) - k0) : 0;
+    const int64_t ks = drafted ? sk2 : sk, vs = drafted ? sv2 : sv;
+    const i32x4 rk = buffer_rsrc((drafted ? kb2 : kb) + k0 * ks, n > 0 ? (n - 1) * (int)ks + p.D * 4 : 0);
+    const i32x4 rv = buffer_rsrc((drafted ? vb2 : vb) + k0 * vs, n > 0 ? (n - 1) * (int)vs + p.D * 4 : 0);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const int at = (j * NW + wave) * 64 + lane, r = at / CPR, x = at % CPR;
       const int ck = x ^ k_key<CPR>(r), cv = x ^ v_key<CPR>(r);
-      lds_fill16(rk, lds0 + par * 2 * TILE + j * NW * 1024, ck * 4 < p.D ? (uint32_t)(r * (int)sk + ck * 16) : kOOB);
-      lds_fill16(rv, lds0 + (par * 2 + 1) * TILE + j * NW * 1024, cv * 4 < p.D ? (uint32_t)(r * (int)sv + cv * 16) : kOOB);
+      lds_fill16(rk, lds0 + par * 2 * TILE + j * NW * 1024, ck * 4 < p.D ? (uint32_t)(r * (int)ks + ck * 16) : kOOB);
+      lds_fill16(rv, lds0 + (par * 2 + 1) * TILE + j * NW * 1024, cv * 4 < p.D ? (uint32_t)(r * (int)vs + cv * 16) : kOOB);
     }
   };
 
@@ -937,8 +1046,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
   for (int d = 0; d < DB; ++d) o[d] = f32x16{};
   float m = -INFINITY, l = 0.0f;
   const float c2 = p.scale * 1.44269504088896340736f;
-  const int masked = p.causal && p.q_len > 1 ? lim_lo / kKeys : INT_MAX;  // the first tile that some rows see a part of
-  int stop = t_wave;                                                      // the tiles from there on are left to add_keys
+  // the first tile that some rows see a part of
+  const int masked = TREE ? t_tree : p.causal && p.q_len > 1 ? lim_lo / kKeys : INT_MAX;
+  int stop = t_wave;  // the tiles from there on are left to add_keys
+  TreeRow tree{};
   auto compute = [&](int par, int t) {
     const char* kt = lds + par * 2 * TILE;
     const char* vt = kt + TILE;
@@ -951,10 +1062,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
       for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], q[e], s, 0, 0, 0);
     }
     const int k0 = t * kKeys + 4 * h;
+    const uint32_t bits = TREE ? (t < t_tree ? first_bits(lim - t * kKeys) : tree.word(t - t_tree)) >> (4 * h) : 0u;
     float top = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      s[e] = k0 + 8 * (e >> 2) + (e & 3) < lim ? s[e] * c2 : -INFINITY;
+      const int at = 8 * (e >> 2) + (e & 3);
+      s[e] = (TREE ? (bits >> at & 1u) != 0u : k0 + at < lim) ? s[e] * c2 : -INFINITY;
       top = fmaxf(top, s[e]);
     }
     const float mn = fmaxf(m, half_max(top));
@@ -982,6 +1095,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
   };
 
   fill(0, 0);
+  if constexpr (TREE) {
+    tree.paths = form_paths<256>(p.parents + (int64_t)b * p.q_len, p.q_len, tree_lds);
+    tree.query = row < R ? i : -1;
+  }
   for (int t = 0, par = 0; t < t_end; ++t, par ^= 1) {
     // tile t has landed for every wave, and every wave is done with the one before, whose place t + 1 takes
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -990,8 +1107,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
     if (t < stop) compute(par, t);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  for (; stop < t_wave; ++stop)
-    add_keys<float, DB, QS>(p, kb, vb, sk, sv, lim, stop * kKeys, (stop + 1) * kKeys, qf, c2, o, m, l);
+  for (; stop < t_wave; ++stop) {
+    if constexpr (TREE)
+      add_keys<float, DB, QS, true>(p, kb2, vb2, sk2, sv2, p.q_len, (stop - t_tree) * kKeys, (stop - t_tree + 1) * kKeys, qf,
+                                    c2, o, m, l, &tree);
+    else
+      add_keys<float, DB, QS>(p, kb, vb, sk, sv, lim, stop * kKeys, (stop + 1) * kKeys, qf, c2, o, m, l);
+  }
   l = half_sum(l);
   if (row >= R) return;
   // (a row without keys is zero; one whose seen scores are all -inf divides zero by zero, as the softmax does)
@@ -1003,7 +1125,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
       const int c = d * 32 + 8 * e + 4 * h;
       float v[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = lim > 0 ? o[d][4 * e + j] / l : 0.0f;
+      for (int j = 0; j < 4; ++j) v[j] = TREE || lim > 0 ? o[d][4 * e + j] / l : 0.0f;
       if (c < p.D) *(float4*)(y + c) = make_float4(v[0], v[1], v[2], v[3]);
     }
 }
@@ -1018,7 +1140,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p, int l
   // rows of one sequence per workgroup row (blockIdx.y), so that a wave has one set of chunks
   const int b = blockIdx.y;
   const int len = batch_len(p, b);
-  const int2 ck = len > 0 ? ((const int2*)p.ws)[b] : make_int2(0, 0);  // first chunk, count
+  const int2 ck = len > 0 || p.tree ? ((const int2*)p.ws)[b] : make_int2(0, 0);  // first chunk, count
   const int slot = threadIdx.x / lanes, g0 = slot % split;
   const int at = blockIdx.x * (256 / lanes / split) + slot / split;  // (key head, packed row)
   const int c = threadIdx.x % lanes * 4;
@@ -1078,7 +1200,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p, int l
     }
   }
   if (!live) return;
-  const bool any = seen_keys(p, len, row) > 0;
+  const bool any = p.tree || seen_keys(p, len, row) > 0;
   const int i = row / p.group, g = row - i * p.group;
   const int64_t out = (b * (int64_t)p.q_len + i) * p.ldy + (kh * p.group + g) * p.D + c;
 #pragma unroll
@@ -1106,11 +1228,12 @@ int row_blocks(const AttnParams& p) {
 int split_tiles(const AttnParams& p, int64_t blocks) {
   const double tile = p.D <= 64 ? 0.4 : p.D <= 96 ? 0.93 : p.D <= 128 ? 1.03 : p.D <= 192 ? 2.1 : 2.65;
   const double shared = p.D <= 64 ? 1.0 : 0.4;  // (at 64 columns, which the vector ALU bounds, a second workgroup gains nothing)
-  const double tiles = ceil_div(p.k_len, kTileKeys);
+  const int64_t keys = p.k_len + (p.tree ? p.q_len : 0);
+  const double tiles = ceil_div(keys, kTileKeys);
   const double part = 8e-6 / 4.1 * p.D * p.batch * p.kv_heads * p.q_len * p.group;  // a chunk's sums, written and read
   int best = 1;
   double least = INFINITY;
-  const int64_t most = std::min<int64_t>((p.D > 128 ? 256 : 512) / blocks, ceil_div(p.k_len, 4 * kTileKeys));
+  const int64_t most = std::min<int64_t>((p.D > 128 ? 256 : 512) / blocks, ceil_div(keys, 4 * kTileKeys));
   for (int n = 1; n <= most; ++n) {
     const double t = tiles / n * tile * (1.0 + shared * std::max(0.0, blocks * n / 256.0 - 1.0)) + (n > 1 ? 6.0 + part * n : 0.0);
     if (t < least) least = t, best = n;
@@ -1126,8 +1249,9 @@ int split_tiles(const AttnParams& p, int64_t blocks) {
 // 512, 12 of 64, 84, 77; 4 x 512 over 256, 8 of 128, 45, 36).
 void choose_attention(AttnParams& p) {
   const int64_t rows = p.q_len * (int64_t)p.group;
+  const int64_t keys = p.k_len + (p.tree ? p.q_len : 0);
   const int64_t quads = (int64_t)p.batch * p.kv_heads * ceil_div(rows, 128);
-  const bool tiled = rows > 32 && (!p.f32 || quads >= (p.D <= 64 ? 512 : 256) || (p.k_len <= 4 * kKeys && quads >= 128));
+  const bool tiled = rows > 32 && (!p.f32 || quads >= (p.D <= 64 ? 512 : 256) || (keys <= 4 * kKeys && quads >= 128));
   // Up to 64 columns a head, two waves along the rows and two along the keys where 128-row workgroups would
   // not fill the chip twice: causal 1 x 2048, 16 heads of 64: 30.5 us as 256 workgroups of 128 rows, 21.4 as
   // 512 of 64; 128 columns need the LDS of a CU for that and lose (1 x 1024, 32 over 8 of 128: 25.1, 29.1).
@@ -1140,7 +1264,7 @@ void choose_attention(AttnParams& p) {
     // Rows: one workgroup has a CU to itself; three rounds of its waves in each at least, which take as
     // long as the join
     chunks = std::min<int64_t>(256 / std::max<int64_t>(1, blocks / p.batch),
-                               p.batch * (ceil_div(p.k_len, kKeys * row_waves(p)) / 3));
+                               p.batch * (ceil_div(keys, kKeys * row_waves(p)) / 3));
   } else if (blocks < 256) {
     chunks = p.batch * split_tiles(p, blocks);
   }
@@ -1148,6 +1272,10 @@ void choose_attention(AttnParams& p) {
 }
 
 const char* attention_name(const AttnParams& p) {
+  if (p.tree) {
+    if (p.tile_rows > kCols) return p.f32 ? "attention_tree_tiles_f32" : "attention_tree_tiles";
+    return p.f32 ? "attention_tree_rows_f32" : "attention_tree_rows";
+  }
   if (p.tile_rows > kCols) return p.f32 ? "attention_tiles_f32" : "attention_tiles";
   return p.f32 ? "attention_rows_f32" : "attention_rows";
 }
@@ -1157,42 +1285,52 @@ int64_t attn_workspace(const AttnParams& p) {
   return (head_floats(p) + (int64_t)p.kv_heads * p.q_len * p.group * p.chunks * (p.D + 2)) * 4;
 }
 
-hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
-  if (p.D < 8 || p.D > 256 || p.D % 8 != 0 || p.chunks < p.batch) return hipErrorInvalidValue;
-  const int grid = p.chunks * p.kv_heads * row_blocks(p);
+namespace {
+
+template <bool TREE>
+void launch_as(const AttnParams& p, int grid, hipStream_t s) {
   if (p.tile_rows > kCols) {
     if (p.f32) {
-      if (p.D <= 32) attention_tiles_f32_kernel<64, 32><<<grid, 256, 0, s>>>(p);
-      else if (p.D <= 64) attention_tiles_f32_kernel<64, 64><<<grid, 256, 0, s>>>(p);
-      else if (p.D <= 96) attention_tiles_f32_kernel<128, 96><<<grid, 256, 0, s>>>(p);
-      else if (p.D <= 128) attention_tiles_f32_kernel<128, 128><<<grid, 256, 0, s>>>(p);
-      else if (p.D <= 192) attention_tiles_f32_kernel<256, 192><<<grid, 256, 0, s>>>(p);
-      else attention_tiles_f32_kernel<256, 256><<<grid, 256, 0, s>>>(p);
+      if (p.D <= 32) attention_tiles_f32_kernel<64, 32, TREE><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 64) attention_tiles_f32_kernel<64, 64, TREE><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 96) attention_tiles_f32_kernel<128, 96, TREE><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 128) attention_tiles_f32_kernel<128, 128, TREE><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 192) attention_tiles_f32_kernel<256, 192, TREE><<<grid, 256, 0, s>>>(p);
+      else attention_tiles_f32_kernel<256, 256, TREE><<<grid, 256, 0, s>>>(p);
     } else if (p.tile_rows == 64) {
-      if (p.D <= 32) attention_tiles_kernel<64, 32, 2><<<grid, 256, 0, s>>>(p);
-      else attention_tiles_kernel<64, 64, 2><<<grid, 256, 0, s>>>(p);
+      if (p.D <= 32) attention_tiles_kernel<64, 32, 2, TREE><<<grid, 256, 0, s>>>(p);
+      else attention_tiles_kernel<64, 64, 2, TREE><<<grid, 256, 0, s>>>(p);
     } else {
-      if (p.D <= 32) attention_tiles_kernel<64, 32, 1><<<grid, 256, 0, s>>>(p);
-      else if (p.D <= 64) attention_tiles_kernel<64, 64, 1><<<grid, 256, 0, s>>>(p);
-      else if (p.D <= 96) attention_tiles_kernel<128, 96, 1><<<grid, 256, 0, s>>>(p);
-      else if (p.D <= 128) attention_tiles_kernel<128, 128, 1><<<grid, 256, 0, s>>>(p);
-      else if (p.D <= 192) attention_tiles_kernel<256, 192, 1><<<grid, 256, 0, s>>>(p);
-      else attention_tiles_kernel<256, 256, 1><<<grid, 256, 0, s>>>(p);
+      if (p.D <= 32) attention_tiles_kernel<64, 32, 1, TREE><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 64) attention_tiles_kernel<64, 64, 1, TREE><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 96) attention_tiles_kernel<128, 96, 1, TREE><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 128) attention_tiles_kernel<128, 128, 1, TREE><<<grid, 256, 0, s>>>(p);
+      else if (p.D <= 192) attention_tiles_kernel<256, 192, 1, TREE><<<grid, 256, 0, s>>>(p);
+      else attention_tiles_kernel<256, 256, 1, TREE><<<grid, 256, 0, s>>>(p);
     }
-    return hipGetLastError();
+    return;
   }
   if (p.f32) {
-    if (p.D <= 32) attention_rows_kernel<float, 64, 32, 4><<<grid, 256, 0, s>>>(p);
-    else if (p.D <= 64) attention_rows_kernel<float, 64, 64, 4><<<grid, 256, 0, s>>>(p);
-    else if (p.D <= 96) attention_rows_kernel<float, 128, 96, 4><<<grid, 256, 0, s>>>(p);
-    else if (p.D <= 128) attention_rows_kernel<float, 128, 128, 4><<<grid, 256, 0, s>>>(p);
-    else if (p.D <= 192) attention_rows_kernel<float, 256, 192, 2><<<grid, 128, 0, s>>>(p);
-    else attention_rows_kernel<float, 256, 256, 2><<<grid, 128, 0, s>>>(p);
+    if (p.D <= 32) attention_rows_kernel<float, 64, 32, 4, TREE><<<grid, 256, 0, s>>>(p);
+    else if (p.D <= 64) attention_rows_kernel<float, 64, 64, 4, TREE><<<grid, 256, 0, s>>>(p);
+    else if (p.D <= 96) attention_rows_kernel<float, 128, 96, 4, TREE><<<grid, 256, 0, s>>>(p);
+    else if (p.D <= 128) attention_rows_kernel<float, 128, 128, 4, TREE><<<grid, 256, 0, s>>>(p);
+    else if (p.D <= 192) attention_rows_kernel<float, 256, 192, 2, TREE><<<grid, 128, 0, s>>>(p);
+    else attention_rows_kernel<float, 256, 256, 2, TREE><<<grid, 128, 0, s>>>(p);
   } else {
-    if (p.D <= 64) attention_rows_kernel<bf16_t, 64, 64, 8><<<grid, 512, 0, s>>>(p);
-    else if (p.D <= 128) attention_rows_kernel<bf16_t, 128, 128, 4><<<grid, 256, 0, s>>>(p);
-    else attention_rows_kernel<bf16_t, 256, 256, 2><<<grid, 128, 0, s>>>(p);
+    if (p.D <= 64) attention_rows_kernel<bf16_t, 64, 64, 8, TREE><<<grid, 512, 0, s>>>(p);
+    else if (p.D <= 128) attention_rows_kernel<bf16_t, 128, 128, 4, TREE><<<grid, 256, 0, s>>>(p);
+    else attention_rows_kernel<bf16_t, 256, 256, 2, TREE><<<grid, 128, 0, s>>>(p);
   }
+}
+
+}  // namespace
+
+hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
+  if (p.D < 8 || p.D > 256 || p.D % 8 != 0 || p.chunks < p.batch || (p.tree && p.q_len > kMaxTree)) return hipErrorInvalidValue;
+  const int grid = p.chunks * p.kv_heads * row_blocks(p);
+  if (p.tree) launch_as<true>(p, grid, s);
+  else launch_as<false>(p, grid, s);
   return hipGetLastError();
 }
 

@@ -33,12 +33,12 @@ constexpr int kKPad = 64;     // packed reduction length is padded to this (the 
 constexpr int kHaloStages = 3;  // halo kernel weight ring: 3 stages of one kernel row (built-in choice)
 
 struct PackJob {
-  enum Kind { ConvW, DwW, DwW32, RowsW32, Vec, Copy, StemW, Host, QDenseW } kind;  // Host: copy blob n, built on the host
+  enum Kind { ConvW, DwW, DwW32, RowsW32, Vec, Copy, StemW, Host, QDenseW, MxDenseW } kind;  // Host: copy blob n, built on the host
   int cidx = -1;       // constant index
   int64_t dst = 0;     // byte offset in the weights region
   int K = 0, Cg = 0, R = 0, S = 0, Cp = 0, Kgp = 0, rows = 0;
   int n = 0, n_out = 0;
-  int64_t dst2 = 0;    // QDenseW: the scales
+  int64_t dst2 = 0;    // QDenseW, MxDenseW: the scales
 };
 
 // float32 form of a real rescaling factor of an int8 graph (rounded from
@@ -364,11 +364,13 @@ struct Planner {
   const byoc_const* consts = nullptr;       // host constants (int8 weights are quantized on the host)
   std::vector<std::vector<uint8_t>> blobs;  // host-built constant blocks (PackJob::Host)
   std::vector<Launch> quant_of;  // value -> its QuantRows launch, shared by the qdense nodes that read it (x.kind None: none)
+  std::vector<Launch> mx_of;     // the same of MxRows and mxdense
 
   Planner(Engine* e_, Graph& g_) : e(e_), g(g_), bf16(g_.compute == DType::BF16), i8(g_.compute == DType::I8) {
     loc.resize(g.values.size());
     cp.assign(g.values.size(), 0);
     quant_of.resize(g.values.size());
+    mx_of.resize(g.values.size());
   }
 
   int64_t internal_bytes(int v) const {
@@ -418,22 +420,22 @@ struct Planner {
     return r;
   }
 
-  // Reads of value v by nodes and by outputs past the first, and whether qdense nodes alone read it as rows
-  // or residual.
+  // Reads of value v by nodes and by outputs past the first, and whether only nodes that take rows of any
+  // width read it: qdense and mxdense as rows or residual, logits.
   int reads(int v) const {
     int n = -1;
     for (const IoDesc& o : g.outputs) n += o.value == v;
     n = std::max(n, 0);
     for (const Node& x : g.nodes) {
-      for (int a : {x.data, x.residual, x.other, x.key, x.value, x.index}) n += a == v;
-      if (x.op == OpKind::Concat) n += (int)std::count(x.cat.begin() + 1, x.cat.end(), v);
+      for (int a : x.inputs()) n += a == v;
     }
     return n;
   }
-  bool only_qdense_reads(int v) const {
+  static bool any_width(const Node& n) { return n.op == OpKind::QDense || n.op == OpKind::MxDense || n.op == OpKind::Logits; }
+  bool only_any_width_reads(int v) const {
     int n = 0;
     for (const Node& x : g.nodes)
-      if (x.op == OpKind::QDense) n += (x.data == v) + (x.residual == v);
+      if (any_width(x)) n += (x.data == v) + (x.residual == v);
     for (const IoDesc& o : g.outputs)
       if (o.value == v && g.values[v].source == Value::Input) return false;
     return n == reads(v);
@@ -456,8 +458,10 @@ struct Planner {
   void plan_ir(int ci);
   void plan_block_i8(int ci);
   void plan_qdense(int ni);
+  void plan_mxdense(int ni);
   void plan_rotary(int ni);
   void plan_attention(int ni);
+  void plan_logits(int ni);
   Ref slice(int vcat, int channel) const {  // channel slice of a concatenation's buffer
     Ref r = loc[vcat];
     r.off += (int64_t)channel * 2;
@@ -1113,7 +1117,7 @@ Status Planner::plan() {
   for (size_t i = 0; i < g.inputs.size(); ++i) {
     const IoDesc& in = g.inputs[i];
     const int v = in.value;
-    if (in.dtype == DType::I32) {  // positions or lengths, read in place
+    if (in.dtype == DType::I32 || g.values[v].param) {  // positions, lengths, strengths and the like, read in place
       loc[v] = io(Ref::Input, (int)i);
       continue;
     }
@@ -1127,9 +1131,9 @@ Status Planner::plan() {
       continue;
     }
     const bool rows = bf16 && s.size() == 2 && in.dtype == DType::BF16;
-    const bool direct = bf16 ? rows && (s[1] % 8 == 0 || only_qdense_reads(v)) : (in.dtype == DType::F32);
+    const bool direct = bf16 ? rows && (s[1] % 8 == 0 || only_any_width_reads(v)) : (in.dtype == DType::F32);
     if (direct) {
-      if (bf16) cp[v] = (int)s[1];  // (qdense takes rows of any width)
+      if (bf16) cp[v] = (int)s[1];  // (rows of any width)
       loc[v] = io(Ref::Input, (int)i);
       continue;
     }
@@ -1169,10 +1173,10 @@ Status Planner::plan() {
       const IoDesc& o = g.outputs[j];
       if (o.value != v || direct_out[j]) continue;
       const bool rows = bf16 && s.size() == 2 && o.dtype == DType::BF16;
-      const bool ok = bf16 ? rows && (s[1] % 8 == 0 || (n.op == OpKind::QDense && only_qdense_reads(v) && reads(v) == 0))
+      const bool ok = bf16 ? rows && (s[1] % 8 == 0 || (any_width(n) && only_any_width_reads(v) && reads(v) == 0))
                            : (o.dtype == DType::F32);
       if (ok) {
-        if (bf16) cp[v] = (int)s[1];  // (qdense writes rows of any width)
+        if (bf16) cp[v] = (int)s[1];  // (rows of any width)
         loc[v] = io(Ref::Output, (int)j);
         direct_out[j] = true;
         placed = true;
@@ -1304,6 +1308,77 @@ void Planner::plan_qdense(int ni) {
   e->launches.push_back(L);
 }
 
+// Dense on microscaled 4-bit floats: as plan_qdense.
+void Planner::plan_mxdense(int ni) {
+  const Node& n = g.nodes[ni];
+  const auto& xs = g.values[n.data].shape;
+  const auto& ws = g.values[n.weight].shape;
+  const int M = (int)xs[0], K = (int)xs[1], N = (int)ws[0];
+  const int Kq = (int)rup(K, 256), rows = (int)rup(N, kRowPad), Mq = (int)rup(M, 32);
+  auto packed = [&](int64_t r) { return r * (Kq / 2); };       // bytes of r rows' codes
+  auto scales = [&](int64_t r) { return r / 32 * Kq; };        // and of their scales
+  Launch L;
+  const bool fused = L.fused = mxdense_fuses_rows(M, cp[n.out], Kq);
+  Launch& Q = mx_of[n.data];
+  MxRowsParams r{};
+  r.ldx = cp[n.data];
+  r.M = M, r.rows = Mq, r.K = K, r.Kq = Kq;
+  r.f32 = !bf16;
+  if (fused) {
+    L.x = loc[n.data];
+    L.mr = r;
+  } else if (Q.x.kind == Ref::None) {
+    Q.op = Launch::MxRows;
+    Q.info.kind = BYOC_K_MXDENSE;
+    Q.info.node = ni;
+    Q.x = loc[n.data];
+    Q.qr_scales = rup(packed(Mq), 256);
+    Q.y = arena(Q.qr_scales + scales(Mq));
+    Q.mr = r;
+    Q.info.bytes = act_bytes(n.data) + (int64_t)M * (K / 2 + (K + 31) / 32);
+    name(Q, "mx_rows");
+    e->launches.push_back(Q);
+  }
+  L.op = Launch::MxDense;
+  L.info.kind = BYOC_K_MXDENSE;
+  L.info.node = ni;
+  L.info.flops = 2 * n.macs;
+  L.info.bytes = ((int64_t)M + N) * (K / 2 + (K + 31) / 32) + (n.bias >= 0 ? N * 4 : 0) +
+                 act_bytes(n.out) * (n.residual >= 0 ? 2 : 1);
+  if (!fused) {
+    L.x = Q.y;
+    L.qr_scales = Q.qr_scales;
+  }
+  L.y = loc[n.out];
+  if (n.residual >= 0) L.res = loc[n.residual];
+  L.w = wslot(packed(rows));
+  L.w2 = wslot(scales(rows));
+  PackJob j{PackJob::MxDenseW, g.values[n.weight].index, L.w.off};
+  j.K = N, j.rows = rows, j.Kgp = Kq, j.n = K;
+  j.dst2 = L.w2.off;
+  jobs.push_back(j);
+  if (n.bias >= 0) {
+    L.bias = wslot((int64_t)rows * 4);
+    PackJob b{PackJob::Vec, g.values[n.bias].index, L.bias.off};
+    b.n = N, b.n_out = rows;
+    jobs.push_back(b);
+  }
+  MxDenseParams& p = L.mx;
+  p.M = M, p.N = cp[n.out], p.Kq = Kq;
+  p.ldy = cp[n.out];
+  p.ldr = n.residual >= 0 ? cp[n.residual] : 0;
+  p.channels = N;
+  p.act = (int)n.act;
+  p.alpha = n.alpha;
+  p.f32 = !bf16;
+  L.mt = choose_mxdense_tile(p.M, p.N, Kq);
+  // BYOC_MXDENSE_TILE=<id>: that tile wherever a tile is chosen (tests run every one with it)
+  if (const char* ev = std::getenv("BYOC_MXDENSE_TILE"); ev && L.mt.id != kMxDenseRows) (void)mxdense_tile_of(std::atoi(ev), &L.mt);
+  if (L.mt.id == kMxDenseRows) std::snprintf(L.info.name, sizeof(L.info.name), "mxdense_rows_m%d%s", M, fused ? "_fused" : "");
+  else std::snprintf(L.info.name, sizeof(L.info.name), "mxdense_%dx%d_s%d", L.mt.bm, L.mt.bn, L.mt.stages);
+  e->launches.push_back(L);
+}
+
 void Planner::plan_rotary(int ni) {
   const Node& n = g.nodes[ni];
   Launch L;
@@ -1363,12 +1438,20 @@ void Planner::plan_attention(int ni) {
   p.batch = n.batch, p.q_len = n.q_len, p.k_len = n.k_len;
   p.kv_heads = n.kv_heads, p.group = n.heads / n.kv_heads, p.D = n.head_dim;
   p.causal = n.causal;
+  p.tree = n.parents >= 0;
   p.scale = (float)n.scale;
   p.f32 = !bf16;
+  if (p.tree) {
+    L.more = {loc[n.key2], loc[n.value2], loc[n.parents]};
+    L.more[0].off += n.cols[3] * es;
+    L.more[1].off += n.cols[4] * es;
+    p.ldk2 = cp[n.key2], p.ldv2 = cp[n.value2];
+  }
   choose_attention(p);
-  // (every pair of a full context: the lengths are not known yet)
-  L.info.flops = 4 * (int64_t)n.batch * n.heads * n.q_len * n.k_len * n.head_dim;
-  L.info.bytes = 2 * act_bytes(n.out) + 2 * (int64_t)n.batch * n.k_len * n.kv_heads * n.head_dim * es;
+  // (every pair of a full context, and of a tree: the lengths and paths are not known yet)
+  const int64_t keys = n.k_len + (p.tree ? n.q_len : 0);
+  L.info.flops = 4 * (int64_t)n.batch * n.heads * n.q_len * keys * n.head_dim;
+  L.info.bytes = 2 * act_bytes(n.out) + 2 * (int64_t)n.batch * keys * n.kv_heads * n.head_dim * es;
   name(L, attention_name(p));
   if (p.chunks <= p.batch) {
     e->launches.push_back(L);
@@ -1379,17 +1462,47 @@ void Planner::plan_attention(int ni) {
   L.y = Ref();
   J.op = Launch::AttentionJoin;
   J.x = J.other = J.res = Ref();
+  J.more.clear();
   J.info.flops = J.info.bytes = 0;
   name(J, "attention_join");
   e->launches.push_back(L);
   e->launches.push_back(J);
 }
 
+void Planner::plan_logits(int ni) {
+  const Node& n = g.nodes[ni];
+  Launch L;
+  L.op = Launch::Logits;
+  L.info.kind = BYOC_K_LOGITS;
+  L.info.node = ni;
+  L.x = loc[n.data];
+  L.y = loc[n.out];
+  LogitsParams& p = L.lg;
+  L.info.bytes = 2 * act_bytes(n.out);
+  for (int v : {n.history, n.prompts, n.index, n.strengths, n.draft_tokens, n.parents, n.bias_tokens, n.bias_values,
+                n.mask_words}) {
+    L.more.push_back(v >= 0 ? loc[v] : Ref());
+    if (v >= 0) L.info.bytes += numel(g.values[v].shape) * 4;
+  }
+  const auto& s = g.values[n.data].shape;
+  p.ldx = cp[n.data];
+  p.ldy = p.cols_out = cp[n.out];
+  p.batch = n.batch, p.rows = (int)(s[0] / n.batch), p.V = (int)s[1];
+  p.T = n.penalties ? (int)(g.values[n.history].shape[0] / n.batch) : 0;
+  p.E = n.has_bias ? (int)(g.values[n.bias_tokens].shape[0] / n.batch) : 0;
+  p.f32 = !bf16;
+  choose_logits(p);
+  name(L, n.composite.c_str());
+  e->launches.push_back(L);
+}
+
 void Planner::plan_node(int ni) {
   const Node& n = g.nodes[ni];
   if (n.op == OpKind::QDense) return plan_qdense(ni);
+  if (n.op == OpKind::MxDense) return plan_mxdense(ni);
   if (n.op == OpKind::Rotary) return plan_rotary(ni);
   if (n.op == OpKind::Attention) return plan_attention(ni);
+  if (n.op == OpKind::Logits) return plan_logits(ni);
   const auto& xs = g.values[n.data].shape;
   const auto& ys = g.values[n.out].shape;
   Launch L;
@@ -2281,7 +2394,8 @@ void layout_arena(Engine* e) {
       head = (int)i;
       left = std::max(1, L.group);
     }
-    for (const Ref* r : {&L.x, &L.w, &L.bias, &L.res, &L.y, &L.partial, &L.other}) touch(*r, head);
+    for (const Ref* r : L.reads()) touch(*r, head);
+    for (const Ref* r : {&L.y, &L.partial}) touch(*r, head);
   }
   OffsetAlloc a;
   for (size_t i = 0; i < e->launches.size(); ++i) {
@@ -2306,9 +2420,9 @@ bool must_follow(const Launch& i, const Launch& j) {
     return (a.kind == Ref::Input || a.kind == Ref::Output) && (b.kind == Ref::Input || b.kind == Ref::Output);
   };
   auto reads = [&](const Launch& L, const Ref& r) {
-    for (const Ref* a : {&L.x, &L.w, &L.bias, &L.res, &L.partial, &L.other})
+    for (const Ref* a : L.reads())
       if (same(*a, r)) return true;
-    return false;
+    return same(L.partial, r);
   };
   if (reads(j, i.y) || reads(j, i.partial) || reads(i, j.y) || reads(i, j.partial)) return true;
   if (!same(i.y, j.y)) return false;
@@ -2637,7 +2751,52 @@ hipError_t exec(const Launch& L, const RunCtx& c) {
       p.lengths = (const int*)c.ptr(L.bias);
       p.y = c.ptr(L.y);
       p.ws = (float*)c.ptr(L.partial);
+      if (L.more.size() == 3) {
+        p.k2 = c.ptr(L.more[0]);
+        p.v2 = c.ptr(L.more[1]);
+        p.parents = (const int*)c.ptr(L.more[2]);
+      }
       return L.op == Launch::Attention ? launch_attention(p, c.s) : launch_attention_join(p, c.s);
+    }
+    case Launch::MxRows: {
+      MxRowsParams p = L.mr;
+      p.x = c.ptr(L.x);
+      p.q = (uint8_t*)c.ptr(L.y);
+      p.scale = (uint8_t*)c.ptr(L.y) + L.qr_scales;
+      return launch_mx_rows(p, c.s);
+    }
+    case Launch::MxDense: {
+      MxDenseParams p = L.mx;
+      if (!L.fused) {
+        p.x = (const uint8_t*)c.ptr(L.x);
+        p.xs = (const uint8_t*)c.ptr(L.x) + L.qr_scales;
+      }
+      p.w = (const uint8_t*)c.ptr(L.w);
+      p.ws = (const uint8_t*)c.ptr(L.w2);
+      p.bias = (const float*)c.ptr(L.bias);
+      p.res = c.ptr(L.res);
+      p.y = c.ptr(L.y);
+      if (L.fused) {
+        MxRowsParams q = L.mr;
+        q.x = c.ptr(L.x);
+        return launch_mxdense_fused(p, q, c.s);
+      }
+      return launch_mxdense(p, L.mt, c.s);
+    }
+    case Launch::Logits: {
+      LogitsParams p = L.lg;
+      p.x = c.ptr(L.x);
+      p.history = (const int*)c.ptr(L.more[0]);
+      p.prompts = (const int*)c.ptr(L.more[1]);
+      p.lengths = (const int*)c.ptr(L.more[2]);
+      p.strengths = (const float*)c.ptr(L.more[3]);
+      p.drafts = (const int*)c.ptr(L.more[4]);
+      p.parents = (const int*)c.ptr(L.more[5]);
+      p.bias_tokens = (const int*)c.ptr(L.more[6]);
+      p.bias_values = (const float*)c.ptr(L.more[7]);
+      p.mask = (const uint32_t*)c.ptr(L.more[8]);
+      p.y = c.ptr(L.y);
+      return launch_logits(p, c.s);
     }
   }
   return hipErrorInvalidValue;
@@ -2750,6 +2909,9 @@ Status build_device_state(Engine* e, Planner& pl, const byoc_const* consts) {
         case PackJob::QDenseW:
           err = launch_quant_rows({src, (int8_t*)dst, (float*)(e->weights + j.dst2), j.n, j.K, j.rows, j.n, j.Kgp, !sb}, nullptr);
           break;
+        case PackJob::MxDenseW:
+          err = launch_mx_rows({src, (uint8_t*)dst, (uint8_t*)e->weights + j.dst2, j.n, j.K, j.rows, j.n, j.Kgp, !sb}, nullptr);
+          break;
       }
     }
     if (err != hipSuccess) st = Status::Err(BYOC_ERR_DEVICE, std::string("constant packing: ") + hipGetErrorString(err));
@@ -2814,7 +2976,7 @@ Status plan_streams(Engine* e) {
   for (size_t i = 0; i < n; ++i) {
     const Launch& L = e->launches[i];
     Span sp;
-    for (const Ref* r : {&L.x, &L.w, &L.bias, &L.res, &L.other})
+    for (const Ref* r : L.reads())
       if (span_of(e, *r, &sp)) rd[i].push_back(sp);
     if (span_of(e, L.partial, &sp)) {
       rd[i].push_back(sp);
@@ -2874,13 +3036,14 @@ Status engine_create(Graph&& g, const byoc_const* consts, int32_t n_consts, int 
   Status st = pl.plan();
   for (const Launch& L : e->launches) {
     if (L.op != Launch::QuantRows && L.op != Launch::QDense && L.op != Launch::Rotary && L.op != Launch::Attention &&
-        L.op != Launch::AttentionJoin)
+        L.op != Launch::AttentionJoin && L.op != Launch::Logits && L.op != Launch::MxRows && L.op != Launch::MxDense)
       continue;
-    for (const Ref* r : {&L.x, &L.bias, &L.res, &L.y, &L.other}) {
-      if (r->kind == Ref::Input)
-        e->in_align.push_back({r->idx, e->graph.inputs[r->idx].dtype == DType::I32 ? 4 : 16});
-      if (r->kind == Ref::Output) e->out_align.push_back({r->idx, 16});
+    for (const Ref* r : L.reads()) {
+      if (r->kind != Ref::Input) continue;
+      const IoDesc& in = e->graph.inputs[r->idx];
+      e->in_align.push_back({r->idx, in.dtype == DType::I32 || e->graph.values[in.value].param ? 4 : 16});
     }
+    if (L.y.kind == Ref::Output) e->out_align.push_back({L.y.idx, 16});
   }
   if (st.ok()) {
     int ndev = 0;

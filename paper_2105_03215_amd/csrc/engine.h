@@ -27,7 +27,8 @@ struct Launch {
     ConvMfma, SplitReduce, ConvF32, Depthwise, MaxPoolBf16, AvgPoolBf16, MaxPoolF32, AvgPoolF32,
     AddBf16, AddF32, NchwToNhwc, NhwcToNchw, RowsToPadded, PaddedToRows, Cast, StemConvPool, DenseRows,
     ConvI8, MaxPoolI8, AvgPoolI8, AddI8, QuantizeI8, DequantizeI8, AvgPoolWinBf16, CopyChannels, QuantizeIm2colI8,
-    DepthwiseI8, Bottleneck, IrBlock, QuantRows, QDense, Rotary, Attention, AttentionJoin
+    DepthwiseI8, Bottleneck, IrBlock, QuantRows, QDense, Rotary, Attention, AttentionJoin,
+    Logits, MxRows, MxDense
   } op;
   byoc_launch_info info{};
   Ref x, w, bias, res, y, partial, other;
@@ -50,6 +51,7 @@ struct Launch {
   // in w3 / b3
   IrParams ir{};
   Ref w2, b2, w3, b3, wp, bp;
+  std::vector<Ref> more;  // what it reads besides x, w, bias, res and other
   QRowsParams qr{};   // QuantRows: x -> codes in y, scales in y at qr_scales
   int64_t qr_scales = 0;
   QDenseParams qn{};  // QDense: codes (and scales) in x, packed codes in w, their scales in w2, bias, res
@@ -57,6 +59,10 @@ struct Launch {
   bool fused = false;
   RotaryParams rot{};  // Rotary: positions in other, angles in w, norm weights in w2 / w3
   AttnParams at{};     // Attention: queries in x, keys in other, values in res, lengths in bias, split results in partial
+  MxRowsParams mr{};   // MxRows: x -> codes in y, scales in y at qr_scales
+  MxDenseParams mx{};  // MxDense: codes (and scales) in x, packed codes in w, their scales in w2, bias, res
+  MxDenseTile mt{};    //   (x: the rows themselves, described in mr, where the product quantizes them: fused)
+  LogitsParams lg{};   // Logits: history, prompts, lengths, strengths, drafts, parents, bias tokens, bias values, mask in more
   int bnF = 0, bnC = 0, bnCout = 0, bnS = 1;
   int group = 0;      // > 1: this launch and the group - 1 after it go out as one (bf16 convs)
   bool bnI8 = false;  // on int8 codes (w*, b* hold the int8 conv's weights and tables)
@@ -70,6 +76,13 @@ struct Launch {
   bool src_bf16 = false, dst_bf16 = false;
   bool count_include_pad = false;  // windowed average pool
   int N = 0, C = 0, H = 0, W = 0, Cp = 0, M = 0, K = 0, Kp = 0;
+
+  // every place it reads besides partial (packed weights among them)
+  std::vector<const Ref*> reads() const {
+    std::vector<const Ref*> r{&x, &w, &bias, &res, &other};
+    for (const Ref& m : more) r.push_back(&m);
+    return r;
+  }
 };
 
 struct ArenaBuf {

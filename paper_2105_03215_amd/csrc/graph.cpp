@@ -117,6 +117,7 @@ Status attr_padding(const JsonValue* attrs, const std::string& where, int out[4]
 struct CompositeName {
   OpKind op;
   bool bias = false, add = false;
+  bool penalties = false, drafts = false, mask = false;  // Logits
   Act act = Act::None;
 };
 
@@ -142,6 +143,7 @@ Status attr_positive(const JsonValue* attrs, const char* key, const std::string&
 }
 
 constexpr int kMaxHeads = 4096;
+constexpr int kMaxDrafts = 256;  // drafted tokens of a sequence, whose paths the kernels hold as bits in LDS
 constexpr int64_t kMaxCols = 1 << 22;  // columns of a row that the packed-head kernels address (tiles of 64 rows in 31 bits)
 
 // The angle per position of each pair, and the factor on the rotated values.
@@ -204,7 +206,7 @@ bool split_composite(const std::string& name, CompositeName* c) {
     c->op = OpKind::Rotary;
     return true;
   }
-  if (name == "attention" || name == "attention_lengths") {
+  if (name == "attention" || name == "attention_lengths" || name == "attention_tree") {
     c->op = OpKind::Attention;
     return true;
   }
@@ -236,9 +238,19 @@ bool split_composite(const std::string& name, CompositeName* c) {
   }
   parts.push_back(cur);
   size_t i = 0;
+  if (parts[0] == "logits") {
+    c->op = OpKind::Logits;
+    ++i;
+    if (i < parts.size() && parts[i] == "penalties") c->penalties = true, ++i;
+    if (c->penalties && i < parts.size() && parts[i] == "drafts") c->drafts = true, ++i;
+    if (i < parts.size() && parts[i] == "bias") c->bias = true, ++i;
+    if (i < parts.size() && parts[i] == "mask") c->mask = true, ++i;
+    return i > 1 && i == parts.size();
+  }
   if (parts[0] == "conv2d") c->op = OpKind::Conv;
   else if (parts[0] == "dense") c->op = OpKind::Dense;
   else if (parts[0] == "qdense") c->op = OpKind::QDense;
+  else if (parts[0] == "mxdense") c->op = OpKind::MxDense;
   else if (parts[0] == "add") c->op = OpKind::Add;
   else return false;
   ++i;
@@ -401,6 +413,9 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
     n.has_bias = cn.bias;
     n.has_add = cn.add;
     n.act = cn.act;
+    n.penalties = cn.penalties;
+    n.drafts = cn.drafts;
+    n.mask = cn.mask;
     std::string odt;
     DType out_dtype;
     if (get_string(d, "out_dtype", &odt) && (odt == "int8" || odt == "i8")) out_dtype = DType::I8;
@@ -426,6 +441,8 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
     auto is_const = [&](int v) { return g.values[v].source == Value::Const; };
     auto shp = [&](int v) -> const std::vector<int64_t>& { return g.values[v].shape; };
     std::vector<int64_t> oshape;
+    const bool tree = n.composite == "attention_tree";
+    const bool weighted = n.op == OpKind::Conv || n.op == OpKind::Dense || n.op == OpKind::QDense || n.op == OpKind::MxDense;
 
     size_t want = 0;
     switch (n.op) {
@@ -433,9 +450,13 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
         n.norm = n.composite == "qk_norm_rotary";
         want = n.norm ? (args.size() == 3 ? 3 : 4) : 2;  // (no key heads: no key weight)
         break;
-      case OpKind::Attention: want = n.composite == "attention" ? 3 : 4; break;
+      case OpKind::Attention: want = tree ? 7 : n.composite == "attention" ? 3 : 4; break;
+      case OpKind::Logits:
+        want = 1 + (n.penalties ? 4 : 0) + (n.drafts ? 2 : 0) + (n.has_bias ? 2 : 0) + (n.mask ? 1 : 0);
+        break;
       case OpKind::Conv:
       case OpKind::QDense:
+      case OpKind::MxDense:
       case OpKind::Dense: want = 2 + (n.has_bias ? 1 : 0) + (n.has_add ? 1 : 0); break;
       case OpKind::MaxPool:
       case OpKind::AvgPool:
@@ -446,21 +467,39 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
     if (args.size() != want)
       return perr(where + ": expects " + std::to_string(want) + " inputs, got " +
                   std::to_string(args.size()));
+    // Logits: the places of the inputs in the order that the composite's name gives them
+    int slot_history = -1, slot_drafts = -1, slot_bias = -1, slot_mask = -1;
+    if (n.op == OpKind::Logits) {
+      int k = 1;
+      if (n.penalties) slot_history = k, k += 4;
+      if (n.drafts) slot_drafts = k, k += 2;
+      if (n.has_bias) slot_bias = k, k += 2;
+      if (n.mask) slot_mask = k;
+    }
     for (size_t k = 0; k < args.size(); ++k) {
-      bool weight_slot = (n.op == OpKind::Conv || n.op == OpKind::Dense || n.op == OpKind::QDense) &&
-                         (k == 1 || (k == 2 && n.has_bias));
+      bool weight_slot = weighted && (k == 1 || (k == 2 && n.has_bias));
       if (n.op == OpKind::Rotary) weight_slot = k > 0 && k + 1 < args.size();
-      const bool index_slot = (n.op == OpKind::Rotary && k + 1 == args.size()) || (n.op == OpKind::Attention && k == 3);
-      if (index_slot != (g.values[args[k]].dtype == DType::I32))
+      const bool param_slot = n.op == OpKind::Logits && ((n.penalties && (int)k == slot_history + 3) ||
+                                                          (n.has_bias && (int)k == slot_bias + 1));
+      const bool index_slot = (n.op == OpKind::Rotary && k + 1 == args.size()) ||
+                              (n.op == OpKind::Attention && k >= (tree ? 5u : 3u)) ||
+                              (n.op == OpKind::Logits && k > 0 && !param_slot);
+      Value& arg = g.values[args[k]];
+      if (index_slot != (arg.dtype == DType::I32))
         return serr(where + ": input " + std::to_string(k) + (index_slot ? " must be an i32 input" : " must not be i32"));
       if (weight_slot && !is_const(args[k]))
         return uerr(where + ": input " + std::to_string(k) + " must be a constant");
       if (!weight_slot && is_const(args[k]))
         return uerr(where + ": input " + std::to_string(k) + " must be an activation, got constant '" +
                     g.values[args[k]].name + "'");
+      if (param_slot) {
+        if (arg.source != Value::Input || arg.dtype != DType::F32)
+          return serr(where + ": input " + std::to_string(k) + " must be an f32 input of the graph");
+        arg.param = true;
+      }
     }
     n.data = args[0];
-    if (n.op == OpKind::Conv || n.op == OpKind::Dense || n.op == OpKind::QDense) {
+    if (weighted) {
       n.weight = args[1];
       size_t k = 2;
       if (n.has_bias) n.bias = args[k++];
@@ -477,8 +516,18 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
       n.key = args[1];
       n.value = args[2];
       if (args.size() == 4) n.index = args[3];
+      if (tree) n.key2 = args[3], n.value2 = args[4], n.index = args[5], n.parents = args[6];
+    } else if (n.op == OpKind::Logits) {
+      if (n.penalties) {
+        n.history = args[slot_history], n.prompts = args[slot_history + 1], n.index = args[slot_history + 2];
+        n.strengths = args[slot_history + 3];
+      }
+      if (n.drafts) n.draft_tokens = args[slot_drafts], n.parents = args[slot_drafts + 1];
+      if (n.has_bias) n.bias_tokens = args[slot_bias], n.bias_values = args[slot_bias + 1];
+      if (n.mask) n.mask_words = args[slot_mask];
     }
-    if ((n.op == OpKind::QDense || n.op == OpKind::Rotary || n.op == OpKind::Attention) && out_dtype == DType::I8)
+    if ((n.op == OpKind::QDense || n.op == OpKind::Rotary || n.op == OpKind::Attention || n.op == OpKind::MxDense ||
+         n.op == OpKind::Logits) && out_dtype == DType::I8)
       return uerr(where + ": " + n.composite + " only in bf16 and f32 graphs");
     const auto& xs = shp(n.data);
     if (n.act == Act::Leaky && attrs && attrs->get("alpha")) {
@@ -579,9 +628,11 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
         if (cv->kind != JsonValue::Bool) return perr(where + ": attrs.causal must be a boolean");
         n.causal = cv->b;
       }
-      const char* col_names[3] = {"q_col", "k_col", "v_col"};
-      const std::vector<int64_t>* shapes[3] = {&xs, &ks, &vs};
-      for (int i = 0; i < 3; ++i) {
+      if (tree && attrs->get("causal")) return uerr(where + ": attrs.causal on a tree, whose parents order it");
+      const char* col_names[5] = {"q_col", "k_col", "v_col", "draft_k_col", "draft_v_col"};
+      const std::vector<int64_t>* shapes[5] = {&xs, &ks, &vs, tree ? &shp(n.key2) : nullptr, tree ? &shp(n.value2) : nullptr};
+      for (int i = 0; i < (tree ? 5 : 3); ++i) {
+        if (shapes[i]->size() != 2) return serr(where + ": drafted keys and values must be 2-D");
         if (!(st = attr_int(attrs, col_names[i], where, 0, kMaxCols, &n.cols[i])).ok()) return st;
         if (n.cols[i] % 8) return uerr(where + ": attrs." + col_names[i] + " must be a multiple of 8");
         const int64_t cols = (*shapes[i])[1];
@@ -599,11 +650,52 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
       n.k_len = (int)(ks[0] / n.batch);
       if (n.index >= 0 && shp(n.index) != std::vector<int64_t>{n.batch})
         return serr(where + ": lengths shape " + shape_str(shp(n.index)) + " != [" + std::to_string(n.batch) + "]");
+      if (tree) {
+        if ((*shapes[3])[0] != xs[0] || (*shapes[4])[0] != xs[0])
+          return serr(where + ": drafted keys " + shape_str(*shapes[3]) + " or values " + shape_str(*shapes[4]) +
+                      " differ in rows from the queries " + shape_str(xs));
+        if (shp(n.parents) != std::vector<int64_t>{xs[0]})
+          return serr(where + ": parents shape " + shape_str(shp(n.parents)) + " != [" + std::to_string(xs[0]) + "]");
+        if (n.q_len > kMaxDrafts)
+          return uerr(where + ": more than " + std::to_string(kMaxDrafts) + " drafted tokens of a sequence");
+      }
       // packed rows, workgroups and split results are counted in 31 bits
       if ((int64_t)n.q_len * (n.heads / n.kv_heads) > kMaxElems / 64 || xs[0] * n.heads > kMaxElems / 64)
         return uerr(where + ": too many query rows");
       oshape = {xs[0], (int64_t)n.heads * n.head_dim};
-    } else if (n.op == OpKind::Dense || n.op == OpKind::QDense) {
+    } else if (n.op == OpKind::Logits) {
+      if (xs.size() != 2) return serr(where + ": data must be 2-D, got " + shape_str(xs));
+      n.batch = 0;
+      Status st = attr_int(attrs, "batch", where, 1, 1 << 20, &n.batch);
+      if (!st.ok()) return st;
+      if (!n.batch) return perr(where + ": attrs.batch is required");
+      const int64_t b = n.batch, rows = xs[0] / b;
+      if (xs[0] % b) return serr(where + ": rows of " + shape_str(xs) + " are not a multiple of attrs.batch");
+      auto expect = [&](int v, const char* what, const std::vector<int64_t>& want_shape) {
+        if (shp(v) == want_shape) return Status::Ok();
+        return serr(where + ": " + what + " shape " + shape_str(shp(v)) + " != " + shape_str(want_shape));
+      };
+      if (n.penalties) {
+        if (shp(n.history)[0] % b)
+          return serr(where + ": history " + shape_str(shp(n.history)) + " is not a multiple of attrs.batch");
+        if (!(st = expect(n.prompts, "prompt lengths", {b})).ok()) return st;
+        if (!(st = expect(n.index, "lengths", {b})).ok()) return st;
+        if (!(st = expect(n.strengths, "strengths", {b, 3})).ok()) return st;
+      }
+      if (n.drafts) {
+        if (!(st = expect(n.draft_tokens, "drafted tokens", {xs[0]})).ok()) return st;
+        if (!(st = expect(n.parents, "parents", {xs[0]})).ok()) return st;
+        if (rows > kMaxDrafts)
+          return uerr(where + ": more than " + std::to_string(kMaxDrafts) + " drafted tokens of a sequence");
+      }
+      if (n.has_bias) {
+        if (shp(n.bias_tokens)[0] % b)
+          return serr(where + ": bias tokens " + shape_str(shp(n.bias_tokens)) + " are not a multiple of attrs.batch");
+        if (!(st = expect(n.bias_values, "bias values", {b, shp(n.bias_tokens)[0] / b})).ok()) return st;
+      }
+      if (n.mask && !(st = expect(n.mask_words, "mask", {xs[0] * ((xs[1] + 31) / 32)})).ok()) return st;
+      oshape = xs;
+    } else if (n.op == OpKind::Dense || n.op == OpKind::QDense || n.op == OpKind::MxDense) {
       if (xs.size() != 2) return serr(where + ": data must be 2-D [M,K], got " + shape_str(xs));
       const auto& ws = shp(n.weight);
       if (ws.size() != 2 || ws[1] != xs[1])
@@ -615,6 +707,8 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
       n.macs = xs[0] * ws[0] * xs[1];
       if (n.op == OpKind::QDense && xs[1] > 131072)  // 127^2 K stays under 2^31
         return uerr(where + ": reduction of more than 131072 elements on 8-bit codes");
+      if (n.op == OpKind::MxDense && xs[1] > 131072)  // 256 rows of a tile are addressed in 31 bits
+        return uerr(where + ": reduction of more than 131072 elements on 4-bit codes");
     } else if (n.op == OpKind::MaxPool) {
       if (xs.size() != 4) return serr(where + ": data must be 4-D NCHW, got " + shape_str(xs));
       if (!attrs || !attrs->get("pool_size")) return perr(where + ": attrs.pool_size missing");
@@ -725,6 +819,10 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
     g.nodes.push_back(n);
   }
 
+  for (const Node& n : g.nodes)
+    for (int a : n.inputs())
+      if (g.values[a].param && a != n.strengths && a != n.bias_values)
+        return uerr("node " + n.name + ": input '" + g.values[a].name + "' is read as strengths or biases elsewhere");
   for (const IoDesc& in : g.inputs) {
     const Value& v = g.values[in.value];
     if (g.compute != DType::I8 && v.has_q)
@@ -749,6 +847,8 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
       return uerr(where + ": a constant cannot be a subgraph output");
     if (g.values[it->second].dtype == DType::I32)
       return uerr(where + ": an i32 input cannot be a subgraph output");
+    if (g.values[it->second].param)
+      return uerr(where + ": an input of strengths or biases cannot be a subgraph output");
     IoDesc io;
     io.value = it->second;
     const auto& s = g.values[io.value].shape;

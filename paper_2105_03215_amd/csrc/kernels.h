@@ -484,6 +484,52 @@ bool qdense_fuses_rows(int64_t M, int64_t N, int64_t Kq);
 hipError_t launch_qdense_fused(const QDenseParams& p, const QRowsParams& q, hipStream_t s);
 hipError_t launch_qdense(const QDenseParams& p, QDenseTile t, hipStream_t s);
 
+// Rows of activations (or weights) -> microscaled 4-bit floating point.  A block is 32
+// values along a row under a shared power of two 2^(s - 127), s = max(E, 2) - 2 with E the
+// biased exponent of the block's largest magnitude (255 for a block that holds an infinity
+// or a NaN); a code is the value over it, rounded to 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (ties to even,
+// what lies past 6 to 6) and a sign bit.  `rows` rows (a multiple of 32) of Kq codes (a multiple of
+// 256) are written, zero past row M and column K: two codes a byte, the first in the lower
+// half, and the scales in the order that the product's lanes take them in (mxdense.hip).
+struct MxRowsParams {
+  const void* x;   // [M][ldx], bf16 or f32
+  uint8_t* q;      // [rows][Kq / 2]
+  uint8_t* scale;  // [rows / 32][Kq / 256][256]
+  int64_t ldx;
+  int M, rows, K, Kq;
+  int f32;
+};
+hipError_t launch_mx_rows(const MxRowsParams& p, hipStream_t s);
+
+// y[m][n] = act(sum_k x[m][k] w[n][k] + bias[n] (+ res[m][n])) on microscaled codes,
+// the sum in float32.
+struct MxDenseParams {
+  const uint8_t* x;    // [M][Kq / 2], rows of a multiple of 32
+  const uint8_t* xs;   // scales
+  const uint8_t* w;    // [rows of a multiple of 256][Kq / 2], zero past the channels
+  const uint8_t* ws;   // scales
+  const float* bias;   // [as many] or nullptr
+  const void* res;     // [M][ldr], the type of y, or nullptr
+  void* y;             // [M][ldy], bf16 or f32
+  int64_t ldy, ldr;
+  int M, N, Kq;        // N: columns written (of y: channels and their padding)
+  int channels;        // of the layer
+  int act;
+  float alpha;
+  int f32;
+  int py;              // tile grid partition over the XCDs (set by the launcher)
+};
+constexpr int kMxDenseRows = -1;  // MxDenseTile::id of the kernel of few rows
+struct MxDenseTile {
+  int id, bm, bn, stages;
+};
+MxDenseTile choose_mxdense_tile(int64_t M, int64_t N, int64_t Kq);
+bool mxdense_tile_of(int id, MxDenseTile* t);  // false: no such tile
+// Few enough rows for the product's workgroups to quantize them for themselves (q: the rows; p.x and p.xs unused).
+bool mxdense_fuses_rows(int64_t M, int64_t N, int64_t Kq);
+hipError_t launch_mxdense_fused(const MxDenseParams& p, const MxRowsParams& q, hipStream_t s);
+hipError_t launch_mxdense(const MxDenseParams& p, MxDenseTile t, hipStream_t s);
+
 // Position rotation of the leading `heads + kv_heads` heads of each row, after
 // an optional RMS norm of each head.  theta: turns (angle / 2 pi) per position
 // of each of the rd / 2 pairs.
@@ -506,16 +552,22 @@ hipError_t launch_rotary(const RotaryParams& p, hipStream_t s);
 // Softmax attention.  Query row i of batch b and head h reads head h / group of
 // the keys and values; key j is seen while j < len_b and, causal, while
 // j < len_b - q_len + i + 1; a row that sees none is zero.
+// With parents (a tree) the keys and values are a cache that every query sees the first len_b
+// of, and query i also sees the drafted key j of each token j on its path (tree_paths.h); in
+// the tiles of the key axis the drafted keys come after the cache's last tile.
 struct AttnParams {
   const void* q;       // [batch * q_len][ldq], head h at column h D
   const void* k;       // [batch * k_len][ldk], head at column (h / group) D
   const void* v;
+  const void* k2;      // a tree's drafted keys and values: [batch * q_len][ldk2]
+  const void* v2;
   const int* lengths;  // [batch] or nullptr (k_len)
+  const int* parents;  // [batch * q_len] or nullptr (no tree)
   void* y;             // [batch * q_len][ldy]
   float* ws;           // attn_workspace() bytes when chunks > batch
-  int64_t ldq, ldk, ldv, ldy;
+  int64_t ldq, ldk, ldv, ldk2, ldv2, ldy;
   int batch, q_len, k_len, kv_heads, group, D;
-  int causal;
+  int causal, tree;
   int tile_rows, tile_keys;  // packed query rows and keys of a tile (set with chunks by choose_attention)
   int chunks;                // of the key axes of all sequences; batch: one each, no join
   float scale;
@@ -526,5 +578,29 @@ const char* attention_name(const AttnParams& p);
 int64_t attn_workspace(const AttnParams& p);
 hipError_t launch_attention(const AttnParams& p, hipStream_t s);
 hipError_t launch_attention_join(const AttnParams& p, hipStream_t s);
+
+// Rules on logits (logits.hip).  Sequence b has rows b * rows .. of x, a history of
+// clamp(lengths[b], 0, T) tokens, of which the first prompts[b] are its prompt, and E
+// bias entries; tokens outside [0, V) are passed over.
+struct LogitsParams {
+  const void* x;             // [batch * rows][ldx], bf16 or f32
+  const int* history;        // [batch][T], nullptr: no penalties
+  const int* prompts;        // [batch]
+  const int* lengths;        // [batch]
+  const float* strengths;    // [batch][3]: repetition, presence, frequency
+  const int* drafts;         // [batch * rows] or nullptr: row i is that of drafted token i
+  const int* parents;        // [batch * rows]
+  const int* bias_tokens;    // [batch][E] or nullptr
+  const float* bias_values;  // [batch][E]
+  const uint32_t* mask;      // [batch * rows][ceil(V / 32)] or nullptr
+  void* y;                   // [batch * rows][ldy], the type of x
+  int64_t ldx, ldy;
+  int batch, rows, V, T, E;
+  int cols_out;              // columns written: V, zeros up to here
+  int group;                 // rows of a workgroup (choose_logits)
+  int f32;
+};
+void choose_logits(LogitsParams& p);
+hipError_t launch_logits(const LogitsParams& p, hipStream_t s);
 
 }  // namespace byoc

@@ -12,60 +12,12 @@
 #include <type_traits>
 
 #include "lds_dma.h"
+#include "dense_epilogue.h"
 
 namespace byoc {
 namespace {
 
 using namespace dma;
-
-// 8 consecutive values of a row as they are stored, zero from column K on.  Rows are
-// any number of columns apart, so that they need only be aligned to a value: the
-// memory takes 16 bytes at any address (8000 x 513 x 3001, bf16: 83 us value by
-// value, 49 so).
-struct __attribute__((packed, aligned(4))) F32x4u {
-  float v[4];
-};
-struct __attribute__((packed, aligned(2))) Bf16x8u {
-  uint32_t v[4];
-};
-template <bool F32>
-struct Chunk;
-template <>
-struct Chunk<true> {
-  float v[8];
-  __device__ __forceinline__ void load(const void* x, int64_t row, int col, int K) {
-    const float* p = (const float*)x + row + col;
-    if (col + 8 <= K) {
-      const F32x4u a = *(const F32x4u*)p, b = *(const F32x4u*)(p + 4);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = a.v[e], v[4 + e] = b.v[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = col + e < K ? p[e] : 0.0f;
-    }
-  }
-  __device__ __forceinline__ void get(float* f) const {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = v[e];
-  }
-};
-template <>
-struct Chunk<false> {
-  uint4 u;
-  __device__ __forceinline__ void load(const void* x, int64_t row, int col, int K) {
-    const bf16_t* p = (const bf16_t*)x + row + col;
-    if (col + 8 <= K) {
-      const Bf16x8u a = *(const Bf16x8u*)p;
-      u = make_uint4(a.v[0], a.v[1], a.v[2], a.v[3]);
-    } else {
-      uint32_t w[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = col + e < K ? p[e] : 0u;
-      u = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
-    }
-  }
-  __device__ __forceinline__ void get(float* f) const { unpack8(u, f); }
-};
 
 // A row's scale, and what its codes are formed with.  The magnitudes are compared
 // as integers, which orders NaN above infinity above every number.
@@ -195,50 +147,6 @@ __device__ __forceinline__ i32x4 mma(uint4 a, uint4 b, i32x4 c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }
 
-// GELU for bf16 outputs: gelu's polynomial with exp(-a^2) straight from the hardware's
-// exp2, without the residual of the square: 18 instructions in place of 29, relative
-// error below 2^-18 down to x = -5 and 2^-16 to -9, where the output's rounding is 2^-8
-// (1024 x 768 x 3072, quantization included: 15.3 us with gelu, 13.9 with this).
-__device__ __forceinline__ float gelu_short(float v) {
-  constexpr float kErfcP[9] = {2.820777595e-01f, 2.825488448e-01f, 2.416709065e-01f, 2.090727836e-01f,
-                               -4.348613694e-02f, 3.051838875e-01f, -5.132555962e-01f, 2.983081341e-01f,
-                               -6.212075427e-02f};
-  const float a = fminf(fabsf(v) * 0.70710678118654752440f, 10.0f);
-  const float k = __builtin_amdgcn_rcpf(__builtin_fmaf(0.5f, a, 1.0f));
-  float p = kErfcP[8];
-#pragma unroll
-  for (int i = 7; i >= 0; --i) p = __builtin_fmaf(p, k, kErfcP[i]);
-  const float e = __builtin_amdgcn_exp2f(a * -1.44269504088896340736f * a);
-  const float half = 0.5f * k * p * e;  // erfc(a) / 2
-  return v * (v < 0.0f ? half : 1.0f - half);
-}
-
-// The activation, which keeps a NaN (the row of an infinity or a NaN; the clamp's
-// median would drop it).
-template <bool F32, int MODE>
-__device__ __forceinline__ float act_nan(float v, ActClamp ac) {
-  if constexpr (MODE == 1) return F32 ? gelu(v) : gelu_short(v);
-  const float y = act_apply<MODE>(v, ac);
-  return v != v ? v : y;
-}
-
-__device__ __forceinline__ void load8f(const float* p, float* v) {
-  const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
-  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-}
-
-// Eight columns of a row of the residual (zeros without one).
-template <bool F32>
-__device__ __forceinline__ Chunk<F32> load_res(const QDenseParams& p, int64_t m, int n) {
-  Chunk<F32> r;
-  if constexpr (F32) {
-    r.load(p.res, m * p.ldr, n, p.res ? p.N : 0);
-  } else {
-    r.load(p.res, m * p.ldr, n, p.res ? (p.ldr % 8 == 0 ? (int)p.ldr : p.channels) : 0);
-  }
-  return r;
-}
-
 // Eight columns of one output row: y = act(acc * scale + bias + res).  The sum meets the
 // channel's scale first: the product of the two scales alone may leave float32 where the result
 // does not (rows of 2^-64 under weights of 2^-64: the product of the scales has 7 bits left).
@@ -249,27 +157,7 @@ __device__ __forceinline__ void finish8(const QDenseParams& p, const int* acc, f
   res.get(r);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = act_nan<F32, MODE>(__builtin_fmaf((float)acc[e] * ws[e], xs, bias[e]) + r[e], ac);
-  if constexpr (F32) {
-    float* y = (float*)p.y + m * p.ldy + n;
-    if (n + 8 <= p.N) {
-      *(F32x4u*)y = F32x4u{v[0], v[1], v[2], v[3]};
-      *(F32x4u*)(y + 4) = F32x4u{v[4], v[5], v[6], v[7]};
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (n + e < p.N) y[e] = v[e];
-    }
-  } else {
-    bf16_t* y = (bf16_t*)p.y + m * p.ldy + n;
-    if (n + 8 <= p.N) {
-      const uint4 u = pack8(v);
-      *(Bf16x8u*)y = Bf16x8u{u.x, u.y, u.z, u.w};
-    } else {  // (a row of the caller's, of any width: its last columns)
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (n + e < p.N) y[e] = f32_to_bf16(v[e]);
-    }
-  }
+  store_chunk<F32>(p.y, m * p.ldy, n, p.N, v);  // (a row of the caller's, of any width, ends where it ends)
 }
 
 // BM rows x BN channels per workgroup of WM x WN waves; both operands streamed

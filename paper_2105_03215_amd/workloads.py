@@ -34,6 +34,7 @@ CONFIG_IDS = {
     "darknet53": 6,
     "inception_v3": 7,
     "decoder_layer": 8,
+    "verify_step": 9,
 }
 
 _BN_EPS = 1e-5
@@ -163,6 +164,14 @@ class GraphBuilder:
         self.shapes[name] = list(a.shape)
         return name
 
+    def param_input(self, name, values):
+        """Float32 parameters of a run (strengths, biases), given: read as they come in bf16 graphs too."""
+        a = np.ascontiguousarray(values, dtype=np.float32)
+        self.inputs.append({"name": name, "shape": list(a.shape), "dtype": "f32", "layout": "ROWMAJOR"})
+        self.input_arrays.append(a)
+        self.shapes[name] = list(a.shape)
+        return name
+
     def _after_add_act(self, m2_stream, m2_branch, act):
         if not act:
             return m2_stream + m2_branch
@@ -263,6 +272,10 @@ class GraphBuilder:
         """Dense composite on 8-bit codes with a scale for each row and each output channel."""
         return self.dense(x, n_out, op="qdense", **kw)
 
+    def mxdense(self, x, n_out, **kw):
+        """Dense composite on microscaled 4-bit floating point."""
+        return self.dense(x, n_out, op="mxdense", **kw)
+
     def rotary(self, x, positions, heads, kv_heads, head_dim, norm=False, name=None, **attrs):
         """Rotation of the leading heads of each row, with norm after an RMS norm of each head."""
         name = name or "n%d" % len(self.nodes)
@@ -291,6 +304,29 @@ class GraphBuilder:
         # the mean of n values weighted by a softmax of scores of variance 1 keeps about e / n of
         # their mean square (causal rows see n / 2 on average); the first rows keep all of it
         self.m2[name] = self.m2[v] * min(1.0, 2.0 * math.e * batch / self.shapes[k][0])
+        return name
+
+    def attention_tree(self, q, k, v, draft_k, draft_v, lengths, parents, batch, heads, head_dim, name=None, **attrs):
+        """Attention of drafted tokens over a cache and over the tokens that lead to each."""
+        name = name or "n%d" % len(self.nodes)
+        self.nodes.append({"name": name, "composite": "attention_tree",
+                           "inputs": [q, k, v, draft_k, draft_v, lengths, parents],
+                           "attrs": dict({"batch": batch, "heads": heads, "head_dim": head_dim}, **attrs),
+                           "out_dtype": self.dtype})
+        self.shapes[name] = [self.shapes[q][0], heads * head_dim]
+        self.m2[name] = self.m2[v] * min(1.0, 2.0 * math.e * batch / self.shapes[k][0])
+        return name
+
+    def logits(self, x, batch, penalties=None, drafts=None, bias=None, mask=None, name=None):
+        """Rules on logits.  penalties: (history, prompt lengths, lengths, strengths); drafts: (tokens,
+        parents); bias: (tokens, values); mask: words.  All names of inputs."""
+        name = name or "n%d" % len(self.nodes)
+        rules = [("penalties", penalties), ("drafts", drafts), ("bias", bias), ("mask", (mask,) if mask else None)]
+        self.nodes.append({"name": name, "composite": "_".join(["logits"] + [r for r, given in rules if given]),
+                           "inputs": [x] + [v for _, given in rules if given for v in given],
+                           "attrs": {"batch": batch}, "out_dtype": self.dtype})
+        self.shapes[name] = list(self.shapes[x])
+        self.m2[name] = self.m2[x]
         return name
 
     def max_pool(self, x, size=3, stride=2, pad=1, name=None, gain=None):
@@ -507,6 +543,51 @@ def decoder_layer(batch=8, tokens=128, encoder_tokens=200, hidden=768, heads=12,
     return g.finish({"batch": batch, "tokens": tokens})
 
 
+def verify_step(batch=4, drafts=16, cached=1024, hidden=768, heads=12, kv_heads=4, ffn=2048, vocab=32000, history=200,
+                dtype="bf16"):
+    """A step that verifies drafted tokens, in one engine: a tree of them for each sequence through one
+    decoder layer on microscaled 4-bit weights - attention over a cache that is read only and over the
+    drafted tokens themselves, the feed-forward block, each with its residual - and the projection to the
+    vocabulary, whose logits meet penalties for repeated tokens, biases and a mask.  The second
+    and third output hold the drafted tokens' values and rotated keys, of which the caller copies those of the
+    tokens that it accepts into its cache.  x and the cache N(0,1), W N(0, 0.02), output projections N(0, 0.01)."""
+    g = GraphBuilder("verify_step", CONFIG_IDS["verify_step"], dtype=dtype)
+    r = g.rng(200)
+    d = hidden // heads
+    qk, kv = (heads + kv_heads) * d, kv_heads * d
+    n = batch * drafts
+    parents = np.concatenate([[r.integers(-1, i) if i else -1 for i in range(drafts)] for _ in range(batch)])
+    depth = np.zeros(n, dtype=np.int64)
+    for i in range(n):
+        if parents[i] >= 0:
+            depth[i] = depth[i - i % drafts + parents[i]] + 1
+    lengths = np.array([max(0, cached * (4 - 3 * i % 5) // 4) for i in range(batch)])
+    past = np.array([max(1, history * (3 + 5 * i % 8) // 10) for i in range(batch)])
+    x = g.input("x", [n, hidden], "normal")
+    cache = g.input("cache", [batch * cached, 2 * kv], "normal")
+    pos = g.index_input("positions", np.repeat(lengths, drafts) + depth)
+    lens = g.index_input("lengths", lengths)
+    par = g.index_input("parents", parents)
+    penalties = (g.index_input("history", r.integers(0, vocab, batch * history)), g.index_input("prompts", past // 2),
+                 g.index_input("past", past),
+                 g.param_input("strengths", np.stack([1 + 0.3 * r.random(batch), r.random(batch), 0.5 * r.random(batch)], axis=1)))
+    tokens = g.index_input("tokens", r.integers(0, vocab, n))
+    bias = (g.index_input("bias_tokens", r.integers(0, vocab, batch * 8)), g.param_input("bias", r.normal(size=(batch, 8))))
+    mask = g.index_input("mask", r.integers(-2 ** 31, 2 ** 31, n * ((vocab + 31) // 32)))
+    qkv = g.mxdense(x, qk + kv, w_std=0.02, b_std=0.02, name="qkv")
+    rot = g.rotary(qkv, pos, heads, kv_heads, d, norm=True, name="rotary")
+    a = g.attention_tree(rot, cache, cache, rot, qkv, lens, par, batch, heads, d, kv_heads=kv_heads, v_col=kv,
+                         draft_k_col=heads * d, draft_v_col=qk, name="attention")
+    x = g.mxdense(a, hidden, residual=x, w_std=0.01, b_std=0.02, name="out")
+    h = g.mxdense(x, ffn, act="gelu", w_std=0.02, b_std=0.02, name="ffn1")
+    x = g.mxdense(h, hidden, residual=x, w_std=0.01, b_std=0.02, name="ffn2")
+    y = g.mxdense(x, vocab, w_std=0.02, b_std=0.02, name="vocabulary")
+    g.output(g.logits(y, batch, penalties, (tokens, par), bias, mask, name="logits"))
+    g.output(qkv)
+    g.output(rot)
+    return g.finish({"batch": batch, "drafts": drafts})
+
+
 _VGG19 = [64, 64, "M", 128, 128, "M", 256, 256, 256, 256, "M", 512, 512, 512, 512, "M",
           512, 512, 512, 512, "M"]
 
@@ -664,7 +745,7 @@ def inception_v3(n=1, hw=299, input_dtype="bf16", num_classes=1000):
 def build(name, **kw):
     """Build a workload by name: conv_f32, resnet18_block, resnet50_v1,
     resnet50_v1b, mobilenet_v2, bert_ffn, vgg19, darknet53, inception_v3,
-    decoder_layer."""
+    decoder_layer, verify_step."""
     if name == "conv_f32":
         return conv_f32(**kw)
     if name == "resnet18_block":
@@ -685,4 +766,6 @@ def build(name, **kw):
         return inception_v3(**kw)
     if name == "decoder_layer":
         return decoder_layer(**kw)
+    if name == "verify_step":
+        return verify_step(**kw)
     raise ValueError("unknown workload %r" % name)
