@@ -597,9 +597,11 @@ struct LogitsParams {
   int64_t ldx, ldy;
   int batch, rows, V, T, E;
   int cols_out;              // columns written: V, zeros up to here
-  int group;                 // rows of a workgroup (choose_logits)
+  int group, chunks, threads;  // rows, chunks of the vocabulary and threads of a workgroup (set by choose_logits)
+  int count_bits;            // of a table word
   int f32;
 };
+bool logits_word_fits(int64_t history, int64_t entries);  // of a sequence, what a table word has room for
 void choose_logits(LogitsParams& p);
 hipError_t launch_logits(const LogitsParams& p, hipStream_t s);
 
