@@ -92,7 +92,8 @@
  *                     s c with s = 2^(floor(log2 max|v|) - 2), at least 2^-127, and c the nearest
  *                     of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (ties to the even code); the
  *                     products of these summed in float32, then bias, residual and
- *                     activation.  A row that holds an infinity or a NaN gives NaN.
+ *                     activation.  A row that holds an infinity or a NaN gives NaN; terms
+ *                     whose magnitudes sum to more than float32 holds may give an infinity or a NaN.
  *                     K <= 131072.
  *   attention_tree    queries [B T, *], keys and values of a cache [B Lk, *] each, drafted
  *                     keys and values [B T, *] each, lengths [B] (i32), parents [B T] (i32)

@@ -1314,9 +1314,7 @@ void Planner::plan_mxdense(int ni) {
   const auto& xs = g.values[n.data].shape;
   const auto& ws = g.values[n.weight].shape;
   const int M = (int)xs[0], K = (int)xs[1], N = (int)ws[0];
-  const int Kq = (int)rup(K, 256), rows = (int)rup(N, kRowPad), Mq = (int)rup(M, 32);
-  auto packed = [&](int64_t r) { return r * (Kq / 2); };       // bytes of r rows' codes
-  auto scales = [&](int64_t r) { return r / 32 * Kq; };        // and of their scales
+  const int Kq = (int)rup(K, 256), rows = (int)rup(N, kRowPad), Mq = (int)rup(M, 64);
   Launch L;
   const bool fused = L.fused = mxdense_fuses_rows(M, cp[n.out], Kq);
   Launch& Q = mx_of[n.data];
@@ -1332,8 +1330,8 @@ void Planner::plan_mxdense(int ni) {
     Q.info.kind = BYOC_K_MXDENSE;
     Q.info.node = ni;
     Q.x = loc[n.data];
-    Q.qr_scales = rup(packed(Mq), 256);
-    Q.y = arena(Q.qr_scales + scales(Mq));
+    Q.qr_scales = rup(mx_code_bytes(Mq, Kq), 256);
+    Q.y = arena(Q.qr_scales + mx_scale_bytes(Mq, Kq));
     Q.mr = r;
     Q.info.bytes = act_bytes(n.data) + (int64_t)M * (K / 2 + (K + 31) / 32);
     name(Q, "mx_rows");
@@ -1351,10 +1349,14 @@ void Planner::plan_mxdense(int ni) {
   }
   L.y = loc[n.out];
   if (n.residual >= 0) L.res = loc[n.residual];
-  L.w = wslot(packed(rows));
-  L.w2 = wslot(scales(rows));
+  L.w = wslot(mx_code_bytes(rows, Kq));
+  L.w2 = wslot(mx_scale_bytes(rows, Kq));
+  L.mt = choose_mxdense_tile(M, cp[n.out], Kq);
+  // BYOC_MXDENSE_TILE=<id>: that tile wherever a tile is chosen (tests run every one with it)
+  if (const char* ev = std::getenv("BYOC_MXDENSE_TILE"); ev && L.mt.id != kMxDenseRows) (void)mxdense_tile_of(std::atoi(ev), &L.mt);
   PackJob j{PackJob::MxDenseW, g.values[n.weight].index, L.w.off};
   j.K = N, j.rows = rows, j.Kgp = Kq, j.n = K;
+  j.Cg = mx_weight_order(L.mt);
   j.dst2 = L.w2.off;
   jobs.push_back(j);
   if (n.bias >= 0) {
@@ -1364,6 +1366,7 @@ void Planner::plan_mxdense(int ni) {
     jobs.push_back(b);
   }
   MxDenseParams& p = L.mx;
+  p.blocks = rows / 16;
   p.M = M, p.N = cp[n.out], p.Kq = Kq;
   p.ldy = cp[n.out];
   p.ldr = n.residual >= 0 ? cp[n.residual] : 0;
@@ -1371,9 +1374,6 @@ void Planner::plan_mxdense(int ni) {
   p.act = (int)n.act;
   p.alpha = n.alpha;
   p.f32 = !bf16;
-  L.mt = choose_mxdense_tile(p.M, p.N, Kq);
-  // BYOC_MXDENSE_TILE=<id>: that tile wherever a tile is chosen (tests run every one with it)
-  if (const char* ev = std::getenv("BYOC_MXDENSE_TILE"); ev && L.mt.id != kMxDenseRows) (void)mxdense_tile_of(std::atoi(ev), &L.mt);
   if (L.mt.id == kMxDenseRows) std::snprintf(L.info.name, sizeof(L.info.name), "mxdense_rows_m%d%s", M, fused ? "_fused" : "");
   else std::snprintf(L.info.name, sizeof(L.info.name), "mxdense_%dx%d_s%d", L.mt.bm, L.mt.bn, L.mt.stages);
   e->launches.push_back(L);
@@ -2915,7 +2915,7 @@ Status build_device_state(Engine* e, Planner& pl, const byoc_const* consts) {
           err = launch_quant_rows({src, (int8_t*)dst, (float*)(e->weights + j.dst2), j.n, j.K, j.rows, j.n, j.Kgp, !sb}, nullptr);
           break;
         case PackJob::MxDenseW:
-          err = launch_mx_rows({src, (uint8_t*)dst, (uint8_t*)e->weights + j.dst2, j.n, j.K, j.rows, j.n, j.Kgp, !sb}, nullptr);
+          err = launch_mx_rows({src, (uint8_t*)dst, (uint8_t*)e->weights + j.dst2, j.n, j.K, j.rows, j.n, j.Kgp, !sb, j.Cg}, nullptr);
           break;
       }
     }

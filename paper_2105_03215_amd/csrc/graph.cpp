@@ -709,6 +709,9 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
         return uerr(where + ": reduction of more than 131072 elements on 8-bit codes");
       if (n.op == OpKind::MxDense && xs[1] > 131072)  // 256 rows of a tile are addressed in 31 bits
         return uerr(where + ": reduction of more than 131072 elements on 4-bit codes");
+      // (codes, padded to 256 along both axes and two a byte, are addressed in 31 bits)
+      if (n.op == OpKind::MxDense && (std::max(xs[0], ws[0]) + 255) / 256 * 256 * ((xs[1] + 255) / 256 * 256) >= int64_t(1) << 32)
+        return uerr(where + ": more than 2^32 4-bit codes, padded to blocks of 256, of " + shape_str(xs) + " or " + shape_str(ws));
     } else if (n.op == OpKind::MaxPool) {
       if (xs.size() != 4) return serr(where + ": data must be 4-D NCHW, got " + shape_str(xs));
       if (!attrs || !attrs->get("pool_size")) return perr(where + ": attrs.pool_size missing");

@@ -488,25 +488,27 @@ hipError_t launch_qdense(const QDenseParams& p, QDenseTile t, hipStream_t s);
 // values along a row under a shared power of two 2^(s - 127), s = max(E, 2) - 2 with E the
 // biased exponent of the block's largest magnitude (255 for a block that holds an infinity
 // or a NaN); a code is the value over it, rounded to 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (ties to even,
-// what lies past 6 to 6) and a sign bit.  `rows` rows (a multiple of 32) of Kq codes (a multiple of
-// 256) are written, zero past row M and column K: two codes a byte, the first in the lower
-// half, and the scales in the order that the product's lanes take them in (mxdense.hip).
+// what lies past 6 to 6) and a sign bit.  `rows` rows (a multiple of 64) of Kq codes (a multiple of
+// 256) are written, zero past row M and column K, in the order in which the product takes them (mxdense.hip).
 struct MxRowsParams {
   const void* x;   // [M][ldx], bf16 or f32
-  uint8_t* q;      // [rows][Kq / 2]
-  uint8_t* scale;  // [rows / 32][Kq / 256][256]
+  uint8_t* q;      // mx_code_bytes
+  uint8_t* scale;  // mx_scale_bytes
   int64_t ldx;
   int M, rows, K, Kq;
   int f32;
+  int order;       // 0: activations; mx_weight_order: weights
 };
+int64_t mx_code_bytes(int64_t rows, int64_t Kq);
+int64_t mx_scale_bytes(int64_t rows, int64_t Kq);
 hipError_t launch_mx_rows(const MxRowsParams& p, hipStream_t s);
 
 // y[m][n] = act(sum_k x[m][k] w[n][k] + bias[n] (+ res[m][n])) on microscaled codes,
 // the sum in float32.
 struct MxDenseParams {
-  const uint8_t* x;    // [M][Kq / 2], rows of a multiple of 32
+  const uint8_t* x;    // codes of rows up to a multiple of 64
   const uint8_t* xs;   // scales
-  const uint8_t* w;    // [rows of a multiple of 256][Kq / 2], zero past the channels
+  const uint8_t* w;    // codes of channels up to a multiple of 256
   const uint8_t* ws;   // scales
   const float* bias;   // [as many] or nullptr
   const void* res;     // [M][ldr], the type of y, or nullptr
@@ -514,6 +516,7 @@ struct MxDenseParams {
   int64_t ldy, ldr;
   int M, N, Kq;        // N: columns written (of y: channels and their padding)
   int channels;        // of the layer
+  int blocks;          // of 16 channels, of the weight
   int act;
   float alpha;
   int f32;
@@ -525,6 +528,7 @@ struct MxDenseTile {
 };
 MxDenseTile choose_mxdense_tile(int64_t M, int64_t N, int64_t Kq);
 bool mxdense_tile_of(int id, MxDenseTile* t);  // false: no such tile
+int mx_weight_order(MxDenseTile t);            // of the weights that the tile's kernel multiplies
 // Few enough rows for the product's workgroups to quantize them for themselves (q: the rows; p.x and p.xs unused).
 bool mxdense_fuses_rows(int64_t M, int64_t N, int64_t Kq);
 hipError_t launch_mxdense_fused(const MxDenseParams& p, const MxRowsParams& q, hipStream_t s);

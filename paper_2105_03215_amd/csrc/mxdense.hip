@@ -9,6 +9,7 @@
 // A block's scale is a power of two and every product of two codes a multiple of 1/4 of at
 // most 36, so that only the float32 sum rounds.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <type_traits>
 
@@ -23,13 +24,27 @@ using namespace dma;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
-// Where the scale of row r's block c stands.  A stage of 256 codes of 32 rows has 64 words of
-// scales, one for each lane of a wave: lane 16 (c % 4) + 4 (r % 32 / 8) + r % 4 has those of rows
-// r and r + 4, each for the stage's two steps of 128 codes.
-__device__ __forceinline__ int64_t mx_scale_at(int64_t r, int c, int Kq) {
-  const int lr = (int)(r % 32) / 8 * 4 + (int)(r % 4);
-  return ((r / 32 * (Kq / 256) + c / 8) * 64 + c % 4 * 16 + lr) * 4 + (r / 4 % 2) * 2 + c / 4 % 2;
+constexpr int kStep = 128;  // codes along the reduction of a matrix instruction
+
+// Codes and scales are kept in the order that the matrix instructions' lanes take them in: a block of 16 rows and
+// a step of 128 codes is 1 KB, lane l's 16 bytes those of row l % 16 and of the 32 codes l / 16, which share a
+// scale; it is moved to LDS and from there to registers without a calculated address or a bank conflict.  The blocks of a
+// step follow one another, then those of the next step: workgroups that multiply different rows of a weight are at about the
+// same step, and so read one stretch of memory together instead of places a power of two apart.
+//
+// Row r of a tensor is row r % 16 of block r / 16; of a weight that the tiles multiply (CHANNELS) the two
+// blocks of 32 rows hold rows 8 (l / 4) + l % 4 and those 4 further on, so that a lane of the result has 8
+// consecutive channels.
+enum Order { ROWS = 0, CHANNELS = 1, ALONE = 2 };
+struct Place {
+  int block, lane;
+};
+__device__ __forceinline__ Place place_of(int r, int order) {
+  if (order != CHANNELS) return Place{r >> 4, r & 15};
+  return Place{(r >> 5) * 2 + (r >> 2 & 1), (r >> 3 & 3) * 4 + (r & 3)};
 }
+// Scales: a word for each lane, of four blocks in a row and one step; of a weight that the few-row kernel multiplies
+// (ALONE, in the order of rows) of one block and four steps in a row.
 
 // The magnitudes' largest bits of 8 values.  They are compared as integers, which orders NaN
 // above infinity above every number.
@@ -78,33 +93,40 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {
   return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));  // 2 3 0 1
 }
 
-// 32 rows x a stage of 256 codes per workgroup, 4 lanes of 8 values to a block; the stage's
-// scales leave as whole words through LDS.
+// 64 rows x a step of 128 codes per workgroup (ALONE: 16 rows x 4 steps), 4 lanes of 8 values to a block of 32;
+// the 4 KB of codes and 256 bytes of scales leave through LDS as they lie in memory.
 template <bool F32>
 __global__ __launch_bounds__(256) void mx_rows_kernel(MxRowsParams p) {
+  __shared__ __align__(16) uint32_t codes[1024];
   __shared__ uint32_t words[64];
-  const int tid = threadIdx.x, nst = p.Kq / 256;
-  const int rg = blockIdx.x / nst, st = blockIdx.x - rg * nst;
-  const int c = tid & 31, col = st * 256 + c * 8;
+  const int tid = threadIdx.x, steps = p.Kq / kStep;
+  const bool alone = p.order == ALONE;
+  const int across = alone ? (steps + 3) / 4 : steps;
+  const int g = blockIdx.x / across, a = blockIdx.x - g * across;
+  const int row0 = g * (alone ? 16 : 64), step0 = a * (alone ? 4 : 1);
+  // pass i: 16 rows of a step (ALONE: the i-th step of the rows)
+  const int c = tid & 15;
   Chunk<F32> v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int row = rg * 32 + i * 8 + (tid >> 5);
+    const int row = row0 + (alone ? 0 : i * 16) + (tid >> 4), col = (step0 + (alone ? i : 0)) * kStep + c * 8;
     v[i].load(p.x, (int64_t)row * p.ldx, col, row < p.M ? p.K : 0);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int r = i * 8 + (tid >> 5);
+    const Place at = place_of((alone ? 0 : i * 16) + (tid >> 4), p.order);
+    const int block = alone ? i : at.block, lane = (c >> 2) * 16 + at.lane;
     const uint32_t byte = scale_byte(quad_max(top_bits(v[i])));
-    *(uint32_t*)(p.q + (int64_t)(rg * 32 + r) * (p.Kq / 2) + col / 2) = codes_of(v[i], scale_power(byte));
-    if ((c & 3) == 0) ((uint8_t*)words)[mx_scale_at(r, c >> 2, 256)] = (uint8_t)byte;
+    codes[(block * 64 + lane) * 4 + (c & 3)] = codes_of(v[i], scale_power(byte));
+    if ((c & 3) == 0) ((uint8_t*)words)[lane * 4 + block] = (uint8_t)byte;
   }
   __syncthreads();
-  if (tid < 64) ((uint32_t*)p.scale)[(int64_t)blockIdx.x * 64 + tid] = words[tid];
+  const int block = tid >> 6, lane = tid & 63;
+  const int blocks = p.rows / 16;
+  const int64_t at = alone ? (int64_t)(step0 + block) * blocks + g : (int64_t)a * blocks + g * 4 + block;
+  if (!alone || step0 + block < steps) ((uint4*)p.q)[at * 64 + lane] = ((const uint4*)codes)[tid];
+  if (tid < 64) ((uint32_t*)p.scale)[((int64_t)a * (alone ? blocks : blocks / 4) + g) * 64 + tid] = words[tid];
 }
-
-constexpr int kCH = 8;         // 16-byte chunks of an LDS row
-constexpr int kStageK = 256;   // codes of a stage: 128 bytes of a row
 
 // D += A B of 128 codes, each with the scale byte SA / SB of its lane's word.
 template <int SA, int SB>
@@ -114,16 +136,24 @@ __device__ __forceinline__ f32x4 mma(uint4 a, uint4 b, f32x4 c, uint32_t sa, uin
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, 4, 4, SA, (int)sa, SB, (int)sb);
 }
 
-// 4 bytes per lane from a buffer straight into LDS (the form of lds_fill16).
+// A block (16 bytes per lane) or a word per lane from a buffer straight into LDS, `at` bytes on (as lds_fill16).
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void lds_fill4(i32x4 rsrc, uint32_t lds_addr, uint32_t voff) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+__device__ __forceinline__ void fill_block(i32x4 rsrc, uint32_t lds_addr, uint32_t voff, int at) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                :
-               : "s"(lds_addr), "v"(voff), "s"(rsrc)
+               : "s"(lds_addr), "v"(voff), "s"(rsrc), "s"(at)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void fill_words(i32x4 rsrc, uint32_t lds_addr, uint32_t voff, int at) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, %3 offen lds"
+               :
+               : "s"(lds_addr), "v"(voff), "s"(rsrc), "s"(at)
                : "memory", "m0");
 }
 #pragma clang diagnostic pop
+
+constexpr int kNoAct = 4;  // of an epilogue without an activation (its others are act_apply's)
 
 // Eight columns of one output row.
 template <bool F32, int MODE, class P>
@@ -137,25 +167,23 @@ __device__ __forceinline__ void finish8(const P& p, const float* acc, const floa
 }
 
 // BM rows x BN channels per workgroup of WM x WN waves; codes and scales of both operands streamed
-// HBM -> LDS in stages of 256 codes through a ring of NS, the MFMA operands of a step of 128 codes read
-// while the previous step multiplies.  Both operands' rows are permuted within 32 (MFMA row r of tile i is
-// row 32 (i / 2) + 8 (r / 4) + 4 (i % 2) + r % 4): a lane then has one word of scales for a pair of tiles
-// and a stage, and 8 consecutive channels of an output row.
-template <int BM, int BN, int WM, int WN, int NS, bool F32>
+// HBM -> LDS through a ring of NS stages of KS steps of 128 codes, with one barrier a stage, the MFMA operands of a
+// step read while the previous step multiplies.
+template <int BM, int BN, int WM, int WN, int KS, int NS, bool F32>
 __global__ __launch_bounds__(64 * WM * WN) void mxdense_kernel(MxDenseParams p) {
-  constexpr int kNT = 64 * WM * WN, NW = WM * WN;
-  constexpr int kRowsPerPass = kNT / kCH;
+  constexpr int NW = WM * WN;
   constexpr int WTM = BM / WM, WTN = BN / WN;
   constexpr int TM = WTM / 16, TN = WTN / 16;
-  constexpr int AR = BM / kRowsPerPass, BR = BN / kRowsPerPass;
-  constexpr int GM = BM / 32, GN = BN / 32;      // groups of 32 rows: 256 bytes of scales a stage each
-  constexpr int SR = (GM + GN + NW - 1) / NW;    // of them a wave
-  static_assert(BM % kRowsPerPass == 0 && BN % kRowsPerPass == 0 && kRowsPerPass % 16 == 0, "fill shape");
+  constexpr int GM = BM / 16, GN = BN / 16;                // blocks of a step
+  constexpr int SM = (BM + 63) / 64, SN = (BN + 63) / 64;  // words of scales a lane
+  constexpr int AR = GM * KS / NW, BR = GN * KS / NW, SR = ((SM + SN) * KS + NW - 1) / NW;  // of them a wave and stage
+  static_assert(GM * KS % NW == 0 && GN * KS % NW == 0, "fill shape");
   static_assert(WTM % 16 == 0 && WTN % 32 == 0, "wave tile: whole MFMA rows, pairs of channel tiles");
-  static_assert(TM % 2 == 0 || (TM == 1 && WM == 2), "row tiles in pairs");
+  static_assert((TM % 4 == 0 || 4 % TM == 0) && (TN % 4 == 0 || 4 % TN == 0), "scales: whole words or a part of one");
+  static_assert(KS == 2 || (KS == 1 && NS % 2 == 0), "turns of one step come in pairs");
   constexpr int LPS = AR + BR + SR;
-  constexpr int CODES = (BM + BN) * kCH;           // uint4 per stage
-  constexpr int STAGE = CODES + SR * NW * 16;      // with the scales
+  constexpr int CODES = (GM + GN) * KS * 64;    // uint4 per stage
+  constexpr int STAGE = CODES + SR * NW * 16;   // with the scales
   static_assert(NS >= 2 && (NS - 1) * LPS <= 63, "vmcnt immediate");
   static_assert(NS * STAGE * 16 <= kLdsLimit, "LDS");
   __shared__ uint4 ring[NS * STAGE];
@@ -163,222 +191,299 @@ __global__ __launch_bounds__(64 * WM * WN) void mxdense_kernel(MxDenseParams p) 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
-  const int r0 = tid / kCH;
-  const int cv = (lane & 7) ^ ((r0 & 3) | ((r0 & 8) >> 1));
 
   // XCD x = (gx, gy) of 8 / py x py owns a block of the tile grid (workgroup b runs on XCD b % 8) and
-  // walks it in bands of 4 row tiles
+  // walks it in bands of 4 row tiles; its workgroups take every gridDim / 8-th of them
   constexpr int kBand = 4;
   const int ntm = (p.M + BM - 1) / BM, ntn = (p.N + BN - 1) / BN;
-  const int x = blockIdx.x & 7, j = blockIdx.x >> 3;
+  const int x = blockIdx.x & 7;
   const int px = 8 / p.py;
   const int mh = (ntm + px - 1) / px, nh = (ntn + p.py - 1) / p.py;
   const int gx = x / p.py, gy = x - gx * p.py;
-  const int band = j / (kBand * nh), at = j - band * kBand * nh;
-  const int bm = min(kBand, mh - band * kBand);
-  if (bm <= 0) return;
-  const int jn = at / bm;
-  const int tm = gx * mh + band * kBand + at - jn * bm, tn = gy * nh + jn;
-  if (jn >= nh || tm >= ntm || tn >= ntn) return;
-  const int m0 = tm * BM, n0 = tn * BN;
-  const int nst = p.Kq / kStageK, rb = p.Kq / 2;  // bytes of a row of codes
+  int j = blockIdx.x >> 3;
+  struct Tile {
+    int m0, n0;  // m0 < 0: none
+  };
+  auto next_tile = [&] {
+    for (; j < mh * nh; j += gridDim.x >> 3) {
+      const int band = j / (kBand * nh), at = j - band * kBand * nh;
+      const int bm = min(kBand, mh - band * kBand), jn = at / bm;
+      const int tm = gx * mh + band * kBand + at - jn * bm, tn = gy * nh + jn;
+      if (tm >= ntm || tn >= ntn) continue;
+      j += gridDim.x >> 3;
+      return Tile{tm * BM, tn * BN};
+    }
+    return Tile{-1, 0};
+  };
+  const int steps = p.Kq / kStep, stages = steps / KS;
 
-  // (rows past M and their scales read as zeros from past the buffer; weight rows are padded to 256)
-  const int live_groups = (min(BM, p.M - m0) + 31) / 32;
-  const i32x4 xr = buffer_rsrc(p.x + (int64_t)m0 * rb, min(BM, p.M - m0) * rb);
-  const i32x4 wr = buffer_rsrc(p.w + (int64_t)n0 * rb, BN * rb);
-  const i32x4 xsr = buffer_rsrc(p.xs + (int64_t)(m0 / 32) * nst * 256, live_groups * nst * 256);
-  const i32x4 wsr = buffer_rsrc(p.ws + (int64_t)(n0 / 32) * nst * 256, GN * nst * 256);
-  uint32_t avoff[AR], wvoff[BR], svoff[SR];
+  // What this wave fills of a stage: blocks wave, wave + NW, ... of each operand, step by step, and words of scales.
+  // (Blocks past the rows' last read what is there in their place: rows that are not used.)
+  const int mb = (p.M + 63) / 64 * 4, nb = p.blocks;  // blocks of the rows and of the weight, of a step
+  i32x4 xr, wr, sr[SR];
+  int x_at[AR], w_at[BR], s_at[SR], s_step[SR];  // bytes from the tile's first stage to the blocks and words of this wave's
+  auto set_tile = [&](Tile t) {
+    constexpr int kAll = 0x7FFFFFFF;
+    xr = buffer_rsrc(p.x + (int64_t)(t.m0 / 16) * 1024, kAll);
+    wr = buffer_rsrc(p.w + (int64_t)(t.n0 / 16) * 1024, kAll);
 #pragma unroll
-  for (int i = 0; i < AR; ++i) avoff[i] = (uint32_t)((r0 + i * kRowsPerPass) * rb + cv * 16);
+    for (int i = 0; i < AR; ++i) {
+      const int g = i * NW + wave;
+      x_at[i] = (g / GM * mb + min(g % GM, mb - 1 - t.m0 / 16)) * 1024;
+    }
 #pragma unroll
-  for (int i = 0; i < BR; ++i) wvoff[i] = (uint32_t)((r0 + i * kRowsPerPass) * rb + cv * 16);
+    for (int i = 0; i < BR; ++i) {
+      const int g = i * NW + wave;
+      w_at[i] = (g / GN * nb + g % GN) * 1024;
+    }
 #pragma unroll
-  for (int i = 0; i < SR; ++i) {  // (uniform over a wave but for the lane)
+    for (int i = 0; i < SR; ++i) {
+      const int g = min(i * NW + wave, (SM + SN) * KS - 1), of = g % (SM + SN);
+      const bool rows = of < SM;
+      sr[i] = buffer_rsrc(rows ? p.xs + (int64_t)min(t.m0 / 64 + of, mb / 4 - 1) * 256
+                               : p.ws + (int64_t)(t.n0 / 64 + of - SM) * 256, kAll);
+      s_step[i] = (rows ? mb : nb) / 4 * 256;
+      s_at[i] = g / (SM + SN) * s_step[i];
+    }
+  };
+  Tile tile = next_tile();
+  if (tile.m0 < 0) return;
+  set_tile(tile);
+  const uint32_t off16 = lane * 16, off4 = lane * 4;
+  // (Scalar instructions are not hidden where a SIMD has one wave: what can be is formed once, per wave or per stage.)
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(ring));
+  uint32_t x_to[AR], w_to[BR];  // LDS places of the blocks in slot 0
+#pragma unroll
+  for (int i = 0; i < AR; ++i) {
     const int g = i * NW + wave;
-    svoff[i] = g < GM + GN ? (uint32_t)((g < GM ? g : g - GM) * nst * 256 + lane * 4) : kOOB;
+    x_to[i] = __builtin_amdgcn_readfirstlane(lds0 + (g / GM * (GM + GN) + g % GM) * 1024);
+  }
+#pragma unroll
+  for (int i = 0; i < BR; ++i) {
+    const int g = i * NW + wave;
+    w_to[i] = __builtin_amdgcn_readfirstlane(lds0 + (g / GN * (GM + GN) + GM + g % GN) * 1024);
   }
   int issued = 0;
-  auto fill = [&](int slot, auto q_tag) {
+  struct Fill {
+    uint32_t slot;  // bytes of the slot
+    int x, w, t;    // bytes of the stage's first step, and its number
+  };
+  auto next_fill = [&](int slot) {
+    const int t = min(issued, stages - 1) * KS;  // (past the last stage: what is not used)
+    ++issued;
+    return Fill{(uint32_t)(slot * STAGE * 16), t * mb * 1024, t * nb * 1024, t};
+  };
+  auto fill = [&](const Fill& f, auto q_tag) {
     constexpr int q = decltype(q_tag)::value;
-    uint4* dst = ring + slot * STAGE;
-    const bool live = issued < nst;
-    if constexpr (q < AR) {
-      lds_fill16(xr, __builtin_amdgcn_readfirstlane(lds_addr(dst + (q * kRowsPerPass + wave * 8) * kCH)),
-                 live ? avoff[q] + (uint32_t)(issued * 128) : kOOB);
-    } else if constexpr (q < AR + BR) {
-      lds_fill16(wr, __builtin_amdgcn_readfirstlane(lds_addr(dst + (BM + (q - AR) * kRowsPerPass + wave * 8) * kCH)),
-                 live ? wvoff[q - AR] + (uint32_t)(issued * 128) : kOOB);
-    } else {
-      constexpr int i = q - AR - BR;
-      const int g = i * NW + wave;
-      lds_fill4(g < GM ? xsr : wsr, __builtin_amdgcn_readfirstlane(lds_addr(dst + CODES + g * 16)),
-                live ? svoff[i] + (uint32_t)(issued * 256) : kOOB);
-    }
+    if constexpr (q < AR)
+      fill_block(xr, x_to[q] + f.slot, off16, x_at[q] + f.x);
+    else if constexpr (q < AR + BR)
+      fill_block(wr, w_to[q - AR] + f.slot, off16, w_at[q - AR] + f.w);
+    else
+      fill_words(sr[q - AR - BR], lds0 + CODES * 16 + ((q - AR - BR) * NW + wave) * 256 + f.slot, off4,
+                 s_at[q - AR - BR] + f.t * s_step[q - AR - BR]);
   };
 
   f32x4 acc[TN][TM];
-#pragma unroll
-  for (int i = 0; i < TN; ++i)
-#pragma unroll
-    for (int k = 0; k < TM; ++k) acc[i][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
   const int lr = lane & 15, lc = lane >> 4;
-  const int prow = 8 * (lr >> 2) + (lr & 3);
-  constexpr bool LONE = TM == 1;  // (a wave has one tile of a pair of row tiles)
-  const int wrow = LONE ? 4 * wm : wm * WTM;
-  int arow[2], brow[2];
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    const int ch = (ks * 4 + lc) ^ ((lr & 3) | (lr & 4));
-    arow[ks] = (wrow + prow) * kCH + ch;
-    brow[ks] = (BM + wn * WTN + prow) * kCH + ch;
-  }
+  constexpr int PM = (TM + 3) / 4, PN = (TN + 3) / 4;
   struct Frags {
     uint4 a[TN], b[TM];
+    uint32_t sa[PN], sb[PM];
   };
-  constexpr int PM = (TM + 1) / 2, PN = TN / 2;
-  struct Scales {
-    uint32_t a[PN], b[PM];
-  };
-  constexpr int NR = TN + TM;
+  constexpr int NR = TN + TM + PN + PM;
   auto read1 = [&](Frags& f, int slot, auto ks_tag, auto q_tag) {
-    constexpr int ks = decltype(ks_tag)::value, q = decltype(q_tag)::value;
-    const uint4* st = ring + slot * STAGE;
-    if constexpr (q < TN)
-      f.a[q] = st[brow[ks] + ((q >> 1) * 32 + (q & 1) * 4) * kCH];
+    constexpr int q = decltype(q_tag)::value, ks = decltype(ks_tag)::value;
+    const uint4* const st = ring + slot * STAGE + ks * (GM + GN) * 64 + lane;
+    const uint32_t* const sc = (const uint32_t*)(ring + slot * STAGE + CODES) + ks * (SM + SN) * 64 + lane;
+    if constexpr (q < PN)
+      f.sa[q] = sc[(SM + wn * TN / 4 + q) * 64];
+    else if constexpr (q < PN + PM)
+      f.sb[q - PN] = sc[(wm * TM / 4 + q - PN) * 64];
+    else if constexpr (q < PN + PM + TN)
+      f.a[q - PN - PM] = st[(GM + wn * TN + q - PN - PM) * 64];
     else
-      f.b[q - TN] = st[arow[ks] + (((q - TN) >> 1) * 32 + ((q - TN) & 1) * 4) * kCH];
+      f.b[q - PN - PM - TN] = st[(wm * TM + q - PN - PM - TN) * 64];
   };
-  auto read_scales = [&](Scales& s, int slot) {
-    const uint32_t* at = (const uint32_t*)(ring + slot * STAGE + CODES) + lane;
-#pragma unroll
-    for (int i = 0; i < PN; ++i) s.a[i] = at[(GM + wn * (WTN / 32) + i) * 64];
-#pragma unroll
-    for (int i = 0; i < PM; ++i) s.b[i] = at[((LONE ? 0 : wm * (WTM / 32)) + i) * 64];
-    if constexpr (LONE) s.b[0] >>= 16 * wm;
-  };
-  auto phase = [&](const Frags& cur, const Scales& sc, Frags& nxt, int rslot, auto ks_tag, int fslot, auto fill_tag) {
-    constexpr bool FILL = decltype(fill_tag)::value;
-    constexpr int ks = 1 - decltype(ks_tag)::value;  // of the step that multiplies
+  int sa_at = 0, sb_at = 0;  // bits
+  // The step in cur multiplies while step ks of a slot is read and, FILL, a slot filled.
+  auto phase = [&](const Frags& cur, Frags& nxt, int rslot, auto ks_tag, const Fill& f, auto fill_tag) {
     constexpr int RG = TM > 4 ? TM - 2 : TM;
+    // (a wave with less than four tiles has them at the place of its own in the word)
+    uint32_t sa[PN], sb[PM];
+#pragma unroll
+    for (int i = 0; i < PN; ++i) sa[i] = TN < 4 ? cur.sa[i] >> sa_at : cur.sa[i];
+#pragma unroll
+    for (int i = 0; i < PM; ++i) sb[i] = TM < 4 ? cur.sb[i] >> sb_at : cur.sb[i];
     static_for<0, TM>([&](auto jj) {
       constexpr int k = decltype(jj)::value;
       static_for<0, TN>([&](auto ii) {
         constexpr int i = decltype(ii)::value;
-        acc[i][k] = mma<(i & 1) * 2 + ks, (k & 1) * 2 + ks>(cur.a[i], cur.b[k], acc[i][k], sc.a[i >> 1], sc.b[k >> 1]);
+        acc[i][k] = mma<i & 3, k & 3>(cur.a[i], cur.b[k], acc[i][k], sa[i >> 2], sb[k >> 2]);
       });
       static_for<0, NR>([&](auto q) {
         if constexpr (decltype(q)::value * RG / NR == k) read1(nxt, rslot, ks_tag, q);
       });
-      if constexpr (FILL)
+      if constexpr (decltype(fill_tag)::value)
         static_for<0, LPS>([&](auto q) {
-          if constexpr (decltype(q)::value * TM / LPS == k) fill(fslot, q);
+          if constexpr (decltype(q)::value * TM / LPS == k) fill(f, q);
         });
       __builtin_amdgcn_sched_barrier(0);
     });
   };
 
   static_for<0, NS>([&](auto i) {
-    static_for<0, LPS>([&](auto q) { fill(decltype(i)::value, q); });
-    ++issued;
+    const Fill f = next_fill(decltype(i)::value);
+    static_for<0, LPS>([&](auto q) { fill(f, q); });
   });
   asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NS - 1) * LPS) : "memory");
   Frags f0, f1;
-  Scales sc, sn;
+  int slot = 0;
   constexpr std::integral_constant<int, 0> k0{};
   constexpr std::integral_constant<int, 1> k1{};
-  static_for<0, NR>([&](auto q) { read1(f0, 0, k0, q); });
-  read_scales(sc, 0);
-  int slot = 0;
-  for (int t = 0; t < nst; ++t) {
+  // A stage's last step is in registers, read by every wave before the barrier: its slot takes the stage NS
+  // further on, while the next stage's first step, which has landed for every wave, is read.
+  auto last_step = [&](const Frags& cur, Frags& nxt) {
     const int next = slot + 1 == NS ? 0 : slot + 1;
-    phase(f0, sc, f1, slot, k1, 0, std::false_type{});
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((NS - 2) * LPS) : "memory");
-    read_scales(sn, next);
-    phase(f1, sc, f0, next, k0, slot, std::true_type{});
-    sc = sn;
-    ++issued;
+    phase(cur, nxt, next, k0, next_fill(slot), std::true_type{});
     slot = next;
-  }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-
-  // Epilogue: lane = row of each row tile, 8 consecutive channels per pair of channel tiles; the
-  // residuals of a batch of rows are on their way together
-  const ActClamp ac = act_clamp_of(p.act, p.alpha);
-  constexpr int BATCH = F32 ? 1 : TM;
-  auto row_of = [&](int k) { return m0 + wrow + (k >> 1) * 32 + (k & 1) * 4 + prow; };
-  auto epilogue = [&](auto mode_tag) {
-#pragma unroll
-    for (int pr = 0; pr < TN / 2; ++pr) {
-      const int n = n0 + wn * WTN + pr * 32 + lc * 8;
-      if (n >= p.N) continue;
-      float bias[8];
-      if (p.bias) {
-        load8f(p.bias + n, bias);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) bias[e] = 0.0f;
+  };
+  auto turns = [&](int t, int end) {
+    if constexpr (KS == 2) {
+      for (; t < end; ++t) {
+        phase(f0, f1, slot, k1, Fill{}, std::false_type{});
+        last_step(f1, f0);
       }
-#pragma unroll
-      for (int kb = 0; kb < TM; kb += BATCH) {
-        Chunk<F32> res[BATCH];
-#pragma unroll
-        for (int k = 0; k < BATCH; ++k) res[k] = load_res<F32>(p, min(row_of(kb + k), p.M - 1), n);
-#pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-          const int m = row_of(kb + k);
-          if (m >= p.M) continue;
-          float a[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) a[e] = acc[2 * pr + (e >> 2)][kb + k][e & 3];
-          finish8<F32, decltype(mode_tag)::value>(p, a, bias, res[k], m, n, ac);
-        }
+    } else {
+      for (; t < end; t += 2) {
+        last_step(f0, f1);
+        last_step(f1, f0);
       }
     }
   };
-  if (act_mode(p.act) == 1)
-    epilogue(std::integral_constant<int, 1>{});
-  else if (act_mode(p.act) == 0)
-    epilogue(std::integral_constant<int, 0>{});
-  else
-    epilogue(std::integral_constant<int, 2>{});
+  const ActClamp ac = act_clamp_of(p.act, p.alpha);
+  // Epilogue: lane = row of each row tile, 8 consecutive channels per pair of channel tiles.  It is bound by the
+  // vector ALU (at 4 cycles an instruction, 550 cycles for 8 values with their checks and a residual of zeros: 7.4 us a
+  // tile of 256 x 256 beside the 20.5 us of its product), so that whole tiles without a residual or an activation
+  // have forms of their own.
+  constexpr int NP = TN / 2, BATCH = F32 ? 1 : TM * NP > 16 ? 16 / NP : TM;  // (rows whose residuals are on their way together)
+  auto epilogue = [&](auto mode_tag, auto res_tag, auto whole_tag) {
+    const int row0 = tile.m0 + wm * WTM + lr, col0 = tile.n0 + wn * WTN + lc * 8;
+    constexpr int MODE = decltype(mode_tag)::value;
+    constexpr bool RES = decltype(res_tag)::value, WHOLE = decltype(whole_tag)::value;
+    float bias[NP][8];
+#pragma unroll
+    for (int pr = 0; pr < NP; ++pr) {
+      if (p.bias) {
+        load8f(p.bias + col0 + pr * 32, bias[pr]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bias[pr][e] = 0.0f;
+      }
+    }
+#pragma unroll
+    for (int kb = 0; kb < TM; kb += BATCH) {
+      Chunk<F32> res[RES ? BATCH : 1][NP];
+      if constexpr (RES) {
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+#pragma unroll
+          for (int pr = 0; pr < NP; ++pr) {
+            if constexpr (WHOLE) res[k][pr].load(p.res, (row0 + (kb + k) * 16) * p.ldr, col0 + pr * 32, INT_MAX);
+            else res[k][pr] = load_res<F32>(p, min(row0 + (kb + k) * 16, p.M - 1), col0 + pr * 32);
+          }
+      }
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k)
+#pragma unroll
+        for (int pr = 0; pr < NP; ++pr) {
+          const int m = row0 + (kb + k) * 16, n = col0 + pr * 32;
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = acc[2 * pr + (e >> 2)][kb + k][e & 3] + bias[pr][e];
+          if constexpr (RES) {
+            float r[8];
+            res[k][pr].get(r);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += r[e];
+          }
+          if constexpr (MODE != kNoAct) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = act_nan<F32, MODE>(v[e], ac);
+          }
+          if constexpr (WHOLE) store_chunk<F32>(p.y, m * p.ldy, n, INT_MAX, v);
+          else if (m < p.M && n < p.N) store_chunk<F32>(p.y, m * p.ldy, n, p.N, v);
+        }
+    }
+  };
+  auto finish = [&](auto mode_tag) {
+    const bool whole = tile.m0 + BM <= p.M && tile.n0 + BN <= min(p.N, p.channels);
+    if (p.res) {
+      if (whole) epilogue(mode_tag, std::true_type{}, std::true_type{});
+      else epilogue(mode_tag, std::true_type{}, std::false_type{});
+    } else {
+      if (whole) epilogue(mode_tag, std::false_type{}, std::true_type{});
+      else epilogue(mode_tag, std::false_type{}, std::false_type{});
+    }
+  };
+  // The last turns of a tile fill the ring with the first steps of the next one, which land during the epilogue.
+  for (;;) {
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int k = 0; k < TM; ++k) acc[i][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    sa_at = 8 * ((wn * TN + tile.n0 / 16) % 4), sb_at = 8 * ((wm * TM + tile.m0 / 16) % 4);
+    static_for<0, NR>([&](auto q) { read1(f0, slot, k0, q); });
+    turns(0, stages - NS);
+    const Tile next = next_tile();
+    if (next.m0 >= 0) {
+      set_tile(next);
+      issued = 0;
+    }
+    turns(max(0, stages - NS), stages);
+    if (p.act == kActNone)
+      finish(std::integral_constant<int, kNoAct>{});
+    else if (act_mode(p.act) == 1)
+      finish(std::integral_constant<int, 1>{});
+    else
+      finish(std::integral_constant<int, 0>{});
+    if (next.m0 < 0) break;
+    tile = next;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 // Few rows: a workgroup of 8 waves owns 16 channels and all rows and splits the reduction over its waves, a
-// stage of 256 codes each in turn, operands straight to registers, the waves' sums joined in LDS in their
-// order; the time is that of reading the weights.  MT tiles of 16 rows.
+// step of 128 codes each in turn, operands straight to registers, the waves' sums joined in LDS in their
+// order; the time is that of reading the weights.  MT blocks of 16 rows.
 //
 // FUSED: the rows are quantized by every workgroup for itself, into LDS, while its first weights are on their
 // way; that saves the launch that would do it.
 constexpr int kRowWaves = 8;
 constexpr int kRowThreads = 64 * kRowWaves;
-constexpr int kRowStages = 2;  // stages per wave with loads in flight together
-constexpr int kFusedCodes = 16 * kRowThreads;  // codes of all rows that FUSED takes
+constexpr int kRowSteps = 4;                   // steps per wave with loads in flight together
+constexpr int kFusedCodes = 64 * kRowThreads;  // codes of all rows that FUSED takes
 
 template <int MT, bool F32, bool FUSED>
 __global__ __launch_bounds__(kRowThreads) void mxdense_rows_kernel(MxDenseParams p, MxRowsParams q) {
   __shared__ f32x4 red[kRowWaves][MT][64];
-  __shared__ __align__(16) uint8_t codes[FUSED ? kFusedCodes / 2 : 16];
-  __shared__ __align__(4) uint8_t scales[FUSED ? kFusedCodes / 32 : 4];  // [row][stage][block % 4][step]
+  __shared__ __align__(16) uint8_t codes[FUSED ? kFusedCodes / 2 : 16];  // [row][Kq / 2]
+  __shared__ uint8_t scales[FUSED ? kFusedCodes / 32 : 4];               // [row][Kq / 32]
   const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lc = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n0 = blockIdx.x * 16;
-  const int nst = p.Kq / kStageK, rb = p.Kq / 2;
-  const uint8_t* wp = p.w + (int64_t)(n0 + lr) * rb + lc * 16;
-  const uint8_t* wsp = p.ws + mx_scale_at(n0 + lr, lc, p.Kq);
-  uint4 a[kRowStages][2];
-  uint32_t as[kRowStages];
+  const int steps = p.Kq / kStep;
+  const uint4* const wp = (const uint4*)p.w + (int64_t)blockIdx.x * 64 + lane;
+  const uint32_t* const wsp = (const uint32_t*)p.ws + (int64_t)blockIdx.x * 64 + lane;
+  uint4 a[kRowSteps];
+  uint32_t as[kRowSteps];
   auto load_w = [&](int t0) {
 #pragma unroll
-    for (int u = 0; u < kRowStages; ++u) {
+    for (int u = 0; u < kRowSteps; ++u) {
       const int t = t0 + u * kRowWaves;
-      const bool live = t < nst;
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-        a[u][ks] = live ? *(const uint4*)(wp + (int64_t)t * 128 + ks * 64) : make_uint4(0u, 0u, 0u, 0u);
-      as[u] = live ? *(const uint16_t*)(wsp + (int64_t)t * 256) : 0u;
+      a[u] = t < steps ? wp[(int64_t)t * p.blocks * 64] : make_uint4(0u, 0u, 0u, 0u);
+      as[u] = t < steps ? wsp[(int64_t)(t >> 2) * p.blocks * 64] >> (8 * (t & 3)) : 0u;
     }
   };
   // this thread's 8 outputs, and what they need besides the sums: on its way from the start
@@ -393,58 +498,57 @@ __global__ __launch_bounds__(kRowThreads) void mxdense_rows_kernel(MxDenseParams
     res = load_res<F32>(p, om, on);
   }
   if constexpr (FUSED) {
-    const int chunks = p.Kq / 8, all = chunks * p.M;  // (32 chunks a stage: 4 lanes share a block)
+    const int chunks = p.Kq / 8, all = chunks * p.M;  // (16 chunks a step: 4 lanes share a block)
     for (int i = tid; i < all; i += kRowThreads) {
       const int row = i / chunks, c = i - row * chunks;
       Chunk<F32> v;
       v.load(q.x, (int64_t)row * q.ldx, c * 8, q.K);
       const uint32_t byte = scale_byte(quad_max(top_bits(v)));
-      *(uint32_t*)(codes + row * rb + c * 4) = codes_of(v, scale_power(byte));
-      const int blk = c >> 2;
-      if ((c & 3) == 0) scales[(row * nst + (blk >> 3)) * 8 + (blk & 3) * 2 + (blk >> 2 & 1)] = (uint8_t)byte;
+      *(uint32_t*)(codes + row * (p.Kq / 2) + c * 4) = codes_of(v, scale_power(byte));
+      if ((c & 3) == 0) scales[row * (p.Kq / 32) + (c >> 2)] = (uint8_t)byte;
     }
     __syncthreads();
   }
   f32x4 acc[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int t0 = wave; t0 < nst; t0 += kRowStages * kRowWaves) {
-    uint4 b[kRowStages][MT][2];
-    uint32_t bs[kRowStages][MT];
+  for (int t0 = wave; t0 < steps; t0 += kRowSteps * kRowWaves) {
+    uint4 b[kRowSteps][MT];
+    uint32_t bs[kRowSteps];
 #pragma unroll
-    for (int u = 0; u < kRowStages; ++u) {
+    for (int u = 0; u < kRowSteps; ++u) {
       const int t = t0 + u * kRowWaves;
+      bs[u] = 0u;
 #pragma unroll
-      for (int k = 0; k < MT; ++k) {
-        const int m = k * 16 + lr;
-        const bool live = m < p.M && t < nst;
-        const uint8_t* xp = (FUSED ? codes : p.x) + (int64_t)m * rb + t * 128 + lc * 16;
+      for (int k = 0; k < MT; ++k) b[u][k] = make_uint4(0u, 0u, 0u, 0u);
+      if (t >= steps) continue;
+      if constexpr (FUSED) {
+        if (lr < p.M) {
+          b[u][0] = *(const uint4*)(codes + lr * (p.Kq / 2) + t * 64 + lc * 16);
+          bs[u] = scales[lr * (p.Kq / 32) + t * 4 + lc];
+        }
+      } else {
+        bs[u] = ((const uint32_t*)p.xs)[t * 64 + lane];  // (up to 64 rows: one word, four blocks a step)
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) b[u][k][ks] = live ? *(const uint4*)(xp + ks * 64) : make_uint4(0u, 0u, 0u, 0u);
-        const uint8_t* sp = FUSED ? scales + (m * nst + t) * 8 + lc * 2 : p.xs + mx_scale_at(m, lc, p.Kq) + (int64_t)t * 256;
-        bs[u][k] = live ? *(const uint16_t*)sp : 0u;
+        for (int k = 0; k < MT; ++k) b[u][k] = ((const uint4*)p.x)[(t * 4 + k) * 64 + lane];
       }
     }
-    uint4 w[kRowStages][2];
-    uint32_t wsc[kRowStages];
+    uint4 w[kRowSteps];
+    uint32_t wsc[kRowSteps];
 #pragma unroll
-    for (int u = 0; u < kRowStages; ++u) {
-      w[u][0] = a[u][0], w[u][1] = a[u][1];
-      wsc[u] = as[u];
-    }
-    load_w(t0 + kRowStages * kRowWaves);
+    for (int u = 0; u < kRowSteps; ++u) w[u] = a[u], wsc[u] = as[u];
+    load_w(t0 + kRowSteps * kRowWaves);
 #pragma unroll
-    for (int u = 0; u < kRowStages; ++u)
-#pragma unroll
-      for (int k = 0; k < MT; ++k) {
-        acc[k] = mma<0, 0>(w[u][0], b[u][k][0], acc[k], wsc[u], bs[u][k]);
-        acc[k] = mma<1, 1>(w[u][1], b[u][k][1], acc[k], wsc[u], bs[u][k]);
-      }
+    for (int u = 0; u < kRowSteps; ++u)
+      static_for<0, MT>([&](auto k) {
+        constexpr int K = decltype(k)::value;
+        acc[K] = mma<0, K>(w[u], b[u][K], acc[K], wsc[u], bs[u]);
+      });
   }
 #pragma unroll
   for (int k = 0; k < MT; ++k) red[wave][k][lane] = acc[k];
   __syncthreads();
-  // row m, channels n0 + 4 c .. + 3 sit in lane 16 c + m % 16 of tile m / 16 of every wave
+  // row m, channels n0 + 4 c .. + 3 sit in lane 16 c + m % 16 of block m / 16 of every wave
   if (!out) return;
   const ActClamp ac = act_clamp_of(p.act, p.alpha);
   float sum[8];
@@ -473,11 +577,13 @@ hipError_t launch_rows(const MxDenseParams& p, const MxRowsParams& q, bool fused
   if (fused) mxdense_rows_kernel<1, F32, true><<<grid, kRowThreads, 0, s>>>(p, q);
   else if (mt == 1) mxdense_rows_kernel<1, F32, false><<<grid, kRowThreads, 0, s>>>(p, q);
   else if (mt == 2) mxdense_rows_kernel<2, F32, false><<<grid, kRowThreads, 0, s>>>(p, q);
+  else if (mt == 3) mxdense_rows_kernel<3, F32, false><<<grid, kRowThreads, 0, s>>>(p, q);
+  else if (mt == 4) mxdense_rows_kernel<4, F32, false><<<grid, kRowThreads, 0, s>>>(p, q);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
 
-template <int BM, int BN, int WM, int WN, int NS, bool F32>
+template <int BM, int BN, int WM, int WN, int KS, int NS, int OCC, bool F32>
 hipError_t launch_one(MxDenseParams p, hipStream_t s) {
   // the split of the tile grid over the XCDs that has each fetch the fewest operand rows
   const int ntm = (p.M + BM - 1) / BM, ntn = (p.N + BN - 1) / BN;
@@ -487,55 +593,74 @@ hipError_t launch_one(MxDenseParams p, hipStream_t s) {
     const int64_t cost = (int64_t)mh * nh * 4096 + mh * BM + nh * BN;  // (first of all no XCD with more tiles)
     if (cost < best) best = cost, p.py = py, blocks = 8 * (int64_t)mh * nh;
   }
-  mxdense_kernel<BM, BN, WM, WN, NS, F32><<<(unsigned)blocks, 64 * WM * WN, 0, s>>>(p);
+  // (a reduction shorter than the ring leaves no room for the next tile in it: a workgroup for each)
+  if (p.Kq >= NS * KS * kStep) blocks = std::min<int64_t>(blocks, 256 * OCC);
+  mxdense_kernel<BM, BN, WM, WN, KS, NS, F32><<<(unsigned)blocks, 64 * WM * WN, 0, s>>>(p);
   return hipGetLastError();
 }
 
-// Tiles (BM, BN, waves along each, ring stages) and what they cost in microseconds: a stage of 256 codes while
-// at most one workgroup runs per CU or all slots (occ per CU) are busy, and a round's prologue and epilogue.
-//   id BM BN WM WN NS  occ  lone  busy  round
-#define BYOC_MXDENSE_TILES(X)                \
-  X(0, 256, 256, 2, 4, 2, 1, 1.33, 1.8, 9.0) \
-  X(1, 256, 128, 4, 2, 3, 1, 0.77, 1.0, 6.0) \
-  X(2, 128, 128, 2, 4, 3, 1, 0.51, 0.6, 4.2) \
-  X(3, 128, 128, 2, 4, 2, 2, 0.71, 1.09, 5.0) \
-  X(4, 128, 64, 4, 2, 3, 2, 0.39, 0.70, 3.5) \
-  X(5, 64, 64, 2, 2, 4, 2, 0.33, 0.46, 2.3)  \
-  X(6, 32, 32, 2, 1, 8, 2, 0.26, 0.30, 1.8)
+// Tiles (BM, BN, waves along each, steps of a stage, ring stages) and what they cost in microseconds: a step of 128
+// codes while at most one workgroup runs per CU or all slots (occ per CU) are busy, and a round's start and end.
+// Fitted to 22 shapes from 1 x 8192 x 12288 to 8192 x 4096 x 8192, on each of which the choice is the fastest
+// tile.  8192 x 4096 x 8192 with its quantization: 141 us as 256x256, 164 as 256x128, 176 as 128x128 twice a CU; the
+// product alone takes 20.3 us a tile for 16.6 of matrix instructions at the 8.3 PFLOP/s that they reach without
+// operands to wait for.  (256x128 twice a CU, with 4 waves of 128 x 64 each: 233 us, as the LDS and the L2 then feed 41 bytes a
+// cycle.)  With random codes the same product is a quarter slower than with equal ones: the clock gives way.
+//   id BM BN WM WN KS NS  occ  lone  busy  round
+#define BYOC_MXDENSE_TILES(X)                       \
+  X(0, 256, 256, 2, 4, 1, 4, 1, 0.535, 0.681, 7.46)  \
+  X(1, 256, 128, 4, 2, 2, 3, 1, 0.319, 0.360, 6.37)  \
+  X(2, 128, 128, 2, 4, 2, 4, 1, 0.202, 0.203, 5.17)  \
+  X(3, 128, 128, 2, 4, 2, 2, 2, 0.285, 0.443, 4.34)  \
+  X(4, 128, 64, 4, 2, 2, 3, 2, 0.136, 0.217, 5.00)   \
+  X(5, 64, 64, 2, 2, 2, 4, 2, 0.077, 0.160, 4.23)    \
+  X(6, 32, 32, 2, 1, 2, 8, 2, 0.010, 0.071, 4.45)
 
 double tile_cost(int bm, int bn, int occ, double lone, double busy, double round, int64_t M, int64_t N, int64_t Kq) {
   const int64_t tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn), slots = 256 * occ;
-  const double stages = (double)(Kq / kStageK);
+  const double stages = (double)(Kq / kStep);
   const int64_t rest = tiles % slots;
   double t = (double)(tiles / slots) * (stages * busy + round);
   if (rest) t += stages * (rest <= (occ == 1 ? 128 : 256) ? lone : busy) + round;
   return t;
 }
 
-constexpr int kRowsN = 16 * 256;  // channels of the rows kernel: a workgroup of 16 for each CU
+constexpr int64_t kRowsOutputs = 64 * 4096;  // rows (in blocks of 16) x channels that the rows kernel takes
 
 }  // namespace
 
 hipError_t launch_mx_rows(const MxRowsParams& p, hipStream_t s) {
-  if (p.rows < 1 || p.rows % 32 != 0 || p.Kq % kStageK != 0 || p.K > p.Kq) return hipErrorInvalidValue;
-  const int64_t grid = (int64_t)(p.rows / 32) * (p.Kq / kStageK);
+  if (p.rows < 1 || p.rows % 64 != 0 || p.Kq % (2 * kStep) != 0 || p.K > p.Kq) return hipErrorInvalidValue;
+  const int steps = p.Kq / kStep;
+  const int64_t grid = p.order == ALONE ? (int64_t)(p.rows / 16) * ((steps + 3) / 4) : (int64_t)(p.rows / 64) * steps;
   if (p.f32) mx_rows_kernel<true><<<(unsigned)grid, 256, 0, s>>>(p);
   else mx_rows_kernel<false><<<(unsigned)grid, 256, 0, s>>>(p);
   return hipGetLastError();
 }
 
-bool mxdense_fuses_rows(int64_t M, int64_t N, int64_t Kq) { return M <= 16 && M * Kq <= kFusedCodes && N <= kRowsN; }
+int64_t mx_code_bytes(int64_t rows, int64_t Kq) { return rows * Kq / 2; }
+int64_t mx_scale_bytes(int64_t rows, int64_t Kq) { return (rows + 15) / 16 * ((Kq / kStep + 3) / 4 * 4) * 64; }
+int mx_weight_order(MxDenseTile t) { return t.id == kMxDenseRows ? ALONE : CHANNELS; }
+
+// (1 x 4096 x 4096: 5.0 us, 7.7 with a launch for the rows; 8 x 4096 x 4096, where every workgroup quantizes 32768
+// values, 6.9 and 7.9; 1 x 8192 x 8192 9.1 and 11.9)
+bool mxdense_fuses_rows(int64_t M, int64_t N, int64_t Kq) {
+  return M <= 16 && M * Kq <= kFusedCodes && 16 * N <= kRowsOutputs;
+}
 
 hipError_t launch_mxdense_fused(const MxDenseParams& p, const MxRowsParams& q, hipStream_t s) {
   if (!mxdense_fuses_rows(p.M, p.N, p.Kq)) return hipErrorInvalidValue;
   return p.f32 ? launch_rows<true>(p, q, true, s) : launch_rows<false>(p, q, true, s);
 }
 
+// The rows kernel up to 64 rows, fewer the more channels there are (32 x 4096 x 4096: 7.5 us, 10.1 on 32x32 tiles; 64 x
+// 4096 x 4096 7.8 and 10.1; 1 x 8192 x 8192 11.8 and 14.6; but 64 x 8192 x 8192, as every workgroup reads all rows,
+// 17.1 and 15.5); else the tile of least modelled time.
 MxDenseTile choose_mxdense_tile(int64_t M, int64_t N, int64_t Kq) {
-  if (M <= 32 && N <= kRowsN) return {kMxDenseRows, (int)(M + 15) / 16 * 16, 16, 0};
+  if (M <= 64 && (M + 15) / 16 * 16 * N <= kRowsOutputs) return {kMxDenseRows, (int)(M + 15) / 16 * 16, 16, 0};
   MxDenseTile best{};
   double least = INFINITY;
-#define X(ID, BM, BN, WM, WN, NS, OCC, LONE, BUSY, ROUND)                                                \
+#define X(ID, BM, BN, WM, WN, KS, NS, OCC, LONE, BUSY, ROUND)                                                \
   if (const double c = tile_cost(BM, BN, OCC, LONE, BUSY, ROUND, M, N, Kq); c < least) least = c, best = {ID, BM, BN, NS};
   BYOC_MXDENSE_TILES(X)
 #undef X
@@ -543,7 +668,7 @@ MxDenseTile choose_mxdense_tile(int64_t M, int64_t N, int64_t Kq) {
 }
 
 bool mxdense_tile_of(int id, MxDenseTile* t) {
-#define X(ID, BM, BN, WM, WN, NS, OCC, LONE, BUSY, ROUND) \
+#define X(ID, BM, BN, WM, WN, KS, NS, OCC, LONE, BUSY, ROUND) \
   if (id == ID) return *t = {ID, BM, BN, NS}, true;
   BYOC_MXDENSE_TILES(X)
 #undef X
@@ -552,8 +677,8 @@ bool mxdense_tile_of(int id, MxDenseTile* t) {
 
 hipError_t launch_mxdense(const MxDenseParams& p, MxDenseTile t, hipStream_t s) {
   if (t.id == kMxDenseRows) return p.f32 ? launch_rows<true>(p, {}, false, s) : launch_rows<false>(p, {}, false, s);
-#define X(ID, BM, BN, WM, WN, NS, OCC, LONE, BUSY, ROUND) \
-  if (t.id == ID) return p.f32 ? launch_one<BM, BN, WM, WN, NS, true>(p, s) : launch_one<BM, BN, WM, WN, NS, false>(p, s);
+#define X(ID, BM, BN, WM, WN, KS, NS, OCC, LONE, BUSY, ROUND) \
+  if (t.id == ID) return p.f32 ? launch_one<BM, BN, WM, WN, KS, NS, OCC, true>(p, s) : launch_one<BM, BN, WM, WN, KS, NS, OCC, false>(p, s);
   BYOC_MXDENSE_TILES(X)
 #undef X
   return hipErrorInvalidValue;

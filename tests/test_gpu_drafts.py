@@ -171,13 +171,12 @@ def test_mxdense_odd_rows(m, dtype):
             x[(3 * i) % m] = to_bf16_values(row.astype(np.float32))
             y = _run("mxdense", {"x": (x, dtype)}, ["x", "w"], {}, dtype, [("w", w)])
             ref, mag = D.mxdense(x, w, magnitudes=True)
-        big = np.abs(ref) > 3e38  # (past float32: an infinity or near its end, as the additions come)
-        assert not np.isnan(y[big]).any()
-        y, ref = np.where(big, 0, y), np.where(big, 0, ref)
-        # (sums of float32 denormals may flush: absolute slack of the smallest normal)
-        big_rows = mag.max(axis=1, keepdims=True) > 3e38  # (partial sums that may have left float32)
-        _close(np.where(big_rows, 0, y) if big_rows.any() else y, np.where(big_rows & ~np.isnan(ref), 0, ref),
-               (k + 8) * 2 * E * mag + 2.0 ** -126, dtype)
+        # (where the terms' magnitudes sum to more than float32 holds, partial sums of either sign may overflow, and an
+        # infinity less an infinity is a NaN: nothing is said of those; and sums of float32 denormals may flush: an
+        # absolute slack of the smallest normal)
+        held = ~(mag > 3e38)
+        assert held.mean() > 0.1 or m == 1
+        _close(np.where(held, y, 0), np.where(held, ref, 0), np.where(held, (k + 8) * 2 * E * mag, 0) + 2.0 ** -126, dtype)
 
 
 def test_mxdense_weights_of_no_finite_value():
