@@ -1491,11 +1491,6 @@ void Planner::plan_logits(int ni) {
   p.T = n.penalties ? (int)(g.values[n.history].shape[0] / n.batch) : 0;
   p.E = n.has_bias ? (int)(g.values[n.bias_tokens].shape[0] / n.batch) : 0;
   p.f32 = !bf16;
-  if (!logits_word_fits(p.T, p.E)) {
-    err = Status::Err(BYOC_ERR_UNSUPPORTED, "node " + n.name + " (" + n.composite + "): a history of " + std::to_string(p.T) +
-                                                " tokens with " + std::to_string(p.E) + " bias entries");
-    return;
-  }
   choose_logits(p);
   name(L, n.composite.c_str());
   e->launches.push_back(L);

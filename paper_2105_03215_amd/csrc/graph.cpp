@@ -693,6 +693,17 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
           return serr(where + ": bias tokens " + shape_str(shp(n.bias_tokens)) + " are not a multiple of attrs.batch");
         if (!(st = expect(n.bias_values, "bias values", {b, shp(n.bias_tokens)[0] / b})).ok()) return st;
       }
+      // the kernel counts a token in a 32-bit word, with two marks and the number of its last bias entry
+      auto bits = [](int64_t most) {
+        int k = 0;
+        while (most >> k) ++k;
+        return k;
+      };
+      const int64_t tokens = n.penalties ? shp(n.history)[0] / b : 0, entries = n.has_bias ? shp(n.bias_tokens)[0] / b : 0;
+      if (bits(tokens + kMaxDrafts) + 2 + std::max(1, bits(entries)) > 32)
+        return uerr(where + ": a history of " + std::to_string(tokens) + " tokens with " + std::to_string(entries) +
+                    " bias entries");
+      if (xs[1] > 1 << 30) return uerr(where + ": more than 2^30 columns");
       if (n.mask && !(st = expect(n.mask_words, "mask", {xs[0] * ((xs[1] + 31) / 32)})).ok()) return st;
       oshape = xs;
     } else if (n.op == OpKind::Dense || n.op == OpKind::QDense || n.op == OpKind::MxDense) {

@@ -605,7 +605,6 @@ struct LogitsParams {
   int count_bits;            // of a table word
   int f32;
 };
-bool logits_word_fits(int64_t history, int64_t entries);  // of a sequence, what a table word has room for
 void choose_logits(LogitsParams& p);
 hipError_t launch_logits(const LogitsParams& p, hipStream_t s);
 

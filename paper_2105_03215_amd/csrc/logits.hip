@@ -280,18 +280,7 @@ hipError_t launch_rules(const LogitsParams& p, hipStream_t s) {
   return hipErrorInvalidValue;
 }
 
-int bits_of(uint32_t n) {
-  int k = 0;
-  while (k < 32 && n >> k) ++k;
-  return k;
-}
-
 }  // namespace
-
-// The bits of a table word's fields; false: history and bias entries that do not fit one together.
-bool logits_word_fits(int64_t history, int64_t entries) {
-  return bits_of((uint32_t)(history + kMaxTree)) + 2 + bits_of((uint32_t)entries) <= 32;
-}
 
 // Threads, rows and chunks of a workgroup.  Large calls and long histories (every chunk looks at all of one) take
 // 1024 threads, whose chunks are 8192 tokens: 256 rows of 131072 after 2048 tokens 45 us, 52 with 512; 32 rows
@@ -300,7 +289,8 @@ bool logits_word_fits(int64_t history, int64_t entries) {
 // holds workgroups for follow one another in them, which starts the next one's loads early and keeps the history
 // in registers: 256 rows of 131072, 16 chunks each, 64 us one by one, 45 eight by eight.
 void choose_logits(LogitsParams& p) {
-  p.count_bits = bits_of((uint32_t)p.T + kMaxTree);
+  p.count_bits = 0;  // (with the other fields at most 32 bits: parse_graph sees to it)
+  while (((int64_t)p.T + kMaxTree) >> p.count_bits) ++p.count_bits;
   const int64_t all = (int64_t)p.batch * p.rows * p.cols_out;
   p.threads = all >= 1 << 24 || p.T > 8192 ? 1024 : p.cols_out > 4096 ? 512 : 256;
   const int64_t blocks = (int64_t)p.batch * ceil_div(p.cols_out, p.threads * 8), room = p.threads == 1024 ? 512 : 768;

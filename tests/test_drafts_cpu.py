@@ -42,6 +42,7 @@ def test_mxdense_accepts():
     (lambda: _graph("mxdense", {"x": ((1, 3, 5, 8), "bf16")}, ["x", "w"], {}, "bf16", [("w", np.zeros((4, 8), np.float32))]),
      "SHAPE", "2-D"),
     (lambda: _mx("mxdense_leaky", alpha=1.5), "PARSE", "alpha"),
+    (lambda: _mx("mxdense", x=(2 ** 24, 1), w=(24, 1)), "UNSUPPORTED", "2^32 4-bit codes"),
 ])
 def test_mxdense_refusals(gc, status, text):
     _expect(gc(), status, text)
@@ -112,6 +113,8 @@ def test_logits_accepts():
                   "penalties_drafts_bias_mask"):
         for dtype in ("bf16", "f32"):
             validate(*_rules(rules, dtype))
+    validate(*_rules("penalties", h=(2 ** 30 - 1024,)))
+    validate(*_rules("penalties_bias", h=(2 ** 22 - 1024,), bt=(1022,), bv=(2, 511)))
 
 
 @pytest.mark.parametrize("kw, status, text", [
@@ -135,6 +138,10 @@ def test_logits_accepts():
     (dict(x=(1, 2, 3, 4)), "SHAPE", "2-D"),
     (dict(x=(514, 70), t=(514,), p=(514,), m=(514 * 3,)), "UNSUPPORTED", "more than 256"),
     (dict(rules="mask", args=["x"]), "PARSE", "expects 2"),
+    # a table word: 30 bits to count 2^29 tokens, two marks and one bit for the entries; 22, two and 9
+    (dict(rules="penalties", h=(2 ** 30,)), "UNSUPPORTED", "536870912 tokens with 0"),
+    (dict(rules="penalties_bias", h=(2 ** 22,), bt=(1022,), bv=(2, 511)), "UNSUPPORTED", "2097152 tokens with 511"),
+    (dict(rules="bias", x=(1, 2 ** 30 + 1), batch=1, bt=(4,), bv=(1, 4)), "UNSUPPORTED", "2^30 columns"),
     (dict(rules="mask", args=["x", "x"]), "SHAPE", "must be an i32"),
 ])
 def test_logits_refusals(kw, status, text):
