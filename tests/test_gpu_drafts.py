@@ -125,6 +125,17 @@ def test_mxdense_every_tile(tile, dtype, monkeypatch):
     test_mxdense(33, 40, 40, dtype, "_bias")
 
 
+@pytest.mark.parametrize("tile, m, k, n, suffix", [
+    (0, 4400, 520, 4400, "_bias_add"), (0, 4400, 520, 4400, "_gelu"), (1, 2600, 1100, 4400, "_bias"),
+    (2, 2100, 1100, 2100, "_bias_add_relu"), (3, 3000, 1100, 3000, ""), (4, 3000, 1100, 1700, "_add"),
+    (5, 1500, 1100, 1500, "_bias_add_leaky"), (6, 800, 2100, 800, "_bias"),
+])
+def test_mxdense_more_tiles_than_workgroups(tile, m, k, n, suffix, monkeypatch):
+    """Workgroups that take several tiles, whose ring goes on from one to the next."""
+    monkeypatch.setenv("BYOC_MXDENSE_TILE", str(tile))
+    test_mxdense(m, k, n, "bf16", suffix)
+
+
 def test_mxdense_exact_products_are_exact():
     """Values on the grid: sums of few bits, which float32 holds whatever the order of the additions."""
     r = np.random.default_rng(5)
@@ -381,6 +392,10 @@ RULES = [
     (2, 257, 65, 20, 0, "f32", "penalties"),
     (4, 2, 50257, 700, 12, "f32", "penalties_drafts_bias_mask"),
     (130, 1, 260, 33, 2, "bf16", "penalties_bias_mask"),
+    (2, 1, 20000, 9000, 2500, "bf16", "penalties_bias_mask"),    # lists that no registers and no LDS hold
+    (120, 1, 150000, 40, 6, "bf16", "penalties_bias_mask"),      # chunks that follow one another in a workgroup
+    (24, 16, 50257, 30, 3, "f32", "penalties_drafts_bias"),      # the same of rows
+    (300, 1, 70001, 1, 0, "bf16", "mask"),
 ]
 
 
@@ -447,6 +462,16 @@ def test_logits_one_token_for_all():
     ins["n"] = (np.array([70000, 69999], np.int32), "i32")
     ins["pl"] = (np.array([0, 3], np.int32), "i32")
     _check_rules(ins, 2, "penalties_drafts_bias", "f32")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logits_every_token_met(dtype):
+    """More tokens of a chunk met than are listed."""
+    ins = _rules_case(2, 3, 9000, 12000, 40, dtype, "penalties_drafts_bias_mask")
+    r = np.random.default_rng(3)
+    ins["h"] = (np.concatenate([r.permutation(12000) % 9000 for _ in range(2)]).astype(np.int32), "i32")
+    ins["n"], ins["pl"] = (np.array([12000, 11000], np.int32), "i32"), (np.array([4000, 0], np.int32), "i32")
+    _check_rules(ins, 2, "penalties_drafts_bias_mask", dtype)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
