@@ -192,7 +192,7 @@ __device__ __forceinline__ int v_key(int row) {
 
 // Weights of 16 keys of one register group, rounded to bf16 for the matrix cores (a
 // relative 2^-8 each at most, as the values' own rounding): an output is then 0.0021 of its size off instead of the
-// 0.0016 of its own rounding.  Many rows take it, which are bound by the products: in two parts, as below,
+// 0.0016 of its own rounding.  Many rows without a tree take it, which are bound by the products: in two parts, as below,
 // causal 2 x 4096, 32 heads over 8 of 128, is 360 us instead of 266, and 8 x 449 over up to 1027, 12 of 64, 23.7
 // instead of 18.9.
 __device__ __forceinline__ uint4 pack_weights(const f32x16& s, int ks) {
@@ -202,18 +202,22 @@ __device__ __forceinline__ uint4 pack_weights(const f32x16& s, int ks) {
 
 // The same in two parts, off by a relative 2^-16 together: the upper bits, and the rest rounded to bf16.  Few rows
 // take it, whose time is that of the keys' and values' bytes (4 x 1 over up to 32768 keys, 32 heads over 8 of 128: 78 us
-// either way; 16 x 1 over up to 1500, 12 of 64, where latency counts: 13.8 us, 13.0 with one part).  The
+// either way; 16 x 1 over up to 1500, 12 of 64, where latency counts: 13.8 us, 13.0 with one part).  Trees of drafted
+// tokens take it too, so that a verified token has the error of one that was generated by itself: on long caches
+// 4 x 24 over up to 32768, 32 over 8 of 128, 103 us and an output 0.0017 of its size off, 101 and 0.0023 with one part;
+// shorter ones, bound by the products, pay for it (16 x 64 over up to 4096, 32 over 8 of 128: 106 us and 87; 8 x 64
+// over up to 2048, 12 of 64: 27.0 and 23.4).  The
 // rest is that of a weight 2^-20 larger, so that the parts of a weight above zero are both above zero (zero
 // times an infinite value would be NaN).
+__device__ __forceinline__ void pack_pair2(float w0, float w1, uint32_t* upper, uint32_t* rest) {
+  const float u0 = __uint_as_float(__float_as_uint(w0) & 0xFFFF0000u), u1 = __uint_as_float(__float_as_uint(w1) & 0xFFFF0000u);
+  *upper = __builtin_amdgcn_perm(__float_as_uint(w1), __float_as_uint(w0), 0x07060302u);
+  *rest = pack2_bf16(__builtin_fmaf(w0, 1.0f + 0x1p-20f, -u0), __builtin_fmaf(w1, 1.0f + 0x1p-20f, -u1));
+}
 __device__ __forceinline__ void pack_weights2(const f32x16& s, int ks, uint4* upper, uint4* rest) {
   uint32_t up[4], lo[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float w0 = s[8 * ks + 2 * e], w1 = s[8 * ks + 2 * e + 1];
-    const float u0 = __uint_as_float(__float_as_uint(w0) & 0xFFFF0000u), u1 = __uint_as_float(__float_as_uint(w1) & 0xFFFF0000u);
-    up[e] = __builtin_amdgcn_perm(__float_as_uint(w1), __float_as_uint(w0), 0x07060302u);
-    lo[e] = pack2_bf16(__builtin_fmaf(w0, 1.0f + 0x1p-20f, -u0), __builtin_fmaf(w1, 1.0f + 0x1p-20f, -u1));
-  }
+  for (int e = 0; e < 4; ++e) pack_pair2(s[8 * ks + 2 * e], s[8 * ks + 2 * e + 1], &up[e], &lo[e]);
   *upper = make_uint4(up[0], up[1], up[2], up[3]);
   *rest = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
@@ -677,19 +681,25 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   const int64_t sk2 = p.ldk2 * 2, sv2 = p.ldv2 * 2;
   const char* kb2 = TREE ? (const char*)p.k2 + (int64_t)b * p.q_len * sk2 + kh * p.D * 2 : nullptr;
   const char* vb2 = TREE ? (const char*)p.v2 + (int64_t)b * p.q_len * sv2 + kh * p.D * 2 : nullptr;
-  uint32_t ko[NI], vo[NI];
-#pragma unroll
-  for (int n = 0; n < NI; ++n) {
-    const int at = (n * NW + wave) * 64 + lane, r = at / CPR, x = at % CPR;
-    const int ck = x ^ k_key<CPR>(r), cv = x ^ v_key<CPR>(r);
-    ko[n] = ck * 8 < p.D ? (uint32_t)(r * (int)sk + ck * 16) : kOOB;
-    vo[n] = cv * 8 < p.D ? (uint32_t)(r * (int)sv + cv * 16) : kOOB;
-  }
-  // Fills of successive tiles, the base moving along (few scalar instructions: they are not hidden); rows past
-  // the length (and tiles past the end) read as zeros, whatever stands there
   char* const kt = lds + kg * 4 * TILE;  // two tiles of keys
   char* const vt = kt + 2 * TILE;        // and of values
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr(kt)) + wave * 1024;
+  // this lane's place in load n of a tile: its row, and the column's chunk of 16 bytes
+  auto place_in = [&](int n, auto values_tag) {
+    const int at = (n * NW + wave) * 64 + lane, r = at / CPR;
+    return int2{r, at % CPR ^ (decltype(values_tag)::value ? v_key<CPR>(r) : k_key<CPR>(r))};
+  };
+  auto offset = [&](int2 x, int stride) { return x.y * 8 < p.D ? (uint32_t)(x.x * stride + x.y * 16) : kOOB; };
+  uint32_t ko[TREE ? 1 : NI], vo[TREE ? 1 : NI];
+  if constexpr (!TREE) {
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      ko[n] = offset(place_in(n, std::false_type{}), (int)sk);
+      vo[n] = offset(place_in(n, std::true_type{}), (int)sv);
+    }
+  }
+  // Fills of successive tiles, the base moving along (few scalar instructions: they are not hidden); rows past
+  // the length (and tiles past the end) read as zeros, whatever stands there
   auto fill = [&](const char*& base, int64_t stride, int& left, const uint32_t* off, uint32_t at) {
     const int valid = min(kTileKeys, left);
     const i32x4 r4 = buffer_rsrc(base, valid > 0 ? (valid - 1) * (int)stride + p.D * 2 : 0);
@@ -702,28 +712,30 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   const char *kp = kb + (int64_t)first * kTileKeys * sk, *vp = vb + (int64_t)first * kTileKeys * sv;
   const int rest = t_end > first ? min(len, t_end * kTileKeys) - first * kTileKeys : 0;  // keys from there on
   int k_left = rest, v_left = rest;
-  // (a tree's drafted tiles, of rows any distance apart: their offsets are formed where they are used)
+  // A tree's tiles, of the cache or of the drafted keys, whose rows are other distances apart: the offsets are formed
+  // anew for each, since the weights' second part needs the registers (kept ones are spilled within the loop at 128 columns:
+  // 16 x 64 over up to 4096 151 us instead of 106).
   int k_at = first, v_at = first;  // the tiles that come next
-  auto fill_drafted = [&](const char* base, int64_t stride, int t, auto values_tag, uint32_t at) {
+  auto fill_tree = [&](int t, auto values_tag, uint32_t at) {
     constexpr bool VALUES = decltype(values_tag)::value;
-    const int j0 = (t - t_tree) * kTileKeys, valid = t < t_end ? min(kTileKeys, p.q_len - j0) : 0;
-    const i32x4 r4 = buffer_rsrc(base + j0 * stride, valid > 0 ? (valid - 1) * (int)stride + p.D * 2 : 0);
+    const bool drafted = t >= t_tree;
+    const int j0 = (drafted ? t - t_tree : t) * kTileKeys;
+    const int valid = t < t_end ? min(kTileKeys, (drafted ? p.q_len : len) - j0) : 0;
+    const int64_t stride = drafted ? (VALUES ? sv2 : sk2) : VALUES ? sv : sk;
+    const char* const base = (drafted ? (VALUES ? vb2 : kb2) : VALUES ? vb : kb) + j0 * stride;
+    const i32x4 r4 = buffer_rsrc(base, valid > 0 ? (valid - 1) * (int)stride + p.D * 2 : 0);
 #pragma unroll
-    for (int n = 0; n < NI; ++n) {
-      const int x = (n * NW + wave) * 64 + lane, r = x / CPR;
-      const int c = x % CPR ^ (VALUES ? v_key<CPR>(r) : k_key<CPR>(r));
-      lds_fill16(r4, at + n * NW * 1024, c * 8 < p.D ? (uint32_t)(r * (int)stride + c * 16) : kOOB);
-    }
+    for (int n = 0; n < NI; ++n) lds_fill16(r4, at + n * NW * 1024, offset(place_in(n, values_tag), (int)stride));
   };
   auto fill_k = [&](auto par_tag) {
     const uint32_t at = lds0 + decltype(par_tag)::value * TILE;
-    if (TREE && k_at >= t_tree) fill_drafted(kb2, sk2, k_at, std::false_type{}, at);
+    if constexpr (TREE) fill_tree(k_at, std::false_type{}, at);
     else fill(kp, sk, k_left, ko, at);
     k_at += KS;
   };
   auto fill_v = [&](auto par_tag) {
     const uint32_t at = lds0 + (2 + decltype(par_tag)::value) * TILE;
-    if (TREE && v_at >= t_tree) fill_drafted(vb2, sv2, v_at, std::true_type{}, at);
+    if constexpr (TREE) fill_tree(v_at, std::true_type{}, at);
     else fill(vp, sv, v_left, vo, at);
     v_at += KS;
   };
@@ -740,17 +752,15 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   int stop = t_wave;                                                          // the tiles from there on are left to add_keys
 
   // LDS offsets of this lane's operands in a tile: its key row at chunk h, whose other chunks are an XOR
-  // away (chunk 2 st + h at st << 5); and its part of V^T for 32-column block d, key group j
+  // away (chunk 2 st + h at st << 5); and its part of V^T for key group j, those of 32-column block d at d << 6
   const uint32_t ka = col * RB + ((h ^ k_key<CPR>(col)) << 4);
-  uint32_t va[DB][2];
+  uint32_t va[2];
 #pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int r = 8 * j + 4 * h + ((lane & 15) >> 2);
-      const int c = d * 4 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-      va[d][j] = r * RB + ((c ^ v_key<CPR>(r)) << 4) + (lane & 1) * 8;
-    }
+  for (int j = 0; j < 2; ++j) {
+    const int r = 8 * j + 4 * h + ((lane & 15) >> 2);
+    const int c = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    va[j] = r * RB + ((c ^ v_key<CPR>(r)) << 4) + (lane & 1) * 8;
+  }
   struct KFrag {
     uint4 a[KB];
   };
@@ -759,20 +769,24 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   };
   auto read_k = [&](auto par_tag, auto st_tag) {
     constexpr int par = decltype(par_tag)::value, st = decltype(st_tag)::value;
+    uint32_t at = ka;
+    if constexpr (TREE) asm("" : "+v"(at));  // (the XORs are not formed ahead of the loop over the tiles)
     KFrag f;
 #pragma unroll
-    for (int n = 0; n < KB; ++n) f.a[n] = *(const uint4*)(kt + (ka ^ (st << 5)) + par * TILE + n * 32 * RB);
+    for (int n = 0; n < KB; ++n) f.a[n] = *(const uint4*)(kt + (at ^ (st << 5)) + par * TILE + n * 32 * RB);
     return f;
   };
   auto read_v = [&](auto par_tag, auto ks_tag) {
     constexpr int par = decltype(par_tag)::value, ks = decltype(ks_tag)::value;
+    uint32_t at[2] = {va[0], va[1]};
+    if constexpr (TREE) asm("" : "+v"(at[0]), "+v"(at[1]));
     VFrag f;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
         f.a[d][j] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                  (lds_s16x4)(vt + va[d][j] + par * TILE + ks * 16 * RB)));
+                                                  (lds_s16x4)(vt + (at[j] ^ (d << 6)) + par * TILE + ks * 16 * RB)));
     return f;
   };
   auto mul_k = [&](const KFrag& f, auto st_tag, f32x16* s) {
@@ -789,16 +803,18 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   };
 
   // Tile t, in the LDS places of its parity: its scores s are there.  While the matrix cores form the next
-  // tile's, the vector ALU turns these into weights, a slice per step; operands are read two steps ahead.
+  // tile's, the vector ALU turns these into weights, a slice per step; operands are read two steps ahead (one, where
+  // the registers of a tree do not hold more).
   // Then the values are weighted.  (Past the last tile the next scores are of whatever the place holds, and
   // not used.)
+  constexpr int AHEAD = TREE && DC == 128 ? 1 : 2;
   auto step = [&](int t, auto par_tag, f32x16* s, f32x16* next) {
     constexpr std::integral_constant<int, 1 - decltype(par_tag)::value> other{};
     constexpr std::integral_constant<int, 0> c0{};
     constexpr std::integral_constant<int, 1> c1{};
-    KFrag kf[3];
+    KFrag kf[AHEAD + 1];
     kf[0] = read_k(other, c0);
-    kf[1] = read_k(other, c1);
+    if constexpr (AHEAD > 1) kf[1] = read_k(other, c1);
     const int k0 = t * kTileKeys;
     if (TREE && t >= t_tree) {
 #pragma unroll
@@ -839,9 +855,9 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
       constexpr int i = decltype(st)::value;
       constexpr int from = 16 * KB * i / QS, to = 16 * KB * (i + 1) / QS;  // weights of a slice
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (i + 2 < QS) kf[(i + 2) % 3] = read_k(other, std::integral_constant<int, i + 2>{});
+      if constexpr (i + AHEAD < QS) kf[(i + AHEAD) % (AHEAD + 1)] = read_k(other, std::integral_constant<int, i + AHEAD>{});
       if constexpr (i == QS - 1) vf[0] = read_v(par_tag, c0);
-      mul_k(kf[i % 3], st, next);
+      mul_k(kf[i % (AHEAD + 1)], st, next);
 #pragma unroll
       for (int e = from; e < to; ++e) {
         const float w = exp2_(__builtin_fmaf(s[e >> 4][e & 15], c2, -use));
@@ -849,15 +865,42 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
         sums[e & 1] += w;
       }
 #pragma unroll
-      for (int ks = from / 8; ks < to / 8; ++ks) pf[ks] = pack_weights(s[ks >> 1], ks & 1);
+      for (int ks = from / 8; !TREE && ks < to / 8; ++ks) pf[ks] = pack_weights(s[ks >> 1], ks & 1);
     });
     l += sums[0] + sums[1];
-    static_for<0, 2 * KB>([&](auto ks) {
-      constexpr int i = decltype(ks)::value;
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (i + 1 < 2 * KB) vf[(i + 1) & 1] = read_v(par_tag, std::integral_constant<int, i + 1>{});
-      mul_v(vf[i & 1], pf[i]);
-    });
+    if constexpr (TREE) {
+      // (the next 16 keys' weights are split while these are multiplied)
+      uint32_t up[2][4], low[2][4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pack_pair2(s[0][2 * e], s[0][2 * e + 1], &up[0][e], &low[0][e]);
+      static_for<0, 2 * KB>([&](auto ks) {
+        constexpr int i = decltype(ks)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (i + 1 < 2 * KB) vf[(i + 1) & 1] = read_v(par_tag, std::integral_constant<int, i + 1>{});
+        static_for<0, 2 * DB>([&](auto slot) {
+          constexpr int j = decltype(slot)::value, d = j % DB;
+          const uint32_t* const w = j < DB ? up[i & 1] : low[i & 1];
+          const VFrag& f = vf[i & 1];
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              as_bf16x8(make_uint4(f.a[d][0].x, f.a[d][0].y, f.a[d][1].x, f.a[d][1].y)),
+              as_bf16x8(make_uint4(w[0], w[1], w[2], w[3])), o[d], 0, 0, 0);
+          if constexpr (i + 1 < 2 * KB) {
+            constexpr int n = (i + 1) >> 1, at = 8 * ((i + 1) & 1);
+#pragma unroll
+            for (int e = 4 * j / (2 * DB); e < 4 * (j + 1) / (2 * DB); ++e)
+              pack_pair2(s[n][at + 2 * e], s[n][at + 2 * e + 1], &up[(i + 1) & 1][e], &low[(i + 1) & 1][e]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      });
+    } else {
+      static_for<0, 2 * KB>([&](auto ks) {
+        constexpr int i = decltype(ks)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (i + 1 < 2 * KB) vf[(i + 1) & 1] = read_v(par_tag, std::integral_constant<int, i + 1>{});
+        mul_v(vf[i & 1], pf[i]);
+      });
+    }
     __builtin_amdgcn_sched_barrier(0);
   };
 
