@@ -833,10 +833,13 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
     g.nodes.push_back(n);
   }
 
-  for (const Node& n : g.nodes)
-    for (int a : n.inputs())
-      if (g.values[a].param && a != n.strengths && a != n.bias_values)
-        return uerr("node " + n.name + ": input '" + g.values[a].name + "' is read as strengths or biases elsewhere");
+  // (by place: a node's strengths or biases may be its activation too)
+  for (const Node& n : g.nodes) {
+    const std::vector<int> in = n.inputs();
+    for (int a : in)
+      if (g.values[a].param && std::count(in.begin(), in.end(), a) != (a == n.strengths) + (a == n.bias_values))
+        return uerr("node " + n.name + ": input '" + g.values[a].name + "' is an activation, but is read as strengths or biases too");
+  }
   for (const IoDesc& in : g.inputs) {
     const Value& v = g.values[in.value];
     if (g.compute != DType::I8 && v.has_q)

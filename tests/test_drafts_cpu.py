@@ -163,6 +163,20 @@ def test_parameters_are_read_in_one_way():
     validate(g, c)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_parameters_are_no_activation_of_their_own_node(dtype):
+    """The logits themselves as strengths or bias values of the same node."""
+    g, c = _rules("penalties", dtype, x=(2, 3), args=["x", "h", "pl", "n", "x"])
+    _expect((g, c), "UNSUPPORTED" if dtype == "f32" else "SHAPE",
+            "read as strengths or biases" if dtype == "f32" else "must be an f32 input")
+    # (an f32 input of a bf16 graph, which the engine rounds where it is an activation)
+    for rules, args, x in (("penalties", ["x", "h", "pl", "n", "x"], (2, 3)), ("bias", ["x", "bt", "x"], (2, 4)),
+                           ("penalties_bias", ["x", "h", "pl", "n", "x", "bt", "x"], (2, 3))):
+        g, c = _rules(rules, dtype, x=x, args=args, **({"bt": (6,)} if rules == "penalties_bias" else {}))
+        g["inputs"][0]["dtype"] = "f32"
+        _expect((g, c), "UNSUPPORTED", "read as strengths or biases")
+
+
 def _steps():
     return [("step", dict(batch=2, drafts=3, cached=5, hidden=64, heads=4, kv_heads=2, ffn=96, vocab=77, history=9)),
             ("step_one", dict(batch=1, drafts=1, cached=1, hidden=64, heads=4, kv_heads=2, ffn=96, vocab=33, history=1)),
