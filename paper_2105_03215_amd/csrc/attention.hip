@@ -67,11 +67,19 @@ __device__ __forceinline__ int batch_len(const AttnParams& p, int b) {
   return p.lengths ? min(max(p.lengths[b], 0), p.k_len) : p.k_len;
 }
 
-// Tiles of the key axis of a sequence: of its keys and, after them, of a tree's drafted keys.
-__device__ __forceinline__ int key_tiles(int keys, int per) { return (keys + per - 1) / per; }
+// Tiles of the key axis of a sequence: of its keys and, after them, of a tree's drafted keys.  (Constants are
+// template arguments: as a function's, the compiler loses on the way that the sum does not overflow.)
+template <int PER>
+__device__ __forceinline__ int key_tiles(int keys) { return (keys + PER - 1) / PER; }
+__device__ __forceinline__ int key_tiles(const AttnParams& p, int keys) { return (keys + p.tile_keys - 1) / p.tile_keys; }
 template <bool TREE>
 __device__ __forceinline__ int batch_tiles(const AttnParams& p, int b) {
-  return key_tiles(batch_len(p, b), p.tile_keys) + (TREE ? key_tiles(p.q_len, p.tile_keys) : 0);
+  return key_tiles(p, batch_len(p, b)) + (TREE ? key_tiles(p, p.q_len) : 0);
+}
+// Of the drafted keys, the tiles that packed rows 0 .. rows - 1 see: a row's own key is the last on its path.
+template <int PER>
+__device__ __forceinline__ int drafted_tiles(const AttnParams& p, int rows) {
+  return key_tiles<PER>((min(rows, p.q_len * p.group) - 1) / p.group + 1);
 }
 
 // A tree's rows: its paths in LDS, which the workgroup forms where it has drafted keys, and this lane's query.
@@ -133,7 +141,7 @@ __device__ __forceinline__ Chunks lane_chunks(const AttnParams& p) {
 template <bool TREE>
 __device__ __forceinline__ Chunks uniform_chunks(const AttnParams& p, int b) {
   const int per = p.chunks / p.batch;
-  const int tiles = key_tiles(p.k_len, p.tile_keys) + (TREE ? key_tiles(p.q_len, p.tile_keys) : 0);
+  const int tiles = key_tiles(p, p.k_len) + (TREE ? key_tiles(p, p.q_len) : 0);
   return Chunks{b * per, per, (tiles + per - 1) / per};
 }
 // The sequence of chunk q, -1 if no sequence needs it.
@@ -362,10 +370,9 @@ __global__ __launch_bounds__(64 * NW) void attention_rows_kernel(AttnParams p) {
   const int lim_lo = uniform(seen_keys(p, len, cb * kCols));  // (rows see more keys further down)
   const int kend = uniform(seen_keys(p, len, min(cb * kCols + kCols, R) - 1));
   const int t0 = (chunk - ck.first) * ck.size;
-  // (a tree: drafted keys from tile t_tree on, a row's own the last it sees)
-  const int t_tree = key_tiles(len, kKeys);
-  const int t_end = min(t0 + ck.size, TREE ? t_tree + key_tiles((min(cb * kCols + kCols, R) - 1) / p.group + 1, kKeys)
-                                           : key_tiles(kend, kKeys));
+  // (a tree: drafted keys from tile t_tree on)
+  const int t_tree = key_tiles<kKeys>(len);
+  const int t_end = min(t0 + ck.size, TREE ? t_tree + drafted_tiles<kKeys>(p, cb * kCols + kCols) : key_tiles<kKeys>(kend));
 
   // this lane's part of its query row: 16-byte chunks 2 st + h
   constexpr int QS = DC * ES / 32;
@@ -659,10 +666,9 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   const int lim_hi = uniform(row0 < R ? seen_keys(p, len, min(row0 + 32, R) - 1) : 0);
   const int kend = uniform(seen_keys(p, len, min((tile + 1) * 32 * NW, R) - 1));
   const int t0 = (chunk - ck.first) * ck.size;
-  // (a tree: drafted keys from tile t_tree on, a row's own the last it sees)
-  const int t_tree = key_tiles(len, kTileKeys);
-  auto last_drafted = [&](int rows) { return t_tree + key_tiles((min(rows, R) - 1) / p.group + 1, kTileKeys); };
-  const int t_end = min(t0 + ck.size, TREE ? last_drafted((tile + 1) * 32 * NW) : key_tiles(kend, kTileKeys));
+  // (a tree: drafted keys from tile t_tree on)
+  const int t_tree = key_tiles<kTileKeys>(len);
+  const int t_end = min(t0 + ck.size, TREE ? t_tree + drafted_tiles<kTileKeys>(p, (tile + 1) * 32 * NW) : key_tiles<kTileKeys>(kend));
 
   uint4 qf[QS];
   const int i = row / p.group, g = row - i * p.group;
@@ -746,7 +752,7 @@ __global__ __launch_bounds__(256, DP * KS <= 128 ? 2 : 1) void attention_tiles_k
   float m = -INFINITY, l = 0.0f;
   const float c2 = p.scale * 1.44269504088896340736f;
   // tiles that this wave's rows see, and the first that some rows see a part of
-  const int t_wave = min(t_end, TREE ? (row0 < R ? last_drafted(row0 + 32) : 0) : key_tiles(lim_hi, kTileKeys));
+  const int t_wave = min(t_end, TREE ? (row0 < R ? t_tree + drafted_tiles<kTileKeys>(p, row0 + 32) : 0) : key_tiles<kTileKeys>(lim_hi));
   const int masked = TREE ? t_tree : p.causal && p.q_len > 1 ? lim_lo / kTileKeys : INT_MAX;
   TreeRow tree{};
   int stop = t_wave;                                                          // the tiles from there on are left to add_keys
@@ -1037,12 +1043,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
   const int lim_lo = uniform(seen_keys(p, len, min(row0, R - 1)));  // (rows see more keys further down)
   const int lim_hi = uniform(row0 < R ? seen_keys(p, len, min(row0 + 32, R) - 1) : 0);
   const int kend = uniform(seen_keys(p, len, min((tile + 1) * 32 * NW, R) - 1));
-  // (a tree: drafted keys from tile t_tree on, a row's own the last it sees)
-  const int t_tree = key_tiles(len, kKeys);
-  auto last_drafted = [&](int rows) { return t_tree + key_tiles((min(rows, R) - 1) / p.group + 1, kKeys); };
-  const int t_end = TREE ? last_drafted((tile + 1) * 32 * NW) : key_tiles(kend, kKeys);
+  // (a tree: drafted keys from tile t_tree on)
+  const int t_tree = key_tiles<kKeys>(len);
+  const int t_end = TREE ? t_tree + drafted_tiles<kKeys>(p, (tile + 1) * 32 * NW) : key_tiles<kKeys>(kend);
   // tiles that this wave's rows see
-  const int t_wave = min(t_end, TREE ? (row0 < R ? last_drafted(row0 + 32) : 0) : key_tiles(lim_hi, kKeys));
+  const int t_wave = min(t_end, TREE ? (row0 < R ? t_tree + drafted_tiles<kKeys>(p, row0 + 32) : 0) : key_tiles<kKeys>(lim_hi));
 
   uint4 qf[QS];
   const int i = row / p.group, g = row - i * p.group;
@@ -1063,7 +1068,23 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
   const uint32_t lds0 = uniform(lds_addr(lds)) + wave * 1024;
   // a tile of keys and values; rows past the length (and tiles past the end) read as zeros, whatever stands there
   auto fill = [&](int par, int t) {
-    const bool drafted = TREE && t >= t_tree;
+    const int64_t k0 = (int64_t)t * kKeys;
+    const int n = t < t_end ? min(kKeys, len - t * kKeys) : 0;
+    const i32x4 rk = buffer_rsrc(kb + k0 * sk, n > 0 ? (n - 1) * (int)sk + p.D * 4 : 0);
+    const i32x4 rv = buffer_rsrc(vb + k0 * sv, n > 0 ? (n - 1) * (int)sv + p.D * 4 : 0);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int at = (j * NW + wave) * 64 + lane, r = at / CPR, x = at % CPR;
+      const int ck = x ^ k_key<CPR>(r), cv = x ^ v_key<CPR>(r);
+      lds_fill16(rk, lds0 + par * 2 * TILE + j * NW * 1024, ck * 4 < p.D ? (uint32_t)(r * (int)sk + ck * 16) : kOOB);
+      lds_fill16(rv, lds0 + (par * 2 + 1) * TILE + j * NW * 1024, cv * 4 < p.D ? (uint32_t)(r * (int)sv + cv * 16) : kOOB);
+    }
+  };
+  // The same of a tree's tiles, of the cache or of the drafted keys.  (Apart from fill: with the choice of places in it, though a
+  // constant one, the scheduler orders the loop without a tree otherwise, and 16 x 300 over 200, 12 of 256, took 246 us
+  // instead of 241.)
+  auto fill_tree = [&](int par, int t) {
+    const bool drafted = t >= t_tree;
     const int k0 = (drafted ? t - t_tree : t) * kKeys;
     const int n = t < t_end ? min(kKeys, (drafted ? p.q_len : len) - k0) : 0;
     const int64_t ks = drafted ? sk2 : sk, vs = drafted ? sv2 : sv;
@@ -1137,7 +1158,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
     }
   };
 
-  fill(0, 0);
+  if constexpr (TREE) fill_tree(0, 0);
+  else fill(0, 0);
   if constexpr (TREE) {
     tree.paths = form_paths<256>(p.parents + (int64_t)b * p.q_len, p.q_len, tree_lds);
     tree.query = row < R ? i : -1;
@@ -1145,7 +1167,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
   for (int t = 0, par = 0; t < t_end; ++t, par ^= 1) {
     // tile t has landed for every wave, and every wave is done with the one before, whose place t + 1 takes
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    fill(par ^ 1, t + 1);
+    if constexpr (TREE) fill_tree(par ^ 1, t + 1);
+    else fill(par ^ 1, t + 1);
     if (t >= masked && t < stop && holds_not_finite<false, TILE>(lds + (par * 2 + 1) * TILE)) stop = t;
     if (t < stop) compute(par, t);
   }
@@ -1176,17 +1199,20 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiles_f32_ke
 // Joins the chunks of a packed row: D / 4 lanes (of 64 / 32 / 16), 4 columns each, and `split` such groups a
 // row that take the chunks in turn, so that many chunks are on their way together where there are few rows
 // (one token over 32768 keys, 16 heads on one of 128, 16 rows of 85 chunks: 39 us by one group, 17 by eight).
-__global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p, int lanes, int split) {
+template <bool TREE>
+__global__ __launch_bounds__(256) void attention_join_kernel(int lanes, int split, AttnParams p) {
   __shared__ float4 part[256];
   __shared__ float2 part_ml[256];
   const int R = p.q_len * p.group;
   // rows of one sequence per workgroup row (blockIdx.y), so that a wave has one set of chunks
   const int b = blockIdx.y;
-  const int len = batch_len(p, b);
-  const int2 ck = len > 0 || p.tree ? ((const int2*)p.ws)[b] : make_int2(0, 0);  // first chunk, count
+  // (formed first, so that these arguments come with the others: 4 x 1 over up to 32768 keys, 32 heads over 8 of 128,
+  // 78.35 us, 78.5 with the lengths first)
   const int slot = threadIdx.x / lanes, g0 = slot % split;
   const int at = blockIdx.x * (256 / lanes / split) + slot / split;  // (key head, packed row)
   const int c = threadIdx.x % lanes * 4;
+  const int len = batch_len(p, b);
+  const int2 ck = TREE || len > 0 ? ((const int2*)p.ws)[b] : make_int2(0, 0);  // first chunk, count
   const bool live = at < p.kv_heads * R && c < p.D;
   const int kh = live ? at / R : 0, row = live ? at - kh * R : 0;
   // eight chunks at a time, their loads on the way together
@@ -1243,7 +1269,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p, int l
     }
   }
   if (!live) return;
-  const bool any = p.tree || seen_keys(p, len, row) > 0;
+  const bool any = TREE || seen_keys(p, len, row) > 0;
   const int i = row / p.group, g = row - i * p.group;
   const int64_t out = (b * (int64_t)p.q_len + i) * p.ldy + (kh * p.group + g) * p.D + c;
 #pragma unroll
@@ -1383,7 +1409,8 @@ hipError_t launch_attention_join(const AttnParams& p, hipStream_t s) {
   int split = 1;
   while (split < 256 / lanes && split * 8 < p.chunks && rows * p.batch * split * lanes < 256 * 256) split *= 2;
   const dim3 grid(ceil_div(rows, 256 / lanes / split), p.batch);
-  attention_join_kernel<<<grid, 256, 0, s>>>(p, lanes, split);
+  if (p.tree) attention_join_kernel<true><<<grid, 256, 0, s>>>(lanes, split, p);
+  else attention_join_kernel<false><<<grid, 256, 0, s>>>(lanes, split, p);
   return hipGetLastError();
 }
 

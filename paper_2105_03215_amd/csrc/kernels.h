@@ -563,19 +563,23 @@ struct AttnParams {
   const void* q;       // [batch * q_len][ldq], head h at column h D
   const void* k;       // [batch * k_len][ldk], head at column (h / group) D
   const void* v;
-  const void* k2;      // a tree's drafted keys and values: [batch * q_len][ldk2]
-  const void* v2;
   const int* lengths;  // [batch] or nullptr (k_len)
-  const int* parents;  // [batch * q_len] or nullptr (no tree)
   void* y;             // [batch * q_len][ldy]
   float* ws;           // attn_workspace() bytes when chunks > batch
-  int64_t ldq, ldk, ldv, ldk2, ldv2, ldy;
+  int64_t ldq, ldk, ldv, ldy;
   int batch, q_len, k_len, kv_heads, group, D;
-  int causal, tree;
+  int causal;
   int tile_rows, tile_keys;  // packed query rows and keys of a tile (set with chunks by choose_attention)
   int chunks;                // of the key axes of all sequences; batch: one each, no join
   float scale;
   int f32;
+  // A tree's.  (Last, so that the kernels without one find theirs together, in few scalar loads: 16 x 1 over up to
+  // 1500 keys, 12 heads of 64, 14.1 us, 14.3 with these in between.)
+  int tree;
+  const void* k2;      // drafted keys and values: [batch * q_len][ldk2]
+  const void* v2;
+  const int* parents;  // [batch * q_len] or nullptr (no tree)
+  int64_t ldk2, ldv2;
 };
 void choose_attention(AttnParams& p);  // the kernel and the split of the key axes
 const char* attention_name(const AttnParams& p);
