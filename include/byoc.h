@@ -94,7 +94,7 @@
  *                     products of these summed in float32, then bias, residual and
  *                     activation.  A row that holds an infinity or a NaN gives NaN; terms
  *                     whose magnitudes sum to more than float32 holds may give an infinity or a NaN.
- *                     K <= 131072.
+ *                     K <= 131072, and M and N by K, each rounded up to a multiple of 256, below 2^32.
  *   attention_tree    queries [B T, *], keys and values of a cache [B Lk, *] each, drafted
  *                     keys and values [B T, *] each, lengths [B] (i32), parents [B T] (i32)
  *                     -> [B T, heads D]: attention of T <= 256 drafted tokens of each
@@ -125,6 +125,7 @@
  *     mask            words [B R ceil(V / 32)] (i32): token t of a row may be chosen where bit
  *                     t % 32 of the row's word t / 32 is set, else its logit is -inf
  *                     Tokens outside [0, V) are passed over, so that -1 marks an unused place.
+ *                     V <= 2^30, and the bits of T + 256 and of E (one at least) together at most 30.
  *       attrs batch B.
  *     The f32 inputs are read in place, aligned to 4 bytes, and are not rounded in bf16 graphs.
  * Buffers that these composites read or write directly are aligned to 16 bytes.

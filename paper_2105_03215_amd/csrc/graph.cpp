@@ -8,6 +8,7 @@
 #include <sstream>
 
 #include "json.h"
+#include "limits.h"
 
 namespace byoc {
 namespace {
@@ -143,7 +144,6 @@ Status attr_positive(const JsonValue* attrs, const char* key, const std::string&
 }
 
 constexpr int kMaxHeads = 4096;
-constexpr int kMaxDrafts = 256;  // drafted tokens of a sequence, whose paths the kernels hold as bits in LDS
 constexpr int64_t kMaxCols = 1 << 22;  // columns of a row that the packed-head kernels address (tiles of 64 rows in 31 bits)
 
 // The angle per position of each pair, and the factor on the rotated values.
@@ -656,8 +656,8 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
                       " differ in rows from the queries " + shape_str(xs));
         if (shp(n.parents) != std::vector<int64_t>{xs[0]})
           return serr(where + ": parents shape " + shape_str(shp(n.parents)) + " != [" + std::to_string(xs[0]) + "]");
-        if (n.q_len > kMaxDrafts)
-          return uerr(where + ": more than " + std::to_string(kMaxDrafts) + " drafted tokens of a sequence");
+        if (n.q_len > kMaxTree)
+          return uerr(where + ": more than " + std::to_string(kMaxTree) + " drafted tokens of a sequence");
       }
       // packed rows, workgroups and split results are counted in 31 bits
       if ((int64_t)n.q_len * (n.heads / n.kv_heads) > kMaxElems / 64 || xs[0] * n.heads > kMaxElems / 64)
@@ -685,8 +685,8 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
       if (n.drafts) {
         if (!(st = expect(n.draft_tokens, "drafted tokens", {xs[0]})).ok()) return st;
         if (!(st = expect(n.parents, "parents", {xs[0]})).ok()) return st;
-        if (rows > kMaxDrafts)
-          return uerr(where + ": more than " + std::to_string(kMaxDrafts) + " drafted tokens of a sequence");
+        if (rows > kMaxTree)
+          return uerr(where + ": more than " + std::to_string(kMaxTree) + " drafted tokens of a sequence");
       }
       if (n.has_bias) {
         if (shp(n.bias_tokens)[0] % b)
@@ -700,7 +700,7 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
         return k;
       };
       const int64_t tokens = n.penalties ? shp(n.history)[0] / b : 0, entries = n.has_bias ? shp(n.bias_tokens)[0] / b : 0;
-      if (bits(tokens + kMaxDrafts) + 2 + std::max(1, bits(entries)) > 32)
+      if (bits(tokens + kMaxTree) + 2 + std::max(1, bits(entries)) > 32)
         return uerr(where + ": a history of " + std::to_string(tokens) + " tokens with " + std::to_string(entries) +
                     " bias entries");
       if (xs[1] > 1 << 30) return uerr(where + ": more than 2^30 columns");
@@ -718,7 +718,7 @@ Status parse_graph(const char* text, size_t len, const byoc_const* consts, int32
       n.macs = xs[0] * ws[0] * xs[1];
       if (n.op == OpKind::QDense && xs[1] > 131072)  // 127^2 K stays under 2^31
         return uerr(where + ": reduction of more than 131072 elements on 8-bit codes");
-      if (n.op == OpKind::MxDense && xs[1] > 131072)  // 256 rows of a tile are addressed in 31 bits
+      if (n.op == OpKind::MxDense && xs[1] > 131072)  // the float32 sum of K terms stays within K 2^-23 = 2^-6 of their magnitudes
         return uerr(where + ": reduction of more than 131072 elements on 4-bit codes");
       // (codes, padded to 256 along both axes and two a byte, are addressed in 31 bits)
       if (n.op == OpKind::MxDense && (std::max(xs[0], ws[0]) + 255) / 256 * 256 * ((xs[1] + 255) / 256 * 256) >= int64_t(1) << 32)

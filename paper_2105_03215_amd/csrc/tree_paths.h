@@ -4,10 +4,9 @@
 #pragma once
 
 #include "device_common.h"
+#include "limits.h"
 
 namespace byoc {
-
-constexpr int kMaxTree = 256;  // drafted tokens of a sequence
 
 // LDS of the paths of n tokens: `words` words a token (bit k: token k is on its path,
 // the token itself included), and the tokens' next ancestors.
