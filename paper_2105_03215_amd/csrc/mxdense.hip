@@ -363,9 +363,9 @@ __global__ __launch_bounds__(64 * WM * WN) void mxdense_kernel(MxDenseParams p) 
     }
   };
   const ActClamp ac = act_clamp_of(p.act, p.alpha);
-  // Epilogue: lane = row of each row tile, 8 consecutive channels per pair of channel tiles.  It is bound by the
-  // vector ALU (at 4 cycles an instruction, 550 cycles for 8 values with their checks and a residual of zeros: 7.4 us a
-  // tile of 256 x 256 beside the 20.5 us of its product), so that whole tiles without a residual or an activation
+  // Epilogue: lane = row of each row tile, 8 consecutive channels per pair of channel tiles.  With every check
+  // it is bound by the vector ALU (at 4 cycles an instruction, 550 cycles for 8 values with a residual of zeros: 7.4 us a
+  // tile of 256 x 256 beside the 25 us of a product over 4096), so that whole tiles without a residual or an activation
   // have forms of their own.
   constexpr int NP = TN / 2, BATCH = F32 ? 1 : TM * NP > 16 ? 16 / NP : TM;  // (rows whose residuals are on their way together)
   auto epilogue = [&](auto mode_tag, auto res_tag, auto whole_tag) {
@@ -601,11 +601,13 @@ hipError_t launch_one(MxDenseParams p, hipStream_t s) {
 
 // Tiles (BM, BN, waves along each, steps of a stage, ring stages) and what they cost in microseconds: a step of 128
 // codes while at most one workgroup runs per CU or all slots (occ per CU) are busy, and a round's start and end.
-// Fitted to 22 shapes from 1 x 8192 x 12288 to 8192 x 4096 x 8192, on each of which the choice is the fastest
-// tile.  8192 x 4096 x 8192 with its quantization: 141 us as 256x256, 164 as 256x128, 176 as 128x128 twice a CU; the
-// product alone takes 20.3 us a tile for 16.6 of matrix instructions at the 8.3 PFLOP/s that they reach without
-// operands to wait for.  (256x128 twice a CU, with 4 waves of 128 x 64 each: 233 us, as the LDS and the L2 then feed 41 bytes a
-// cycle.)  With random codes the same product is a quarter slower than with equal ones: the clock gives way.
+// Fitted to 22 shapes from 1 x 8192 x 12288 to 8192 x 4096 x 8192; the choice is the fastest tile, or within 1% of it, on 20
+// of them, and 6% behind 128x64 on 300 x 4096 x 4096 and 128 x 4096 x 12288 (13.6 us for 12.85, 13.8 for 13.0), where
+// the model has the two alike.  8192 x 4096 x 8192 of random rows with its quantization: 151 us as 256x256, 172 as 256x128,
+// 182 as 128x128 twice a CU; of that the product takes 135, four tiles in a row of 32 steps of 0.78 us each (0.52 is what the
+// matrix instructions need without operands to wait for) and an end of 9 us, which all workgroups
+// reach together: the matrix cores are busy for 58% of the cycles, at a clock of 1.7 GHz.  (256x128 twice a CU, with 4 waves of
+// 128 x 64 each: 233 us, as the LDS and the L2 then feed 41 bytes a cycle.)
 //   id BM BN WM WN KS NS  occ  lone  busy  round
 #define BYOC_MXDENSE_TILES(X)                       \
   X(0, 256, 256, 2, 4, 1, 4, 1, 0.535, 0.681, 7.46)  \
